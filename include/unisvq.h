@@ -29,7 +29,7 @@
  *   - Thread-safe: no global mutable state besides the kernels' dynamic-LDS
  *     limits, raised on first use once per (kernel, device) -- on the device
  *     current when the call is made.
- *   - Shapes: N % 16 == 0, K % 128 == 0, N >= 16, K >= 128, M >= 1.
+ *   - Shapes of the products: N % 16 == 0, K % 128 == 0, N >= 16, K >= 128, M >= 1.
  *
  * ---------------------------------------------------------------------------
  * Packed weight format, version 1 (bytes little endian)
@@ -560,6 +560,178 @@ int unisvq_rht(int64_t n, int64_t M, const void* x, int x_dtype, const int8_t* s
  *             unisvq_gemv */
 int unisvq_gemv_rht_batched(const unisvq_gemv_problem* problems, int count, int64_t M, int x_dtype, int y_dtype,
                             const int8_t* const* signs, void* stream);
+
+/* ---- The attention block around the products ----
+ * Between a decoder layer's q/k/v product and its o product: rotary
+ * positions, a paged key/value cache (16-bit, 8-bit or 4-bit), attention of
+ * new tokens over that cache and attention over prompts.  Rows of activations
+ * are given as (pointer, token stride, head stride): element d of head h of
+ * token t is at t * token_stride + h * head_stride + d, strides in elements,
+ * so that the parts of one fused q/k/v row serve as they are.  Such pointers
+ * are 16-byte aligned and their strides multiples of 8 elements
+ * (UNISVQ_EALIGN otherwise); dtype F16 or BF16.
+ * What the device holds (positions, lengths, page numbers) cannot be checked
+ * before a launch: the kernels check it, and never access memory outside the
+ * buffers described by the arguments, whatever it says. */
+
+/* Cosines and sines of rotary positions: fp32 table[positions][2][rot / 2]
+ * (cosines, then sines), angle position * f_i for pair i, computed in fp64
+ * and rounded once.  f_i = theta^(-2i / rot), and for long contexts
+ *   f_i <- (1 - g) f_i / factor + g f_i,  g = clamp((r - low) / (high - low), 0, 1),
+ * r = original * f_i / (2 pi) the turns of pair i over the original context;
+ * original = 0: g = 0 (positions scaled linearly; factor 1: not at all).
+ * Both are multiplied by `magnitude`.
+ *   positions  1..2^24; rot  even, 2..1024; theta, factor > 0; original >= 0,
+ *   and high > low where original > 0 (UNISVQ_EINVAL otherwise)
+ *   table      device fp32, 16-byte aligned */
+int unisvq_rope_table(int64_t positions, int64_t rot, double theta, double factor, double low, double high,
+                      double original, double magnitude, float* table, void* stream);
+
+/* Rotary positions: the first `rot` dims of every head rotated in pairs by
+ * the table row of the token's position, the others copied:
+ *   (a, b) -> (a c - b s, b c + a s), in fp32 with every product and sum
+ *   rounded by itself, then once to dtype.
+ * Pair i is dims (i, i + rot / 2), or (2i, 2i + 1) where `interleaved`.
+ * `inverse` turns the other way (s -> -s): the transpose of the rotation and
+ * so its gradient.
+ *   tokens >= 0, heads >= 1; head_dim a multiple of 16 to 1024; rot a
+ *   multiple of 16, 16..head_dim (UNISVQ_EUNSUP otherwise)
+ *   positions  device int32 [tokens]; a token whose position is outside
+ *              [0, table_positions) gets NaN in its rotated dims
+ *   table      device fp32 [table_positions][2][rot / 2], 16-byte aligned
+ *   y          may be x with the same strides, and may not overlap it otherwise */
+int unisvq_rope(int64_t tokens, int64_t heads, int64_t head_dim, int64_t rot, int interleaved, int inverse,
+                const void* x, int64_t x_token_stride, int64_t x_head_stride, const int32_t* positions,
+                const float* table, int64_t table_positions, void* y, int64_t y_token_stride, int64_t y_head_stride,
+                int dtype, void* stream);
+
+/* What a cache holds of every key and value.  I8: signed codes c and one fp32
+ * scale a token and head, value c * scale; scale = a / 127, a the largest
+ * magnitude of the head's values.  I4: two codes a byte (even dim in the low
+ * half), stored as c + 8, and two bf16 scales a token and head, one for each
+ * half of the head (dims below and from head_dim / 2), scale = bf16(a / 7).
+ * c = round-to-even(x * (1 / scale)), clamped to +-127 or +-7.  a < 1e-30:
+ * scale 0 and codes 0.  Inf or NaN among the values: scale NaN. */
+typedef enum {
+    UNISVQ_CACHE_F16 = 0,
+    UNISVQ_CACHE_BF16 = 1,
+    UNISVQ_CACHE_I8 = 2,
+    UNISVQ_CACHE_I4 = 3
+} unisvq_cache_kind;
+
+/* A paged cache.  Pools [pages][kv_heads][page_tokens][head_dim] of 2, 1 or
+ * 1/2 bytes an element; a page holds page_tokens consecutive tokens of one
+ * sequence.  A page table, int32 [sequences][table_width], names the page of
+ * tokens page_tokens * i .. page_tokens * (i + 1) - 1 of a sequence in column
+ * i; entries outside [0, pages) are places without a page. */
+typedef struct {
+    int64_t pages;        /* 1..2^31 - 1 */
+    int64_t page_tokens;  /* 16, 32, 64, 128 or 256 */
+    int64_t kv_heads;     /* 1..65535 */
+    int64_t head_dim;     /* 64 or 128 */
+    int kind;             /* unisvq_cache_kind */
+    void* k;              /* device, 16-byte aligned */
+    void* v;
+    void* k_scales;       /* device [pages][kv_heads][page_tokens] of 4 bytes (one fp32, or two bf16), */
+    void* v_scales;       /* 16-byte aligned; NULL for the 16-bit kinds */
+} unisvq_cache;
+
+/* Write the keys and values of new tokens to the cache, rotating keys (and
+ * queries) to their positions in the same launch.
+ *   page_table  device int32 [sequences][table_width]
+ *   seqs        device int32 [tokens]: the sequence of each token; NULL: token
+ *               t belongs to sequence t
+ *   positions   device int32 [tokens]: its position in the sequence.  A token
+ *               whose sequence or position has no page is not stored (so
+ *               position -1 marks a padding token)
+ *   k, v        device [tokens][kv_heads][head_dim] of x_dtype
+ *   q           device [tokens][q_heads][head_dim], or NULL (q_heads 0)
+ *   q_out       q rotated, x_dtype; may be q with the same strides
+ *   rope_table  as unisvq_rope (keys and queries outside it become NaN), or
+ *               NULL: nothing is rotated (then q is copied)
+ * Keys are rotated in fp32 as by unisvq_rope and quantised without rounding
+ * in between; 16-bit kinds round once.  x_dtype F16 or BF16; a 16-bit kind
+ * has to be x_dtype's (UNISVQ_EUNSUP).  Two tokens of one call with the same
+ * place: either is stored, or a mix of both. */
+int unisvq_cache_append(const unisvq_cache* cache, const int32_t* page_table, int64_t sequences, int64_t table_width,
+                        int64_t tokens, const int32_t* seqs, const int32_t* positions, const void* k,
+                        int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
+                        int64_t v_head_stride, const void* q, int64_t q_heads, int64_t q_token_stride,
+                        int64_t q_head_stride, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
+                        int x_dtype, const float* rope_table, int64_t table_positions, int64_t rot, int interleaved,
+                        void* stream);
+
+/* Read tokens of the cache back as packed rows, value = code * scale in fp32
+ * rounded once to dtype.  Row r, cu[b] <= r < cu[b + 1], is token
+ * starts[b] + r - cu[b] of sequence b.
+ *   starts  device int32 [sequences], or NULL: 0
+ *   cu      device int32 [sequences + 1], not decreasing, cu[0] = 0
+ *   tokens  rows of k_out and v_out; rows from cu[sequences] on are left as
+ *           they are, rows of places without a page become NaN
+ *   k_out, v_out  device [tokens][kv_heads][head_dim] of dtype F16 or BF16 */
+int unisvq_cache_read(const unisvq_cache* cache, const int32_t* page_table, int64_t sequences, int64_t table_width,
+                      const int32_t* starts, const int32_t* cu, int64_t tokens, void* k_out, int64_t k_token_stride,
+                      int64_t k_head_stride, void* v_out, int64_t v_token_stride, int64_t v_head_stride, int dtype,
+                      void* stream);
+
+/* Attention of the newest q_len tokens of every sequence over its cache
+ * (which holds their keys and values already):
+ *   out = softmax(scale * q K^T) V,
+ * token j of q_len seeing positions below len - q_len + 1 + j.  Query head h
+ * uses key/value head h / (q_heads / kv_heads).
+ *   lens       device int32 [sequences], the new tokens among them; a length
+ *              is taken as at most table_width * page_tokens.  A token that
+ *              sees nothing (length 0, an empty slot of the batch) gets zeros
+ *              and lse = -inf; places without a page are not seen
+ *   max_len    what the lengths are at most, which sets how the cache is split
+ *              over the GPU; 0: the page table's whole width.  Longer
+ *              sequences are served all the same
+ *   q_len      1..16; q_heads a multiple of kv_heads
+ *   q, out     device [sequences * q_len][q_heads][head_dim], x_dtype; a
+ *              16-bit kind has to be x_dtype's (UNISVQ_EUNSUP)
+ *   lse        device fp32 [sequences * q_len][q_heads] or NULL: the log of
+ *              the sum of exp(scale * q k), to join this with other parts
+ *   workspace  device, >= unisvq_attn_decode_workspace_bytes(...) bytes,
+ *              16-byte aligned (UNISVQ_EWORKSPACE / UNISVQ_EALIGN); may be
+ *              NULL when that size is 0.  Overwritten.
+ * Scores, softmax and sums are fp32; the products run on the matrix cores in
+ * 16 bits (8- and 4-bit codes exactly, the weights of the values rounded to
+ * f16, or to bf16 for a BF16 cache).  Long sequences are split over
+ * workgroups and joined in a fixed order by a second launch. */
+size_t unisvq_attn_decode_workspace_bytes(int64_t sequences, int64_t q_len, int64_t q_heads, int64_t kv_heads,
+                                          int64_t head_dim, int64_t max_len);
+int unisvq_attn_decode(const unisvq_cache* cache, const int32_t* page_table, int64_t sequences, int64_t table_width,
+                       const int32_t* lens, int64_t max_len, int64_t q_len, int64_t q_heads, const void* q,
+                       int64_t q_token_stride, int64_t q_head_stride, int x_dtype, float scale, void* out,
+                       int64_t out_token_stride, int64_t out_head_stride, float* lse, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* Attention over prompts: packed sequences of different lengths.  Sequence b
+ * has queries cu_q[b] .. cu_q[b + 1] - 1 and keys and values cu_k[b] ..
+ * cu_k[b + 1] - 1; with nq and nk of them, query i sees all nk keys, or where
+ * `causal` those up to i + nk - nq (the last query sees all: nk > nq is a
+ * chunk of a prompt after what was cached of it).  A query that sees nothing
+ * gets zeros and lse = -inf.
+ *   cu_q, cu_k  device int32 [sequences + 1], not decreasing, first entry 0;
+ *               entries are taken as at most q_tokens and k_tokens.  Queries
+ *               from cu_q[sequences] on are left as they are
+ *   q, out      device [q_tokens][q_heads][head_dim]; k, v [k_tokens][kv_heads][head_dim]
+ *   head_dim    64 or 128; q_heads a multiple of kv_heads
+ *   lse         device fp32 [q_tokens][q_heads] or NULL, as above
+ *   workspace   device, >= unisvq_attn_prompt_workspace_bytes(...) bytes,
+ *               16-byte aligned; may be NULL when that size is 0 (it is where
+ *               the queries fill the GPU; few queries before many keys are
+ *               split along the keys).  Overwritten.
+ * fp32 scores, softmax and sums; the softmax weights are rounded to dtype
+ * for their product with v. */
+size_t unisvq_attn_prompt_workspace_bytes(int64_t sequences, int64_t q_tokens, int64_t k_tokens, int64_t q_heads,
+                                          int64_t kv_heads, int64_t head_dim);
+int unisvq_attn_prompt(int64_t sequences, int64_t q_tokens, int64_t k_tokens, const int32_t* cu_q,
+                       const int32_t* cu_k, int64_t q_heads, int64_t kv_heads, int64_t head_dim, const void* q,
+                       int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
+                       int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride, int dtype,
+                       int causal, float scale, void* out, int64_t out_token_stride, int64_t out_head_stride,
+                       float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- Bandwidth reference (not part of the method) ----
  * A plain read of `count` device byte ranges in one launch, with the 16-byte

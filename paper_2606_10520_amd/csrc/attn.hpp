@@ -1,0 +1,201 @@
+// Internal declarations of the attention block: rotary positions, the paged
+// cache and attention (attn_api.hip validates; rope.hip, cache.hip,
+// attn_decode.hip and attn_prompt.hip launch).
+#pragma once
+
+#include <type_traits>
+
+#include "common.hpp"
+
+namespace unisvq {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// Rows of activations: element d of head h of token t at p + t * ts + h * hs + d.
+struct Rows {
+    void* p;
+    int64_t ts, hs;
+};
+
+struct Rotary {
+    const float* table;  // [positions][2][rot / 2]; null: no rotation
+    int64_t positions;
+    int rot;
+    int interleaved;
+    int inverse;
+};
+
+// A paged cache and the page table it is looked up in.
+struct CacheView {
+    uint8_t *k, *v;
+    uint32_t *ks, *vs;  // one 4-byte word a token and head
+    const int32_t* table;
+    int64_t sequences, width, pages;
+    int page_shift;  // log2 of page_tokens
+    int heads, head_dim, kind;
+};
+
+constexpr int entry_bits(int kind) { return kind == UNISVQ_CACHE_I8 ? 8 : kind == UNISVQ_CACHE_I4 ? 4 : 16; }
+
+hipError_t launch_rope_table(int64_t positions, int rot, double theta, double factor, double low, double high,
+                             double original, double magnitude, float* table, hipStream_t s);
+hipError_t launch_rope(int64_t tokens, int heads, int head_dim, const Rotary& rotary, Rows x, const int32_t* positions,
+                       Rows y, int dtype, hipStream_t s);
+hipError_t launch_cache_append(const CacheView& c, int64_t tokens, const int32_t* seqs, const int32_t* positions,
+                               Rows k, Rows v, Rows q, int q_heads, Rows q_out, int x_dtype, const Rotary& rotary,
+                               hipStream_t s);
+hipError_t launch_cache_read(const CacheView& c, const int32_t* starts, const int32_t* cu, int64_t tokens, Rows k,
+                             Rows v, int dtype, hipStream_t s);
+
+// Attention over the cache.  splits: workgroups along a sequence.
+int decode_splits(int64_t sequences, int q_len, int q_heads, int kv_heads, int64_t max_len);
+size_t decode_workspace_bytes(int64_t sequences, int q_len, int q_heads, int head_dim, int splits);
+hipError_t launch_attn_decode(const CacheView& c, const int32_t* lens, int64_t max_len, int splits, int q_len, int q_heads, Rows q,
+                              int x_dtype, float scale, Rows out, float* lse, void* workspace, hipStream_t s);
+
+struct PromptArgs {
+    const int32_t *cu_q, *cu_k;
+    int64_t sequences, q_tokens, k_tokens;
+    int q_heads, kv_heads, head_dim;
+    Rows q, k, v, out;
+    int dtype, causal;
+    float scale;
+    float* lse;
+};
+size_t prompt_workspace_bytes(int64_t sequences, int64_t q_tokens, int64_t k_tokens, int q_heads, int kv_heads,
+                              int head_dim);
+hipError_t launch_attn_prompt(const PromptArgs& a, void* workspace, hipStream_t s);
+
+// ---- device helpers ----
+
+// A vector of eight 16-bit elements as floats and back (round to nearest even).
+template <typename T>
+struct Vec8;
+template <>
+struct Vec8<_Float16> {
+    typedef f16x8 type;
+};
+template <>
+struct Vec8<__bf16> {
+    typedef bf16x8 type;
+};
+
+template <typename T>
+__device__ inline void load8(const T* p, float (&f)[8]) {
+    const typename Vec8<T>::type v = *reinterpret_cast<const typename Vec8<T>::type*>(p);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = static_cast<float>(v[i]);
+}
+
+template <typename T>
+__device__ inline void store8(T* p, const float (&f)[8]) {
+    typename Vec8<T>::type v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = static_cast<T>(f[i]);
+    *reinterpret_cast<typename Vec8<T>::type*>(p) = v;
+}
+
+__device__ inline void load8(const float* p, float (&f)[8]) {
+    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = a[i], f[4 + i] = b[i];
+}
+
+// Eight pairs rotated; products and sums are rounded one by one (a contracted
+// product would differ from the plain formula in the last bit, and where the
+// result is quantised, in a code).
+__device__ inline void rotate8(float (&a)[8], float (&b)[8], const float (&c)[8], const float (&s)[8]) {
+#pragma clang fp contract(off)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float x = a[i], y = b[i];
+        const float xc = x * c[i], ys = y * s[i], yc = y * c[i], xs = x * s[i];
+        a[i] = xc - ys;
+        b[i] = yc + xs;
+    }
+}
+
+// Sixteen dims of a head as one thread holds them: dims d0 + i and d1 + i, or
+// where the layout is interleaved (and for dims that are not rotated) the
+// sixteen from d0 on, split into even and odd ones by `turn`.
+struct Chunk {
+    int d0, d1;   // first dims of the two runs of eight
+    bool turned;  // whether they are rotated
+};
+
+__device__ inline Chunk chunk_of(int c, int rot, int interleaved) {
+    Chunk k;
+    k.turned = 16 * c < rot;
+    k.d0 = k.turned && !interleaved ? 8 * c : 16 * c;
+    k.d1 = k.turned && !interleaved ? rot / 2 + 8 * c : 16 * c + 8;
+    return k;
+}
+
+// Rotates a chunk's dims (u from d0, w from d1) with cosines c and sines s of
+// pairs 8 * chunk .. 8 * chunk + 7.
+__device__ inline void turn(float (&u)[8], float (&w)[8], const float (&c)[8], const float (&s)[8], int interleaved) {
+    if (!interleaved) {
+        rotate8(u, w, c, s);
+        return;
+    }
+    float a[8], b[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = u[2 * i], b[i] = u[2 * i + 1], a[4 + i] = w[2 * i], b[4 + i] = w[2 * i + 1];
+    rotate8(a, b, c, s);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[2 * i] = a[i], u[2 * i + 1] = b[i], w[2 * i] = a[4 + i], w[2 * i + 1] = b[4 + i];
+}
+
+// ---- values that are not finite ----
+// A product on the matrix cores takes 0 * inf and 0 * NaN to NaN, so a value
+// that is not finite would reach rows that do not see it.  Where rows of a
+// tile see different keys and the tile holds such a value, the tile's values
+// are split: `finite` has zeros in place of them, `rest` only them, and `mark`
+// a one for each; the rest is added to the sums whose row sees one
+// (mark x seen > 0) and to no other.
+template <typename T>
+__device__ constexpr uint32_t exponent_bits() { return std::is_same_v<T, _Float16> ? 0x7c00u : 0x7f80u; }
+
+// Whether one of the two values in w is not finite.
+template <typename T>
+__device__ inline bool not_finite(uint32_t w) {
+    constexpr uint32_t e = exponent_bits<T>();
+    return (w & e) == e || (w >> 16 & e) == e;
+}
+
+template <typename T>
+struct Split {
+    typename Vec8<T>::type finite, rest, mark;
+};
+
+template <typename T>
+__device__ inline Split<T> split_finite(typename Vec8<T>::type v) {
+    Split<T> s;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint16_t bits = __builtin_bit_cast(uint16_t, static_cast<T>(v[i]));
+        const bool bad = (bits & exponent_bits<T>()) == exponent_bits<T>();
+        s.finite[i] = bad ? static_cast<T>(0.0f) : v[i];
+        s.rest[i] = bad ? v[i] : static_cast<T>(0.0f);
+        s.mark[i] = static_cast<T>(bad ? 1.0f : 0.0f);
+    }
+    return s;
+}
+
+// The sequence that packed row r belongs to: the last b with cu[b] <= r, found
+// by a whole wave together (64 entries a step; r is the same in all lanes).
+// Returns n where r >= cu[n].
+__device__ inline int sequence_of(const int32_t* cu, int n, int64_t r) {
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    for (int i = 0; i < n; i += 64) {
+        const bool past = i + lane < n && cu[i + lane + 1] <= r;
+        const int count = __popcll(__ballot(past));
+        before += count;
+        if (count < 64) break;
+    }
+    return before;
+}
+
+}  // namespace unisvq

@@ -1,0 +1,578 @@
+// Attention of a few new tokens per sequence over a paged cache, on gfx950.
+//
+//   s_t = scale (q . k_t),  p_t = exp(s_t - m),  out = sum_t p_t v_t / sum_t p_t
+//
+// Bound: HBM (every key and value is read once, for two products of at most
+// sixteen rows).  So nothing is staged: a wave reads 32 tokens at a time
+// straight into the registers that the matrix cores take their operands from,
+// and the products are arranged so that this works without moving data
+// between lanes:
+//   S^T = K Q^T   (16 tokens x 16 query rows): lane (i, g) = (lane % 16,
+//                 lane / 16) holds dims of token i; the order of the dims
+//                 along the product's inner axis is free, so each kind takes
+//                 the order in which 16 bytes of a token's row come.
+//   O^T = V^T P^T (16 dims x 16 query rows, 32 tokens inner): the result of
+//                 the first product leaves lane (i, g) with tokens 4g .. 4g+3
+//                 of query i, and the inner order of the second is chosen to
+//                 be just that: V comes as, for each of these tokens, D/16
+//                 consecutive dims a lane; row i of dim tile e is dim (D/16) i + e,
+//                 and pairs of tokens are put together by byte permutes.
+// Query rows are the q_len tokens of the q_heads / kv_heads heads that share a
+// key head.  Codes become f16 integers exactly; the keys' scales multiply the
+// scores and the values' scales the softmax weights, both in fp32.
+//
+// A workgroup's four waves take every fourth 32-token tile of the workgroup's
+// part of the sequence, each with its own running maximum m, sum and outputs,
+// joined through LDS; parts are joined by a second launch.  m is raised only
+// when a score exceeds it by 2^8 (the weights then stay below 2^8, well inside
+// f16), so most tiles need no exchange between lanes and no rescaling.
+#include <cfloat>
+
+#include "attn.hpp"
+
+namespace unisvq {
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4, kTile = 32, kRows = 16;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kSlack = 8.0f;  // log2 of how far scores may exceed the running maximum
+
+struct Decode {
+    CacheView c;
+    const int32_t* lens;
+    Rows q, out;
+    float* lse;
+    float* part;   // [rows][splits][D] sums, null when splits == 1
+    float2* part_ml;  // [rows][splits] maximum (log2) and sum
+    int splits, chunk;  // tokens of a split, a multiple of kTile
+    int q_len, q_heads, group, row_tiles;
+    float scale;  // of the scores, times log2 e
+};
+
+__device__ inline f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ inline uint32_t perm(uint32_t hi, uint32_t lo, uint32_t sel) { return __builtin_amdgcn_perm(hi, lo, sel); }
+__device__ inline f16x2 as_f16x2(uint32_t v) { return __builtin_bit_cast(f16x2, v); }
+__device__ inline uint32_t as_u32(f16x2 v) { return __builtin_bit_cast(uint32_t, v); }
+
+// 1024 + u in both halves (u a byte or a nibble in the low bits) minus `bias`.
+__device__ inline uint32_t minus(uint32_t v, float bias) {
+    const _Float16 b = static_cast<_Float16>(-bias);
+    return as_u32(as_f16x2(v) + f16x2{b, b});
+}
+// 1024 + 16 u in both halves: u - 8.
+__device__ inline uint32_t minus8_of16(uint32_t v) {
+    const _Float16 r = static_cast<_Float16>(0.0625f), b = static_cast<_Float16>(-72.0f);
+    return as_u32(__builtin_elementwise_fma(as_f16x2(v), f16x2{r, r}, f16x2{b, b}));
+}
+
+// Eight nibbles + 8 of w as f16 integers in the order 0 4 1 5 2 6 3 7.
+__device__ inline u32x4 nibbles(uint32_t w) {
+    const uint32_t x = w >> 8;
+    return u32x4{minus((w & 0x000f000fu) | 0x64006400u, 1032.0f), minus8_of16((w & 0x00f000f0u) | 0x64006400u),
+                 minus((x & 0x000f000fu) | 0x64006400u, 1032.0f), minus8_of16((x & 0x00f000f0u) | 0x64006400u)};
+}
+
+// What a lane reads of 16 tokens' keys (K) and of one token's values (V).
+template <int KIND, int D>
+struct Geometry {
+    static constexpr int bits = entry_bits(KIND);
+    static constexpr int row = D * bits / 8;      // bytes of an entry
+    static constexpr int E = D / 16;              // dims of a token's values a lane holds
+    static constexpr int vbytes = E * bits / 8;   // 2, 4, 8 or 16
+    static constexpr int kword = bits == 16 || bits == 8 ? 16 : D / 16;  // bytes a key load: 16, or 8 / 4 (half a head of 4-bit codes over 4 lanes)
+    static constexpr int kloads = row / (4 * kword);
+    static constexpr bool scaled = bits < 16;
+    static constexpr int halves = bits == 4 ? 2 : 1;  // scales of a head
+};
+
+template <int BYTES>
+struct Word;
+template <> struct Word<16> { typedef u32x4 type; };
+template <> struct Word<8> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
+template <> struct Word<4> { typedef uint32_t type; };
+template <> struct Word<2> { typedef uint16_t type; };
+
+template <int KIND, int D>
+struct TileRegs {
+    typedef Geometry<KIND, D> G;
+    typename Word<G::kword>::type k[2][G::kloads];
+    typename Word<G::vbytes>::type v[2][4];
+    f32x4 ks[2], vs[2];  // the scale words of tokens 4g .. 4g + 3
+    bool there[2];       // whether the 16 tokens have a page (the same in all lanes)
+};
+
+template <typename T>
+__device__ inline T load_stream(const uint8_t* p) { return __builtin_nontemporal_load(reinterpret_cast<const T*>(p)); }
+
+template <int KIND, int D>
+__device__ inline void load_tile(const Decode& a, int64_t table_row, int h, int pos, int len, int i, int g,
+                                 TileRegs<KIND, D>& r) {
+    typedef Geometry<KIND, D> G;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int p = pos + 16 * t;
+        int64_t page = -1;
+        if (p < len) page = a.c.table[table_row + (p >> a.c.page_shift)];
+        r.there[t] = page >= 0 && page < a.c.pages;
+        if (!r.there[t]) page = 0;
+        const int64_t e = ((page * a.c.heads + h) << a.c.page_shift) + (p & ((1 << a.c.page_shift) - 1));
+        const uint8_t* kp = a.c.k + e * G::row;
+        const uint8_t* vp = a.c.v + e * G::row;
+#pragma unroll
+        for (int n = 0; n < G::kloads; ++n)
+            r.k[t][n] = load_stream<typename Word<G::kword>::type>(kp + (i * G::row + n * 4 * G::kword + g * G::kword));
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+            r.v[t][n] = load_stream<typename Word<G::vbytes>::type>(vp + ((4 * g + n) * G::row + i * G::vbytes));
+        if constexpr (G::scaled) {
+            r.ks[t] = *reinterpret_cast<const f32x4*>(a.c.ks + e + 4 * g);
+            r.vs[t] = *reinterpret_cast<const f32x4*>(a.c.vs + e + 4 * g);
+        }
+    }
+}
+
+// The dims of query operand step n for lane group g: eight from first on, in
+// natural order or as nibbles() has them.
+template <int KIND, int D>
+__device__ inline int query_dim(int n, int g) {
+    if constexpr (KIND == UNISVQ_CACHE_I8) return 64 * (n / 2) + 16 * g + 8 * (n % 2);
+    if constexpr (KIND == UNISVQ_CACHE_I4) return (n / (D / 64)) * (D / 2) + g * (D / 8) + 8 * (n % (D / 64));
+    return 32 * n + 8 * g;
+}
+
+// Scores of 16 tokens (unscaled; one sum for each half of the head where the
+// scales differ).
+template <int KIND, int D, typename C8>
+__device__ inline void scores16(const TileRegs<KIND, D>& r, int t, const C8 (&q)[D / 32], f32x4 (&s)[Geometry<KIND, D>::halves]) {
+#pragma unroll
+    for (int h = 0; h < Geometry<KIND, D>::halves; ++h) s[h] = f32x4{0, 0, 0, 0};
+    if constexpr (KIND == UNISVQ_CACHE_I8) {
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n) {
+            const uint32_t w0 = r.k[t][n / 2][2 * (n % 2)] ^ 0x80808080u, w1 = r.k[t][n / 2][2 * (n % 2) + 1] ^ 0x80808080u;
+            const uint32_t magic = 0x64646464u;
+            const u32x4 a = {minus(perm(magic, w0, 0x04010400u), 1152.0f), minus(perm(magic, w0, 0x04030402u), 1152.0f),
+                             minus(perm(magic, w1, 0x04010400u), 1152.0f), minus(perm(magic, w1, 0x04030402u), 1152.0f)};
+            s[0] = mfma(__builtin_bit_cast(C8, a), q[n], s[0]);
+        }
+    } else if constexpr (KIND == UNISVQ_CACHE_I4) {
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n) {
+            constexpr int per = D / 64;
+            uint32_t w;
+            if constexpr (per == 2) w = r.k[t][n / per][n % per];
+            else w = r.k[t][n];
+            s[n / per] = mfma(__builtin_bit_cast(C8, nibbles(w)), q[n], s[n / per]);
+        }
+    } else {
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n) s[0] = mfma(__builtin_bit_cast(C8, r.k[t][n]), q[n], s[0]);
+    }
+}
+
+// 32-bit word w of a lane's values of one token.
+template <int KIND, int D>
+__device__ inline uint32_t vword(const TileRegs<KIND, D>& r, int t, int n, int w) {
+    if constexpr (Geometry<KIND, D>::vbytes <= 4) return r.v[t][n];
+    else return r.v[t][n][w];
+}
+
+// The A operand of dim tile e: dim (D/16) i + e of the lane's eight tokens.
+template <int KIND, int D, typename C8>
+__device__ inline void value_operands(const TileRegs<KIND, D>& r, C8 (&v)[D / 16]) {
+    constexpr int E = D / 16;
+    uint32_t w[E][4];  // [dim][token pair]
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int n = 0; n < 4; n += 2) {
+            const int pair = 2 * t + n / 2;
+            if constexpr (KIND == UNISVQ_CACHE_I8) {
+#pragma unroll
+                for (int x = 0; x < E / 4; ++x) {
+                    const uint32_t a = vword<KIND, D>(r, t, n, x) ^ 0x80808080u, b = vword<KIND, D>(r, t, n + 1, x) ^ 0x80808080u;
+                    w[4 * x + 0][pair] = minus(perm(b, a, 0x0c040c00u) | 0x64006400u, 1152.0f);
+                    w[4 * x + 1][pair] = minus(perm(b, a, 0x0c050c01u) | 0x64006400u, 1152.0f);
+                    w[4 * x + 2][pair] = minus(perm(b, a, 0x0c060c02u) | 0x64006400u, 1152.0f);
+                    w[4 * x + 3][pair] = minus(perm(b, a, 0x0c070c03u) | 0x64006400u, 1152.0f);
+                }
+            } else if constexpr (KIND == UNISVQ_CACHE_I4) {
+                const uint32_t a = vword<KIND, D>(r, t, n, 0), b = vword<KIND, D>(r, t, n + 1, 0);
+#pragma unroll
+                for (int x = 0; x < E / 4; ++x) {
+                    const uint32_t both = perm(b, a, x ? 0x07060302u : 0x05040100u);  // four nibbles of each token
+                    const u32x4 d = nibbles(both);
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) w[4 * x + y][pair] = d[y];
+                }
+            } else {
+#pragma unroll
+                for (int x = 0; x < E / 2; ++x) {
+                    const uint32_t a = vword<KIND, D>(r, t, n, x), b = vword<KIND, D>(r, t, n + 1, x);
+                    w[2 * x][pair] = perm(b, a, 0x05040100u);
+                    w[2 * x + 1][pair] = perm(b, a, 0x07060302u);
+                }
+            }
+        }
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = __builtin_bit_cast(C8, u32x4{w[e][0], w[e][1], w[e][2], w[e][3]});
+}
+
+__device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The scale of a token in half h of the head.
+template <int KIND>
+__device__ inline float scale_of(float word, int h) {
+    if constexpr (KIND == UNISVQ_CACHE_I4) {
+        const uint32_t w = __float_as_uint(word);
+        return __uint_as_float(h ? w & 0xffff0000u : w << 16);
+    }
+    return word;
+}
+
+template <int KIND, int D, typename XT>
+__global__ __launch_bounds__(kThreads) void decode_kernel(Decode a) {
+    typedef Geometry<KIND, D> G;
+    typedef std::conditional_t<G::scaled, _Float16, XT> CT;
+    typedef typename Vec8<CT>::type C8;
+    constexpr int E = G::E, HV = G::halves, kPad = 4;
+    const int split = blockIdx.x % a.splits;
+    const int hr = blockIdx.x / a.splits % (a.c.heads * a.row_tiles);
+    const int b = blockIdx.x / a.splits / (a.c.heads * a.row_tiles);
+    const int h = hr / a.row_tiles, row0 = hr % a.row_tiles * kRows;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int i = lane & 15, g = lane >> 4;
+    const int64_t room = a.c.width << a.c.page_shift;
+    int len = max(0, a.lens[b]);
+    if (len > room) len = static_cast<int>(room);
+    const int begin = split * a.chunk;
+    const int end = split == a.splits - 1 ? len : min(len, begin + a.chunk);  // past max_len the last goes on
+    if (split > 0 && begin >= len) return;  // the joining launch goes by the length too
+
+    // the lane's query row: token j, head hq of the group
+    const int rows = a.q_len * a.group;
+    const int row = row0 + i;
+    const bool live = row < rows;
+    const int j = live ? row / a.group : 0, hq = h * a.group + (live ? row % a.group : 0);
+    const int64_t token = static_cast<int64_t>(b) * a.q_len + j;
+    const int limit = live ? len - a.q_len + 1 + j : 0;
+    C8 q[D / 32];
+    float qscale = a.scale;
+    {
+        const XT* x = static_cast<const XT*>(a.q.p) + token * a.q.ts + hq * a.q.hs;
+        typename Vec8<XT>::type raw[D / 32];
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n) {
+            raw[n] = *reinterpret_cast<const typename Vec8<XT>::type*>(x + query_dim<KIND, D>(n, g));
+            if (!live)
+#pragma unroll
+                for (int y = 0; y < 8; ++y) raw[n][y] = static_cast<XT>(0.0f);
+            if constexpr (KIND == UNISVQ_CACHE_I4) {
+                const auto v = raw[n];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) raw[n][2 * y] = v[y], raw[n][2 * y + 1] = v[4 + y];
+            }
+        }
+        if constexpr (std::is_same_v<CT, XT>) {
+#pragma unroll
+            for (int n = 0; n < D / 32; ++n) q[n] = raw[n];
+        } else {
+            // bf16 queries as f16: times a power of two that brings the row's largest into [2^14, 2^15)
+            uint32_t m = 0;
+#pragma unroll
+            for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+                for (int y = 0; y < 8; ++y) m = max(m, __float_as_uint(static_cast<float>(raw[n][y])) & 0x7fffffffu);
+            m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16)));
+            m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 32)));
+            const int exponent = static_cast<int>(m >> 23) - 127;
+            const int up = m == 0 || exponent == 128 ? 0 : 14 - exponent;
+#pragma unroll
+            for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+                for (int y = 0; y < 8; ++y) q[n][y] = static_cast<CT>(ldexpf(static_cast<float>(raw[n][y]), up));
+            qscale = ldexpf(qscale, -up);
+        }
+    }
+
+    float m = -FLT_MAX, l = 0.0f;
+    float vunit = 1.0f;  // power of two that the values' scales are taken in (scaled kinds)
+    f32x4 o[HV][E];
+#pragma unroll
+    for (int x = 0; x < HV; ++x)
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[x][e] = f32x4{0, 0, 0, 0};
+
+    const int64_t table_row = static_cast<int64_t>(b) * a.c.width;
+    TileRegs<KIND, D> r;
+    int pos = begin + wave * kTile;
+    bool first = true;
+    for (; pos < end; pos += kWaves * kTile) {
+        load_tile<KIND, D>(a, table_row, h, pos, len, i, g, r);
+        // scores, log2 units
+        float s[2][4];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            f32x4 acc[HV];
+            scores16<KIND, D>(r, t, q, acc);
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                float v;
+                if constexpr (KIND == UNISVQ_CACHE_I4)
+                    v = acc[0][n] * scale_of<KIND>(r.ks[t][n], 0) + acc[HV - 1][n] * scale_of<KIND>(r.ks[t][n], 1);
+                else if constexpr (KIND == UNISVQ_CACHE_I8)
+                    v = acc[0][n] * r.ks[t][n];
+                else
+                    v = acc[0][n];
+                s[t][n] = v * qscale;
+            }
+        }
+        // whether all 32 tokens are seen by all rows
+        const bool full = pos + kTile <= len - a.q_len + 1 && r.there[0] && r.there[1];
+        if (!full) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    const int p = pos + 16 * t + 4 * g + n;
+                    if (!(p < limit && r.there[t])) s[t][n] = -INFINITY;
+                    // what no row sees may hold anything
+                    if (!(p < len && r.there[t])) {
+                        if constexpr (G::scaled) r.vs[t][n] = 0.0f;
+                        else r.v[t][n] = {};
+                    }
+                }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) top = fmaxf(top, s[t][n]);
+        bool raise = top > m + kSlack;
+        float vtop = 0.0f;
+        if constexpr (G::scaled) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+#pragma unroll
+                    for (int x = 0; x < HV; ++x) vtop = fmaxf(vtop, scale_of<KIND>(r.vs[t][n], x));
+            raise |= first || vtop * vunit > 128.0f;
+        }
+        if (__any(raise)) {
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float m2 = fmaxf(m, top);
+            float c = exp2_(m - m2);
+            l *= c;
+            m = m2;
+            if constexpr (G::scaled) {
+                vtop = fmaxf(vtop, __shfl_xor(vtop, 16));
+                vtop = fmaxf(vtop, __shfl_xor(vtop, 32));
+                if (vtop > 0.0f && vtop < INFINITY && (first || vtop * vunit > 128.0f)) {
+                    // 2^-exponent of the largest scale
+                    const float unit = ldexpf(1.0f, 127 - static_cast<int>(__float_as_uint(vtop) >> 23));
+                    if (!first) c *= unit / vunit;
+                    vunit = unit;
+                    first = false;
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < HV; ++x)
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[x][e] *= c;
+        }
+        C8 p[HV];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const float w = exp2_(s[t][n] - m);
+                l += w;
+#pragma unroll
+                for (int x = 0; x < HV; ++x)
+                    // (a weight of zero stays one where the scale is NaN, for rows that do not see the token)
+                    p[x][4 * t + n] = static_cast<CT>(!G::scaled ? w
+                                                      : full || s[t][n] > -INFINITY || s[t][n] != s[t][n]
+                                                          ? w * (scale_of<KIND>(r.vs[t][n], x) * vunit)
+                                                          : 0.0f);
+            }
+        C8 v[E];
+        value_operands<KIND, D>(r, v);
+        bool dirty = false;  // codes are finite, and a scale that is not is the weight's matter
+        if constexpr (!G::scaled) {
+            if (!full && a.q_len > 1) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const u32x4 w = __builtin_bit_cast(u32x4, v[e]);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) dirty |= not_finite<CT>(w[x]);
+                }
+                dirty = __any(dirty);
+            }
+        }
+        if (!dirty) {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+#pragma unroll
+                for (int x = 0; x < HV; ++x) o[x][e] = mfma(v[e], p[x], o[x][e]);
+        } else if constexpr (!G::scaled) {
+            C8 seen;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+                    seen[4 * t + n] = static_cast<CT>(pos + 16 * t + 4 * g + n < limit && r.there[t] ? 1.0f : 0.0f);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const Split<CT> w = split_finite<CT>(v[e]);
+                const f32x4 rest = mfma(w.rest, p[0], f32x4{}), marks = mfma(w.mark, seen, f32x4{});
+                o[0][e] = mfma(w.finite, p[0], o[0][e]);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) o[0][e][x] += marks[x] > 0.0f ? rest[x] : 0.0f;
+            }
+        }
+    }
+
+    // join the waves: dim E (4g + n) + e of query i
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    __shared__ float so[kWaves][kRows][D + kPad];
+    __shared__ float sm[kWaves][kRows], sl[kWaves][kRows];
+    if (live) {
+        const float back = G::scaled ? 1.0f / vunit : 1.0f;
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                float v = o[0][e][n];
+                if constexpr (HV == 2) v = g < 2 ? v : o[HV - 1][e][n];
+                so[wave][i][E * (4 * g + n) + e] = v * back;
+            }
+        if (g == 0) sm[wave][i] = m, sl[wave][i] = l;
+    }
+    __syncthreads();
+    const int y = threadIdx.x / (D / 8), d = threadIdx.x % (D / 8) * 8;
+    if (y >= kRows || row0 + y >= rows) return;
+    float mt = sm[0][y], lt = 0.0f, f[8];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) mt = fmaxf(mt, sm[w][y]);
+#pragma unroll
+    for (int n = 0; n < 8; ++n) f[n] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        const float c = exp2_(sm[w][y] - mt);
+        lt += c * sl[w][y];
+#pragma unroll
+        for (int n = 0; n < 8; ++n) f[n] += c * so[w][y][d + n];
+    }
+    const int jy = (row0 + y) / a.group, hy = h * a.group + (row0 + y) % a.group;
+    const int64_t ty = static_cast<int64_t>(b) * a.q_len + jy, r_out = ty * a.q_heads + hy;
+    if (a.splits == 1) {
+        const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
+#pragma unroll
+        for (int n = 0; n < 8; ++n) f[n] *= inv;
+        store8(static_cast<XT*>(a.out.p) + ty * a.out.ts + hy * a.out.hs + d, f);
+        if (a.lse && d == 0) a.lse[r_out] = (mt + log2f(lt)) * kLn2;
+    } else {
+        float* to = a.part + (r_out * a.splits + split) * D + d;
+        *reinterpret_cast<f32x4*>(to) = f32x4{f[0], f[1], f[2], f[3]};
+        *reinterpret_cast<f32x4*>(to + 4) = f32x4{f[4], f[5], f[6], f[7]};
+        if (d == 0) a.part_ml[r_out * a.splits + split] = float2{mt, lt};
+    }
+}
+
+// Joins the parts of a row; one wave a row, in the order of the parts.
+template <int D, typename XT>
+__global__ __launch_bounds__(kThreads) void join_kernel(Decode a, int64_t rows) {
+    const int64_t r = static_cast<int64_t>(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
+    if (r >= rows) return;
+    const int lane = threadIdx.x & 63;
+    const int64_t token = r / a.q_heads;
+    const int hq = static_cast<int>(r - token * a.q_heads);
+    const int64_t room = a.c.width << a.c.page_shift;
+    int64_t len = max(0, a.lens[token / a.q_len]);
+    if (len > room) len = room;
+    const int n = static_cast<int>(min(static_cast<int64_t>(a.splits), max(int64_t{1}, (len + a.chunk - 1) / a.chunk)));
+    float mt = -FLT_MAX;
+    for (int x = lane; x < n; x += 64) mt = fmaxf(mt, a.part_ml[r * a.splits + x].x);
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) mt = fmaxf(mt, __shfl_xor(mt, x));
+    float lt = 0.0f, f[D / 64] = {};
+    for (int x = 0; x < n; ++x) {
+        const float2 ml = a.part_ml[r * a.splits + x];
+        if (ml.y == 0.0f) continue;
+        const float c = exp2_(ml.x - mt);
+        lt += c * ml.y;
+        const float* from = a.part + (r * a.splits + x) * D + lane * (D / 64);
+#pragma unroll
+        for (int y = 0; y < D / 64; ++y) f[y] += c * from[y];
+    }
+    const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
+    XT* to = static_cast<XT*>(a.out.p) + token * a.out.ts + hq * a.out.hs + lane * (D / 64);
+#pragma unroll
+    for (int y = 0; y < D / 64; ++y) to[y] = static_cast<XT>(f[y] * inv);
+    if (a.lse && lane == 0) a.lse[r] = (mt + log2f(lt)) * kLn2;
+}
+
+template <int D, typename XT>
+hipError_t run(const Decode& a, hipStream_t s) {
+    const uint32_t blocks = static_cast<uint32_t>(a.c.sequences * a.c.heads * a.row_tiles * a.splits);
+    constexpr int raw = std::is_same_v<XT, _Float16> ? UNISVQ_CACHE_F16 : UNISVQ_CACHE_BF16;
+    if (a.c.kind == UNISVQ_CACHE_I8)
+        decode_kernel<UNISVQ_CACHE_I8, D, XT><<<blocks, kThreads, 0, s>>>(a);
+    else if (a.c.kind == UNISVQ_CACHE_I4)
+        decode_kernel<UNISVQ_CACHE_I4, D, XT><<<blocks, kThreads, 0, s>>>(a);
+    else
+        decode_kernel<raw, D, XT><<<blocks, kThreads, 0, s>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.splits == 1) return e;
+    const int64_t rows = a.c.sequences * a.q_len * a.q_heads;
+    join_kernel<D, XT><<<static_cast<uint32_t>((rows + 3) / 4), kThreads, 0, s>>>(a, rows);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// Splits: about 1024 workgroups (four a CU), of at least one tile a wave.
+int decode_splits(int64_t sequences, int q_len, int q_heads, int kv_heads, int64_t max_len) {
+    const int64_t base = sequences * kv_heads * ((q_len * (q_heads / kv_heads) + kRows - 1) / kRows);
+    const int64_t most = (max_len + kWaves * kTile - 1) / (kWaves * kTile);
+    int64_t n = 1024 / base;
+    n = n > most ? most : n;
+    return static_cast<int>(n < 1 ? 1 : n > 128 ? 128 : n);
+}
+
+size_t decode_workspace_bytes(int64_t sequences, int q_len, int q_heads, int head_dim, int splits) {
+    if (splits == 1) return 0;
+    return static_cast<size_t>(sequences * q_len * q_heads) * splits * (head_dim + 2) * 4;
+}
+
+hipError_t launch_attn_decode(const CacheView& c, const int32_t* lens, int64_t max_len, int splits, int q_len, int q_heads, Rows q,
+                              int x_dtype, float scale, Rows out, float* lse, void* workspace, hipStream_t s) {
+    Decode a{};
+    a.c = c;
+    a.lens = lens;
+    a.q = q;
+    a.out = out;
+    a.lse = lse;
+    a.splits = splits;
+    a.chunk = static_cast<int>(((max_len + splits - 1) / splits + kTile - 1) / kTile * kTile);
+    a.q_len = q_len;
+    a.q_heads = q_heads;
+    a.group = q_heads / c.heads;
+    a.row_tiles = (q_len * a.group + kRows - 1) / kRows;
+    a.scale = scale * kLog2e;
+    if (splits > 1) {
+        a.part = static_cast<float*>(workspace);
+        a.part_ml = reinterpret_cast<float2*>(a.part + c.sequences * q_len * q_heads * splits * c.head_dim);
+    }
+    if (c.head_dim == 128) return x_dtype == UNISVQ_F16 ? run<128, _Float16>(a, s) : run<128, __bf16>(a, s);
+    return x_dtype == UNISVQ_F16 ? run<64, _Float16>(a, s) : run<64, __bf16>(a, s);
+}
+
+}  // namespace unisvq

@@ -30,10 +30,15 @@ EXPORTS = ("unisvq_version", "unisvq_status_string", "unisvq_packed_bytes", "uni
            "unisvq_var_gemm_workspace_bytes", "unisvq_var_gemm", "unisvq_ldlq_workspace_bytes", "unisvq_ldlq",
            "unisvq_ldl_workspace_bytes", "unisvq_ldl",
            "unisvq_gemv_rht_batched", "unisvq_read_sink_words", "unisvq_read_bytes", "unisvq_noalloc_scratch_bytes",
-           "unisvq_gemm_noalloc", "unisvq_gemm_batched_workspace_bytes", "unisvq_gemm_batched")
+           "unisvq_gemm_noalloc", "unisvq_gemm_batched_workspace_bytes", "unisvq_gemm_batched",
+           "unisvq_rope_table", "unisvq_rope", "unisvq_cache_append", "unisvq_cache_read",
+           "unisvq_attn_decode_workspace_bytes", "unisvq_attn_decode", "unisvq_attn_prompt_workspace_bytes",
+           "unisvq_attn_prompt")
 # format variants: (bits, d) pairs served by the unisvq_var_* entry points
 VARIANTS = ((3, 4), (2, 8), (3, 8))
 MAX_BATCH = 8
+# what a cache holds (unisvq_cache_kind)
+CACHE_F16, CACHE_BF16, CACHE_I8, CACHE_I4 = 0, 1, 2, 3
 
 
 class GemvProblem(ctypes.Structure):
@@ -52,6 +57,13 @@ class GemvSharedProblem(ctypes.Structure):
 class ByteRange(ctypes.Structure):
     """Mirror of unisvq_byte_range."""
     _fields_ = [("ptr", ctypes.c_void_p), ("bytes", ctypes.c_int64)]
+
+
+class Cache(ctypes.Structure):
+    """Mirror of unisvq_cache."""
+    _fields_ = [("pages", ctypes.c_int64), ("page_tokens", ctypes.c_int64), ("kv_heads", ctypes.c_int64),
+                ("head_dim", ctypes.c_int64), ("kind", ctypes.c_int), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
 
 
 class UniSVQLibraryMissing(RuntimeError):
@@ -156,6 +168,26 @@ def load():
     lib.unisvq_read_sink_words.restype = i64
     lib.unisvq_read_bytes.argtypes = [ctypes.POINTER(ByteRange), i32, i32, p, i64, p]
     lib.unisvq_read_bytes.restype = i32
+    f64, f32, pc = ctypes.c_double, ctypes.c_float, ctypes.POINTER(Cache)
+    rows = [p, i64, i64]  # pointer, token stride, head stride
+    lib.unisvq_rope_table.argtypes = [i64, i64, f64, f64, f64, f64, f64, f64, p, p]
+    lib.unisvq_rope_table.restype = i32
+    lib.unisvq_rope.argtypes = [i64, i64, i64, i64, i32, i32, *rows, p, p, i64, *rows, i32, p]
+    lib.unisvq_rope.restype = i32
+    lib.unisvq_cache_append.argtypes = [pc, p, i64, i64, i64, p, p, *rows, *rows, p, i64, i64, i64, *rows, i32, p, i64,
+                                        i64, i32, p]
+    lib.unisvq_cache_append.restype = i32
+    lib.unisvq_cache_read.argtypes = [pc, p, i64, i64, p, p, i64, *rows, *rows, i32, p]
+    lib.unisvq_cache_read.restype = i32
+    lib.unisvq_attn_decode_workspace_bytes.argtypes = [i64] * 6
+    lib.unisvq_attn_decode_workspace_bytes.restype = sz
+    lib.unisvq_attn_decode.argtypes = [pc, p, i64, i64, p, i64, i64, i64, *rows, i32, f32, *rows, p, p, sz, p]
+    lib.unisvq_attn_decode.restype = i32
+    lib.unisvq_attn_prompt_workspace_bytes.argtypes = [i64] * 6
+    lib.unisvq_attn_prompt_workspace_bytes.restype = sz
+    lib.unisvq_attn_prompt.argtypes = [i64, i64, i64, p, p, i64, i64, i64, *rows, *rows, *rows, i32, i32, f32, *rows, p,
+                                       p, sz, p]
+    lib.unisvq_attn_prompt.restype = i32
     _lib = lib
     return lib
 
@@ -807,3 +839,250 @@ def read_bytes(buffers, store: bool = True, sink=None, stream=None):
     _check("unisvq_read_bytes", load().unisvq_read_bytes(arr, len(buffers), 1, _ptr(sink), sink.numel(),
                                                          _stream(stream)))
     return sink
+
+
+# ---- the attention block ----
+
+def _rows(t, what: str, heads: int | None = None, head_dim: int | None = None, tokens: int | None = None, dtype=None):
+    """A [tokens][heads][head_dim] fp16/bf16 tensor, its last axis contiguous, any strides of the other two (the C
+    entry refuses those that are not multiples of 8): checked, and as (pointer, token stride, head stride)."""
+    torch = _torch()
+    shape = t.shape
+    if len(shape) != 3:
+        raise ValueError(f"{what} must be [tokens][heads][head_dim], got {tuple(shape)}")
+    if not t.is_cuda:
+        raise ValueError("libunisvq takes device tensors only")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{what} is {t.dtype}, expected {dtype}")
+    if t.dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError(f"{what} must be fp16 or bf16, got {t.dtype}")
+    if (tokens is not None and shape[0] != tokens) or (heads is not None and shape[1] != heads) or \
+            (head_dim is not None and shape[2] != head_dim):
+        raise ValueError(f"{what} is {tuple(shape)}, expected {(tokens, heads, head_dim)}")
+    strides = t.stride()
+    if strides[2] != 1:
+        raise ValueError(f"the dims of {what}'s heads must be contiguous")
+    return t.data_ptr(), strides[0], strides[1]
+
+
+def _ints(t, count: int, what: str):
+    """A contiguous int32 device tensor of `count` elements, as a pointer."""
+    torch = _torch()
+    if t.dtype != torch.int32 or t.numel() != count or not t.is_contiguous():
+        raise ValueError(f"{what} must hold {count} contiguous int32, got {t.dtype} {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise ValueError("libunisvq takes device tensors only")
+    return t.data_ptr()
+
+
+def _out_rows(out, like, tokens: int, heads: int, head_dim: int, what: str = "out"):
+    """The caller's out (checked) or a new tensor, and its rows."""
+    if out is None:
+        out = _torch().empty((tokens, heads, head_dim), dtype=like.dtype, device=like.device)
+    return out, _rows(out, what, heads, head_dim, tokens, like.dtype)
+
+
+def rope_table(positions: int, rot: int, theta: float = 10000.0, factor: float = 1.0, low: float = 1.0,
+               high: float = 4.0, original: float = 0.0, magnitude: float = 1.0, device="cuda", stream=None):
+    """Cosines and sines [positions][2][rot / 2] (fp32) of rotary positions; factor, low, high, original and magnitude
+    stretch them over long contexts as unisvq_rope_table says."""
+    torch = _torch()
+    table = torch.empty((positions, 2, rot // 2), dtype=torch.float32, device=device)
+    _check("unisvq_rope_table", load().unisvq_rope_table(positions, rot, theta, factor, low, high, original, magnitude,
+                                                         _ptr(table), _stream(stream)))
+    return table
+
+
+def _rope_rows(table):
+    """(pointer, positions, rot) of a table of rope_table's."""
+    torch = _torch()
+    shape = table.shape
+    if table.dtype != torch.float32 or len(shape) != 3 or shape[1] != 2 or not table.is_contiguous():
+        raise ValueError("the rope table must be contiguous fp32 [positions][2][rot / 2]")
+    if not table.is_cuda:
+        raise ValueError("libunisvq takes device tensors only")
+    return table.data_ptr(), shape[0], 2 * shape[2]
+
+
+def rope(x, positions, table, interleaved: bool = False, inverse: bool = False, out=None, stream=None):
+    """x [tokens][heads][head_dim] rotated to int32 positions [tokens]: the first rot = 2 * table.shape[2] dims of
+    every head, in pairs (i, i + rot / 2) or, interleaved, (2i, 2i + 1); inverse: the transpose (the gradient).
+    out may be x (in place) or a view with its own strides."""
+    tokens, heads, head_dim = x.shape
+    xr = _rows(x, "x")
+    out, yr = _out_rows(out, x, tokens, heads, head_dim)
+    tp, n, rot = _rope_rows(table)
+    _check("unisvq_rope", load().unisvq_rope(tokens, heads, head_dim, rot, interleaved, inverse, *xr,
+                                             _ints(positions, tokens, "positions"), tp, n, *yr, _dtype_code(x.dtype),
+                                             _stream(stream)))
+    return out
+
+
+def new_cache(pages: int, kv_heads: int, page_tokens: int, head_dim: int, kind: str, device="cuda"):
+    """An empty cache (k, v, k_scales, v_scales) of kind "f16", "bf16", "i8" or "i4": pools [pages][kv_heads]
+    [page_tokens][head_dim] (head_dim / 2 bytes for i4), scales f32 [pages][kv_heads][page_tokens] or bf16 [..][2], None
+    for the 16-bit kinds."""
+    torch = _torch()
+    shape = (pages, kv_heads, page_tokens)
+    dtype, last = {"f16": (torch.float16, head_dim), "bf16": (torch.bfloat16, head_dim), "i8": (torch.int8, head_dim),
+                   "i4": (torch.uint8, head_dim // 2)}[kind]
+    pools = [torch.zeros((*shape, last), dtype=dtype, device=device) for _ in range(2)]
+    if kind == "i8":
+        scales = [torch.zeros(shape, dtype=torch.float32, device=device) for _ in range(2)]
+    elif kind == "i4":
+        scales = [torch.zeros((*shape, 2), dtype=torch.bfloat16, device=device) for _ in range(2)]
+    else:
+        scales = [None, None]
+    return (*pools, *scales)
+
+
+def _cache(cache):
+    """The C description of a cache tuple (k, v, k_scales, v_scales), checked; the kind is the pools' dtype's."""
+    torch = _torch()
+    k, v, ks, vs = cache
+    dt, shape = k.dtype, k.shape
+    if dt == torch.int8:
+        kind, head_dim = CACHE_I8, shape[-1]
+    elif dt == torch.uint8:
+        kind, head_dim = CACHE_I4, 2 * shape[-1]
+    elif dt == torch.float16:
+        kind, head_dim = CACHE_F16, shape[-1]
+    elif dt == torch.bfloat16:
+        kind, head_dim = CACHE_BF16, shape[-1]
+    else:
+        raise TypeError(f"a cache's pools are fp16, bf16, int8 or uint8 (4-bit codes), got {dt}")
+    if len(shape) != 4 or v.shape != shape or v.dtype != dt or not (k.is_contiguous() and v.is_contiguous()):
+        raise ValueError("k and v pools must be contiguous [pages][kv_heads][page_tokens][..] of one dtype")
+    if not (k.is_cuda and v.is_cuda):
+        raise ValueError("libunisvq takes device tensors only")
+    if kind >= CACHE_I8:
+        want = (torch.float32, shape[:3]) if kind == CACHE_I8 else (torch.bfloat16, (*shape[:3], 2))
+        for t in (ks, vs):
+            if t is None or t.dtype != want[0] or t.shape != want[1] or not t.is_contiguous() or not t.is_cuda:
+                raise ValueError(f"scales must be contiguous {want[0]} {tuple(want[1])} on the device")
+        return Cache(shape[0], shape[2], shape[1], head_dim, kind, k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr())
+    return Cache(shape[0], shape[2], shape[1], head_dim, kind, k.data_ptr(), v.data_ptr(), None, None)
+
+
+def _page_table(table):
+    torch = _torch()
+    shape = table.shape
+    if table.dtype != torch.int32 or len(shape) != 2 or not table.is_contiguous() or not table.is_cuda:
+        raise ValueError("the page table must be contiguous int32 [sequences][pages of a sequence] on the device")
+    return table.data_ptr(), shape[0], shape[1]
+
+
+def cache_append(cache, page_table, seqs, positions, k, v, q=None, rope_table=None, interleaved: bool = False,
+                 q_out=None, stream=None):
+    """Write k and v [tokens][kv_heads][head_dim] to the cache, keys rotated by rope_table (None: as they are), at
+    int32 positions [tokens] of sequences seqs [tokens] (None: token t is sequence t's).  q [tokens][q_heads][head_dim]
+    is rotated in the same launch and returned (q_out, which may be q, or a new tensor; None where q is None)."""
+    c = _cache(cache)
+    tokens = k.shape[0]
+    kr = _rows(k, "k", c.kv_heads, c.head_dim)
+    vr = _rows(v, "v", c.kv_heads, c.head_dim, tokens, k.dtype)
+    q_heads, qr, qor = 0, (None, 0, 0), (None, 0, 0)
+    if q is not None:
+        q_heads = q.shape[1]
+        qr = _rows(q, "q", q_heads, c.head_dim, tokens, k.dtype)
+        q_out, qor = _out_rows(q_out, q, tokens, q_heads, c.head_dim, "q_out")
+    rr = (None, 0, 0) if rope_table is None else _rope_rows(rope_table)
+    _check("unisvq_cache_append", load().unisvq_cache_append(
+        c, *_page_table(page_table), tokens, None if seqs is None else _ints(seqs, tokens, "seqs"),
+        _ints(positions, tokens, "positions"), *kr, *vr, qr[0], q_heads, qr[1], qr[2], *qor, _dtype_code(k.dtype), *rr,
+        interleaved, _stream(stream)))
+    return q_out if q is not None else None
+
+
+def cache_read(cache, page_table, starts, cu, tokens: int, out=None, out_dtype=None, stream=None):
+    """Keys and values of tokens starts[b] .. of every sequence as packed rows [tokens][kv_heads][head_dim]: rows
+    cu[b] .. cu[b + 1] - 1 are sequence b's (cu int32 [sequences + 1]; starts int32 [sequences] or None: 0).  out: a
+    pair (k, v) of tensors to write, or None."""
+    torch = _torch()
+    c = _cache(cache)
+    pt = _page_table(page_table)
+    if out is None:
+        dt = out_dtype or (cache[0].dtype if cache[0].dtype.is_floating_point else torch.float16)
+        out = tuple(torch.empty((tokens, c.kv_heads, c.head_dim), dtype=dt, device=cache[0].device) for _ in range(2))
+    k, v = out
+    kr = _rows(k, "out k", c.kv_heads, c.head_dim, tokens)
+    vr = _rows(v, "out v", c.kv_heads, c.head_dim, tokens, k.dtype)
+    _check("unisvq_cache_read", load().unisvq_cache_read(
+        c, *pt, None if starts is None else _ints(starts, pt[1], "starts"), _ints(cu, pt[1] + 1, "cu"), tokens, *kr,
+        *vr, _dtype_code(k.dtype), _stream(stream)))
+    return k, v
+
+
+def _lse(lse, count: int):
+    if lse is None:
+        return None
+    torch = _torch()
+    if lse.dtype != torch.float32 or lse.numel() != count or not lse.is_contiguous() or not lse.is_cuda:
+        raise ValueError(f"lse must hold {count} contiguous fp32 on the device")
+    return lse.data_ptr()
+
+
+def attn_decode_workspace_bytes(sequences: int, q_len: int, q_heads: int, kv_heads: int, head_dim: int,
+                                max_len: int) -> int:
+    return load().unisvq_attn_decode_workspace_bytes(sequences, q_len, q_heads, kv_heads, head_dim, max_len)
+
+
+def attn_decode(q, cache, page_table, lens, scale: float | None = None, max_len: int = 0, out=None, lse=None,
+                workspace=None, stream=None):
+    """Attention of the newest tokens q [sequences][q_heads][head_dim] or [sequences][q_len][q_heads][head_dim] over
+    the cache, which holds their keys and values already; lens int32 [sequences] counts them too.  scale: of the
+    scores (None: head_dim ** -0.5).  max_len: what the lengths are at most (0: the page table's width).  lse: fp32
+    tensor for the log of the sum of exponentials, or None.  workspace: as gemm's."""
+    c = _cache(cache)
+    pt = _page_table(page_table)
+    if q.dim() not in (3, 4):
+        raise ValueError("q must be [sequences][q_heads][head_dim] or [sequences][q_len][q_heads][head_dim]")
+    shape = q.shape
+    sequences, q_len, q_heads = shape[0], shape[1] if len(shape) == 4 else 1, shape[-2]
+    if sequences != pt[1]:
+        raise ValueError(f"q has {sequences} sequences, the page table {pt[1]}")
+    tokens = sequences * q_len
+    q3 = q if len(shape) == 3 else q.view(tokens, q_heads, shape[3])
+    qr = _rows(q3, "q", q_heads, c.head_dim)
+    if out is None:
+        out = _torch().empty(shape, dtype=q.dtype, device=q.device)
+    elif out.shape != shape:
+        raise ValueError(f"out is {tuple(out.shape)}, q {tuple(shape)}")
+    orr = _rows(out if len(shape) == 3 else out.view(tokens, q_heads, shape[3]), "out", dtype=q.dtype)
+    room = pt[2] * c.page_tokens
+    need = attn_decode_workspace_bytes(sequences, q_len, q_heads, c.kv_heads, c.head_dim,
+                                       min(max_len, room) if max_len else room)
+    ws, size = _workspace(workspace, need, q)
+    _check("unisvq_attn_decode", load().unisvq_attn_decode(
+        c, *pt, _ints(lens, sequences, "lens"), max_len, q_len, q_heads, *qr, _dtype_code(q.dtype),
+        c.head_dim ** -0.5 if scale is None else scale, *orr, _lse(lse, tokens * q_heads), _ptr(ws),
+        size, _stream(stream)))
+    return out
+
+
+def attn_prompt_workspace_bytes(sequences: int, q_tokens: int, k_tokens: int, q_heads: int, kv_heads: int,
+                                head_dim: int) -> int:
+    return load().unisvq_attn_prompt_workspace_bytes(sequences, q_tokens, k_tokens, q_heads, kv_heads, head_dim)
+
+
+def attn_prompt(q, k, v, cu_q, cu_k, causal: bool = True, scale: float | None = None, out=None, lse=None,
+                workspace=None, stream=None):
+    """Attention over packed sequences: q [q_tokens][q_heads][head_dim], k and v [k_tokens][kv_heads][head_dim], of any
+    strides (parts of one fused row, say); sequence b has queries cu_q[b] .. cu_q[b + 1] - 1 and keys cu_k[b] .. (int32
+    [sequences + 1]).  Causal: the last query of a sequence sees all its keys, each one before it one key less.  scale,
+    lse, workspace: as attn_decode's."""
+    tokens, q_heads, head_dim = q.shape
+    k_tokens, kv_heads = k.shape[0], k.shape[1]
+    qr = _rows(q, "q")
+    kr = _rows(k, "k", kv_heads, head_dim, k_tokens, q.dtype)
+    vr = _rows(v, "v", kv_heads, head_dim, k_tokens, q.dtype)
+    out, orr = _out_rows(out, q, tokens, q_heads, head_dim)
+    sequences = cu_q.numel() - 1
+    need = attn_prompt_workspace_bytes(sequences, tokens, k_tokens, q_heads, kv_heads, head_dim)
+    ws, size = _workspace(workspace, need, q)
+    _check("unisvq_attn_prompt", load().unisvq_attn_prompt(
+        sequences, tokens, k_tokens, _ints(cu_q, sequences + 1, "cu_q"), _ints(cu_k, sequences + 1, "cu_k"), q_heads,
+        kv_heads, head_dim, *qr, *kr, *vr, _dtype_code(q.dtype), causal,
+        head_dim ** -0.5 if scale is None else scale, *orr, _lse(lse, tokens * q_heads), _ptr(ws),
+        size, _stream(stream)))
+    return out

@@ -1,0 +1,128 @@
+"""Rotary positions on the GPU: the table against fp64, rotations against the formula in fp32 bit for bit, the inverse as
+the gradient, strides, in-place use and positions outside the table."""
+import numpy as np
+import pytest
+
+import attn_ref as ref
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+DT = {"f16": torch.float16, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def u():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2606_10520_amd.unisvq as u
+    u.load()
+    return u
+
+
+def ints(v):
+    return torch.tensor(np.asarray(v), dtype=torch.int32, device=DEV)
+
+
+@pytest.mark.parametrize("args", [
+    dict(positions=1, rot=16), dict(positions=4097, rot=128), dict(positions=300, rot=20, theta=5e5),
+    dict(positions=70000, rot=64, factor=8.0), dict(positions=40000, rot=128, factor=4.0, original=8192.0, magnitude=1.14),
+    dict(positions=1000, rot=96, factor=16.0, original=4096.0, low=1.0, high=32.0),
+])
+def test_table(u, args):
+    got = u.rope_table(**args).cpu().numpy().astype(np.float64)
+    want = ref.table64(**args)
+    # one rounding to fp32 of values up to `magnitude`, and the angle's: positions * (a few 2^-53)
+    tol = args.get("magnitude", 1.0) * (2.0 ** -24 + args["positions"] * 2.0 ** -49)
+    assert got.shape == want.shape and np.max(np.abs(got - want)) <= tol
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("D,rot", [(16, 16), (64, 64), (64, 48), (80, 32), (128, 128), (128, 80), (256, 64), (1024, 1024)])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("tokens,heads", [(1, 1), (3, 5), (67, 8)])
+def test_rotation_bit_for_bit(u, dtype, D, rot, interleaved, tokens, heads):
+    g = torch.Generator().manual_seed(D + rot + tokens)
+    x = torch.randn((tokens, heads, D), generator=g).to(DT[dtype])
+    pos = np.random.default_rng(tokens).integers(0, 500, tokens)
+    table = ref.table64(500, rot).astype(np.float32)
+    for inverse in (False, True):
+        got = u.rope(x.to(DEV), ints(pos), torch.from_numpy(table).to(DEV), interleaved=interleaved, inverse=inverse)
+        want = torch.from_numpy(ref.rotate(x.float().numpy(), pos, table, interleaved, inverse)).to(DT[dtype])
+        assert torch.equal(got.cpu(), want)
+
+
+def test_against_64_bits(u):
+    x = torch.randn((50, 4, 128)).half()
+    pos, table = np.arange(50) * 71, ref.table64(4000, 128).astype(np.float32)
+    got = u.rope(x.to(DEV), ints(pos), torch.from_numpy(table).to(DEV)).double().cpu().numpy()
+    want = ref.rotate(x.double().numpy(), pos, table.astype(np.float64), False)
+    mag = ref.rotate(np.abs(x.double().numpy()), pos, np.abs(table.astype(np.float64)) * [[[1], [-1]]], False)
+    # three fp32 roundings of values up to |a c| + |b s|, one to fp16
+    bound = np.abs(want) * 2.0 ** -11 + (np.abs(mag) + np.abs(want)) * 2.0 ** -22 + 2.0 ** -25
+    assert (np.abs(got - want) <= bound + 2.0 ** -22 * np.abs(x.double().numpy()).max()).all()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_inverse_is_the_gradient(u, interleaved):
+    """d/dx of sum(w . rope(x)): autograd of the formula, and differences of it, in 64 bits."""
+    rng = np.random.default_rng(3)
+    pos, table = rng.integers(0, 900, 6), ref.table64(900, 32).astype(np.float32)
+    w = torch.randn((6, 3, 48)).half()
+    got = u.rope(w.to(DEV), ints(pos), torch.from_numpy(table).to(DEV), interleaved=interleaved, inverse=True)
+    got = got.double().cpu().numpy()
+    x = rng.standard_normal((6, 3, 48))
+    f = lambda x: float(np.sum(w.double().numpy() * ref.rotate(x, pos, table.astype(np.float64), interleaved)))
+    for _ in range(40):
+        at = tuple(rng.integers(0, n) for n in x.shape)
+        d = np.zeros_like(x)
+        d[at] = 0.5
+        diff = f(x + d) - f(x - d)  # the function is linear: exact but for rounding
+        assert abs(got[at] - diff) <= 2.0 ** -11 * abs(diff) + 2.0 ** -20 * 8
+    xt = torch.from_numpy(x).requires_grad_(True)
+    t = torch.from_numpy(table.astype(np.float64))[pos][:, None]
+    a, b = (xt[..., 0:32:2], xt[..., 1:32:2]) if interleaved else (xt[..., :16], xt[..., 16:32])
+    ya, yb = a * t[:, :, 0] - b * t[:, :, 1], b * t[:, :, 0] + a * t[:, :, 1]
+    wd = w.double()
+    wa, wb = (wd[..., 0:32:2], wd[..., 1:32:2]) if interleaved else (wd[..., :16], wd[..., 16:32])
+    ((ya * wa).sum() + (yb * wb).sum() + (xt[..., 32:] * wd[..., 32:]).sum()).backward()
+    assert np.max(np.abs(got - xt.grad.numpy())) <= 2.0 ** -10 * 8
+
+
+def test_strides_in_place_and_views(u):
+    torch.manual_seed(0)
+    table = torch.from_numpy(ref.table64(64, 128).astype(np.float32)).to(DEV)
+    pos = ints(np.arange(9))
+    fused = torch.randn((9, 7, 128), device=DEV).half()
+    want = u.rope(fused[:, 2:5].contiguous(), pos, table)
+    rest = fused.clone()
+    got = u.rope(fused[:, 2:5], pos, table, out=fused[:, 2:5])  # in place, heads 2 to 4 of the fused rows
+    assert torch.equal(got, want) and torch.equal(fused[:, :2], rest[:, :2]) and torch.equal(fused[:, 5:], rest[:, 5:])
+    heads_first = rest[:, 2:5].transpose(0, 1).contiguous().transpose(0, 1)  # [tokens][heads] with heads outermost
+    out = torch.empty((3, 9, 128), dtype=torch.float16, device=DEV).transpose(0, 1)
+    assert torch.equal(u.rope(heads_first, pos, table, out=out), want)
+    with pytest.raises(u.UniSVQError) as e:
+        odd = torch.zeros(9 * 300, dtype=torch.float16, device=DEV)
+        u.rope(odd[: 9 * 132].view(9, 1, 132)[..., :128], pos, table)
+    assert e.value.status == -4
+
+
+def test_positions_outside_the_table_and_no_tokens(u):
+    table = torch.from_numpy(ref.table64(10, 32).astype(np.float32)).to(DEV)
+    x = torch.randn((4, 2, 64), device=DEV).half()
+    y = u.rope(x, ints([3, -1, 10, 2 ** 31 - 1]), table)
+    assert torch.isnan(y[1:, :, :32]).all() and torch.equal(y[1:, :, 32:], x[1:, :, 32:])
+    assert torch.equal(y[:1], u.rope(x[:1], ints([3]), table))
+    assert u.rope(x[:0], ints([]), table).shape == (0, 2, 64)
+
+
+def test_another_stream(u):
+    table = u.rope_table(100, 64)
+    x, pos = torch.randn((100, 4, 64), device=DEV).half(), ints(np.arange(100))
+    want = u.rope(x, pos, table)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    out = torch.empty_like(x)
+    u.rope(x, pos, table, out=out, stream=s)
+    s.synchronize()
+    assert torch.equal(out, want)
