@@ -150,10 +150,9 @@ __device__ inline void turn(float (&u)[8], float (&w)[8], const float (&c)[8], c
 // ---- values that are not finite ----
 // A product on the matrix cores takes 0 * inf and 0 * NaN to NaN, so a value
 // that is not finite would reach rows that do not see it.  Where rows of a
-// tile see different keys and the tile holds such a value, the tile's values
-// are split: `finite` has zeros in place of them, `rest` only them, and `mark`
-// a one for each; the rest is added to the sums whose row sees one
-// (mark x seen > 0) and to no other.
+// tile see different keys and the tile holds such values, they are added to
+// the sums of the rows that see them one by one, and zeros take their places
+// before the product.
 template <typename T>
 __device__ constexpr uint32_t exponent_bits() { return std::is_same_v<T, _Float16> ? 0x7c00u : 0x7f80u; }
 
@@ -164,23 +163,13 @@ __device__ inline bool not_finite(uint32_t w) {
     return (w & e) == e || (w >> 16 & e) == e;
 }
 
+// w with zeros in place of what is not finite.
 template <typename T>
-struct Split {
-    typename Vec8<T>::type finite, rest, mark;
-};
-
-template <typename T>
-__device__ inline Split<T> split_finite(typename Vec8<T>::type v) {
-    Split<T> s;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint16_t bits = __builtin_bit_cast(uint16_t, static_cast<T>(v[i]));
-        const bool bad = (bits & exponent_bits<T>()) == exponent_bits<T>();
-        s.finite[i] = bad ? static_cast<T>(0.0f) : v[i];
-        s.rest[i] = bad ? v[i] : static_cast<T>(0.0f);
-        s.mark[i] = static_cast<T>(bad ? 1.0f : 0.0f);
-    }
-    return s;
+__device__ inline uint32_t finite_only(uint32_t w) {
+    constexpr uint32_t e = exponent_bits<T>();
+    if ((w & e) == e) w &= 0xffff0000u;
+    if ((w >> 16 & e) == e) w &= 0xffffu;
+    return w;
 }
 
 // The sequence that packed row r belongs to: the last b with cu[b] <= r, found

@@ -222,6 +222,37 @@ __device__ inline void value_operands(const TileRegs<KIND, D>& r, C8 (&v)[D / 16
     for (int e = 0; e < E; ++e) v[e] = __builtin_bit_cast(C8, u32x4{w[e][0], w[e][1], w[e][2], w[e][3]});
 }
 
+// Adds the tile's values that are not finite to the sums of the rows that see
+// them, and puts zeros in their places (see not_finite).
+template <int KIND, int D, typename CT>
+__device__ inline void only_where_seen(TileRegs<KIND, D>& r, int pos, int limit, int g, f32x4 (&o)[D / 16]) {
+    constexpr int words = D / 32;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int x = 0; x < words; ++x) {
+                const uint32_t w = vword<KIND, D>(r, t, n, x);
+                uint64_t left = __ballot(not_finite<CT>(w));
+                while (left) {  // rare
+                    const int lane = __ffsll(static_cast<unsigned long long>(left)) - 1;
+                    left &= left - 1;
+                    const uint32_t both = __builtin_amdgcn_readlane(w, lane);
+                    const bool mine = (lane & 15) >> 2 == g && pos + 16 * t + 4 * (lane >> 4) + n < limit;
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const uint16_t bits = static_cast<uint16_t>(both >> 16 * y);
+                        const float add = mine && (bits & exponent_bits<CT>()) == exponent_bits<CT>()
+                                              ? static_cast<float>(__builtin_bit_cast(CT, bits)) : 0.0f;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) o[2 * x + y][c] += (lane & 3) == c ? add : 0.0f;
+                    }
+                }
+                r.v[t][n][x] = finite_only<CT>(w);
+            }
+}
+
 __device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // The scale of a token in half h of the head.
@@ -401,41 +432,15 @@ __global__ __launch_bounds__(kThreads) void decode_kernel(Decode a) {
                                                           ? w * (scale_of<KIND>(r.vs[t][n], x) * vunit)
                                                           : 0.0f);
             }
+        if constexpr (!G::scaled) {  // codes are finite, and a scale that is not is the weight's matter
+            if (!full && a.q_len > 1) only_where_seen<KIND, D, CT>(r, pos, limit, g, o[0]);
+        }
         C8 v[E];
         value_operands<KIND, D>(r, v);
-        bool dirty = false;  // codes are finite, and a scale that is not is the weight's matter
-        if constexpr (!G::scaled) {
-            if (!full && a.q_len > 1) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const u32x4 w = __builtin_bit_cast(u32x4, v[e]);
+        for (int e = 0; e < E; ++e)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) dirty |= not_finite<CT>(w[x]);
-                }
-                dirty = __any(dirty);
-            }
-        }
-        if (!dirty) {
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-#pragma unroll
-                for (int x = 0; x < HV; ++x) o[x][e] = mfma(v[e], p[x], o[x][e]);
-        } else if constexpr (!G::scaled) {
-            C8 seen;
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int n = 0; n < 4; ++n)
-                    seen[4 * t + n] = static_cast<CT>(pos + 16 * t + 4 * g + n < limit && r.there[t] ? 1.0f : 0.0f);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const Split<CT> w = split_finite<CT>(v[e]);
-                const f32x4 rest = mfma(w.rest, p[0], f32x4{}), marks = mfma(w.mark, seen, f32x4{});
-                o[0][e] = mfma(w.finite, p[0], o[0][e]);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) o[0][e][x] += marks[x] > 0.0f ? rest[x] : 0.0f;
-            }
-        }
+            for (int x = 0; x < HV; ++x) o[x][e] = mfma(v[e], p[x], o[x][e]);
     }
 
     // join the waves: dim E (4g + n) + e of query i

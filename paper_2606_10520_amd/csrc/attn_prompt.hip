@@ -59,8 +59,41 @@ __device__ inline void load_tile(const T* p, int64_t ts, int rows, T* lds, int w
     }
 }
 
+// Adds the values of the tile at `vs` that are not finite to the sums o of the
+// queries that see their keys (k0 + row < limit; see not_finite).
 template <int D, typename T>
-__global__ __launch_bounds__(kThreads) void prompt_kernel(PromptArgs a, float scale_log2) {
+__device__ inline void add_not_finite(const T* vs, int k0, int limit, int lane, f32x16 (&o)[D / 32]) {
+    constexpr int chunks = D / 8;
+    for (int at = lane; at < kKeys * chunks; at += 64) {
+        const u32x4 w = reinterpret_cast<const u32x4*>(vs)[at];
+        uint64_t left = __ballot(not_finite<T>(w[0]) || not_finite<T>(w[1]) || not_finite<T>(w[2]) || not_finite<T>(w[3]));
+        while (left) {
+            const int from = __ffsll(static_cast<unsigned long long>(left)) - 1;
+            left &= left - 1;
+            const int place = at - lane + from, row = place / chunks;
+            const bool seen = k0 + row < limit;
+            const int dim = ((place % chunks) ^ turn_v<D>(row)) * 8;
+            uint64_t lo = __builtin_amdgcn_readlane(w[0], from) | static_cast<uint64_t>(__builtin_amdgcn_readlane(w[1], from)) << 32;
+            uint64_t hi = __builtin_amdgcn_readlane(w[2], from) | static_cast<uint64_t>(__builtin_amdgcn_readlane(w[3], from)) << 32;
+#pragma nounroll
+            for (int e = 0; e < 8; ++e) {
+                const uint16_t bits = static_cast<uint16_t>(lo);
+                lo = lo >> 16 | hi << 48;
+                hi >>= 16;
+                if ((bits & exponent_bits<T>()) != exponent_bits<T>()) continue;
+                const float add = seen ? static_cast<float>(__builtin_bit_cast(T, bits)) : 0.0f;
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        o[d][r] += 32 * d + 8 * (r / 4) + 4 * (lane >> 5) + r % 4 == dim + e ? add : 0.0f;
+            }
+        }
+    }
+}
+
+template <int D, typename T>
+__global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, float scale_log2) {
     typedef typename Vec8<T>::type T8;
     constexpr int kQ = 32, kTileQ = kQ * kWaves;
     __shared__ __attribute__((aligned(16))) T sk[2][kKeys * D];
@@ -141,17 +174,24 @@ __global__ __launch_bounds__(kThreads) void prompt_kernel(PromptArgs a, float sc
     for (int t = 0; t < tiles; ++t) {
         __syncthreads();  // the tile is there, and its predecessor's buffer free
         const int k0 = t * kKeys;
-        bool dirty = false;
-        if (k0 + kKeys > block_low) {
+        if (a.causal && k0 + kKeys > block_low) {  // queries see different keys
             bool bad = false;
-            const u32x4* w = reinterpret_cast<const u32x4*>(sv[t & 1]) + threadIdx.x;
+            u32x4* w = reinterpret_cast<u32x4*>(sv[t & 1]) + threadIdx.x;
 #pragma unroll
             for (int n = 0; n < kKeys * D / 8 / kThreads; ++n)
 #pragma unroll
                 for (int x = 0; x < 4; ++x) bad |= not_finite<T>(w[n * kThreads][x]);
             if (bad) bad_tile = t + 1;
             __syncthreads();
-            dirty = bad_tile == t + 1;
+            if (bad_tile == t + 1) {
+                add_not_finite<D, T>(sv[t & 1], k0, limit, lane, o);
+                __syncthreads();
+#pragma unroll
+                for (int n = 0; n < kKeys * D / 8 / kThreads; ++n)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) w[n * kThreads][x] = finite_only<T>(w[n * kThreads][x]);
+                __syncthreads();
+            }
         }
         if (t + 1 < tiles) {
             const int k1 = (t + 1) * kKeys;
@@ -214,19 +254,7 @@ __global__ __launch_bounds__(kThreads) void prompt_kernel(PromptArgs a, float sc
                     part[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
                 }
                 const T8 v8 = __builtin_bit_cast(T8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
-                if (!dirty) {
-                    o[d] = mfma(v8, p[n], o[d]);
-                } else {
-                    const Split<T> v = split_finite<T>(v8);
-                    T8 seen;
-#pragma unroll
-                    for (int x = 0; x < 8; ++x)
-                        seen[x] = static_cast<T>(k0 + 16 * n + 8 * (x / 4) + 4 * hf + x % 4 < limit ? 1.0f : 0.0f);
-                    const f32x16 rest = mfma(v.rest, p[n], f32x16{}), marks = mfma(v.mark, seen, f32x16{});
-                    o[d] = mfma(v.finite, p[n], o[d]);
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) o[d][x] += marks[x] > 0.0f ? rest[x] : 0.0f;
-                }
+                o[d] = mfma(v8, p[n], o[d]);
             }
     }
 
