@@ -716,7 +716,8 @@ int unisvq_attn_decode(const unisvq_cache* cache, const int32_t* page_table, int
  *               entries are taken as at most q_tokens and k_tokens.  Queries
  *               from cu_q[sequences] on are left as they are
  *   q, out      device [q_tokens][q_heads][head_dim]; k, v [k_tokens][kv_heads][head_dim]
- *   head_dim    64 or 128; q_heads a multiple of kv_heads
+ *   head_dim    64 or 128; q_heads a multiple of kv_heads; token strides of k
+ *               and v from head_dim to 2^22 (UNISVQ_EUNSUP otherwise)
  *   lse         device fp32 [q_tokens][q_heads] or NULL, as above
  *   workspace   device, >= unisvq_attn_prompt_workspace_bytes(...) bytes,
  *               16-byte aligned; may be NULL when that size is 0 (it is where

@@ -224,9 +224,10 @@ int unisvq_attn_prompt(int64_t sequences, int64_t q_tokens, int64_t k_tokens, co
         !rows_aligned(v, v_token_stride, v_head_stride) || !rows_aligned(out, out_token_stride, out_head_stride) ||
         !aligned(cu_q, 4) || !aligned(cu_k, 4) || !aligned(lse, 4))
         return UNISVQ_EALIGN;
-    // tiles of keys and values are addressed with 32-bit offsets
+    // tiles of keys and values are addressed with 32-bit offsets from their first row, and end with their last
     const int64_t wide = int64_t{1} << 22;
-    if (k_token_stride < 0 || k_token_stride > wide || v_token_stride < 0 || v_token_stride > wide) return UNISVQ_EUNSUP;
+    if (k_token_stride < head_dim || k_token_stride > wide || v_token_stride < head_dim || v_token_stride > wide)
+        return UNISVQ_EUNSUP;
     if ((q_tokens / 64 + sequences) > kMost / q_heads) return UNISVQ_EUNSUP;
     const size_t need = unisvq::prompt_workspace_bytes(sequences, q_tokens, k_tokens, static_cast<int>(q_heads),
                                                        static_cast<int>(kv_heads), static_cast<int>(head_dim));

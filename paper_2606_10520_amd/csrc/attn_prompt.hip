@@ -41,29 +41,42 @@ __device__ inline int turn_k(int row) { return D == 128 ? row & 15 : row >> 1 & 
 template <int D>
 __device__ inline int turn_v(int row) { return D == 128 ? 4 * (row & 3) : 4 * (row >> 1 & 1); }
 
-// Bring rows of the tile at `p` (of `rows` rows, ts elements apart) to LDS; rows
-// past the end become zeros.  Thread i brings the 16 bytes that are to be at
-// 16 (256 n + i).
-template <int D, typename T, bool VALUES>
-__device__ inline void load_tile(const T* p, int64_t ts, int rows, T* lds, int wave, int lane) {
+// The offset from a tile's first row of what thread i of a group brings to
+// place 16 (256 n + i) of the tile in LDS.
+template <int D, bool VALUES>
+__device__ inline uint32_t load_offset(int n, int i, int64_t ts) {
     constexpr int chunks = D / 8;
-    const uint32_t bytes = static_cast<uint32_t>((rows - 1) * ts * 2 + D * 2);
-    const __amdgpu_buffer_rsrc_t r = make_rsrc(p, bytes);
+    const int at = n * kThreads + i, row = at / chunks, place = at % chunks;
+    const int chunk = place ^ (VALUES ? turn_v<D>(row) : turn_k<D>(row));
+    return static_cast<uint32_t>(row * static_cast<int>(ts) * 2 + chunk * 16);
+}
+
+// Bring the tile at `p` (of `rows` rows, ts elements apart) to LDS.  What is
+// past the last row is past the buffer's end, and becomes zeros.
+template <int D, typename T>
+__device__ __forceinline__ void load_tile(const T* p, int64_t ts, int rows, const uint32_t (&off)[kKeys * D / 8 / kThreads],
+                                          T* lds, int wave) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(p, static_cast<uint32_t>((rows - 1) * ts * 2 + D * 2));
 #pragma unroll
-    for (int n = 0; n < kKeys * chunks / kThreads; ++n) {
-        const int at = n * kThreads + wave * 64 + lane, row = at / chunks, place = at % chunks;
-        const int chunk = place ^ (VALUES ? turn_v<D>(row) : turn_k<D>(row));
-        const uint32_t off = row < rows ? static_cast<uint32_t>(row * static_cast<int>(ts) * 2 + chunk * 16) : kOutOfRange;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(
-            r, (__attribute__((address_space(3))) void*)(lds + (n * kThreads + wave * 64) * 8), 16, off, 0, 0, 0);
+    for (int n = 0; n < kKeys * D / 8 / kThreads; ++n) {
+        const uint32_t to = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(
+            (__attribute__((address_space(3))) void*)(lds + (n * kThreads + wave * 64) * 8))));
+        // (the compiler would wait for a load that it knows of before any read of LDS that might be of its place)
+        asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off[n]), "s"(r) : "memory");
     }
 }
 
-// Adds the values of the tile at `vs` that are not finite to the sums o of the
-// queries that see their keys (k0 + row < limit; see not_finite).
+// Which of a lane's sums have met +inf or NaN, and which -inf or NaN (bit 16 d + r: o[d][r]).
+struct Spoiled {
+    uint64_t up, down;
+};
+
+// Marks the sums that values of the tile at `vs` that are not finite belong to,
+// for queries that see their keys (k0 + row < limit; see not_finite).
 template <int D, typename T>
-__device__ inline void add_not_finite(const T* vs, int k0, int limit, int lane, f32x16 (&o)[D / 32]) {
+__device__ inline void mark_not_finite(const T* vs, int k0, int limit, int lane, Spoiled& spoiled) {
     constexpr int chunks = D / 8;
+#pragma nounroll
     for (int at = lane; at < kKeys * chunks; at += 64) {
         const u32x4 w = reinterpret_cast<const u32x4*>(vs)[at];
         uint64_t left = __ballot(not_finite<T>(w[0]) || not_finite<T>(w[1]) || not_finite<T>(w[2]) || not_finite<T>(w[3]));
@@ -71,35 +84,157 @@ __device__ inline void add_not_finite(const T* vs, int k0, int limit, int lane, 
             const int from = __ffsll(static_cast<unsigned long long>(left)) - 1;
             left &= left - 1;
             const int place = at - lane + from, row = place / chunks;
-            const bool seen = k0 + row < limit;
             const int dim = ((place % chunks) ^ turn_v<D>(row)) * 8;
             uint64_t lo = __builtin_amdgcn_readlane(w[0], from) | static_cast<uint64_t>(__builtin_amdgcn_readlane(w[1], from)) << 32;
             uint64_t hi = __builtin_amdgcn_readlane(w[2], from) | static_cast<uint64_t>(__builtin_amdgcn_readlane(w[3], from)) << 32;
 #pragma nounroll
             for (int e = 0; e < 8; ++e) {
-                const uint16_t bits = static_cast<uint16_t>(lo);
+                const uint32_t bits = static_cast<uint32_t>(lo & 0xffffu);
                 lo = lo >> 16 | hi << 48;
                 hi >>= 16;
                 if ((bits & exponent_bits<T>()) != exponent_bits<T>()) continue;
-                const float add = seen ? static_cast<float>(__builtin_bit_cast(T, bits)) : 0.0f;
-#pragma unroll
-                for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        o[d][r] += 32 * d + 8 * (r / 4) + 4 * (lane >> 5) + r % 4 == dim + e ? add : 0.0f;
+                if (k0 + row < limit && (lane >> 5) == e / 4) {
+                    const uint64_t here = uint64_t{1} << (dim / 32 * 16 + dim % 32 / 8 * 4 + e % 4);
+                    if (bits != (0x8000u | exponent_bits<T>())) spoiled.up |= here;
+                    if (bits != exponent_bits<T>()) spoiled.down |= here;
+                }
             }
         }
     }
 }
 
+// Whether the tile at `vs` holds a value that is not finite (the whole wave's answer).
 template <int D, typename T>
-__global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, float scale_log2) {
+__device__ inline bool any_not_finite(const T* vs, int lane) {
+    bool bad = false;
+#pragma unroll 4
+    for (int at = lane; at < kKeys * D / 8; at += 64) {
+        const u32x4 w = reinterpret_cast<const u32x4*>(vs)[at];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) bad |= not_finite<T>(w[x]);
+    }
+    return __any(bad);
+}
+
+// A barrier of all waves that waits for no loads in flight.
+__device__ inline void phase() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+template <int N>
+__device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+// The order of values() and scores() in one phase: reads of LDS four products ahead.
+template <int D>
+__device__ __forceinline__ void schedule_products() {
+    constexpr int kProducts = D / 8, kAhead = 4;  // of either kind; two reads for one of values', one for one of scores'
+    __builtin_amdgcn_sched_group_barrier(0x100, 2 * kAhead, 0);
+#pragma unroll
+    for (int n = 0; n < kProducts - kAhead; ++n) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    }
+#pragma unroll
+    for (int n = 0; n < kProducts; ++n) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+}
+
+template <int D, typename T>
+struct Wave {
     typedef typename Vec8<T>::type T8;
-    constexpr int kQ = 32, kTileQ = kQ * kWaves;
-    __shared__ __attribute__((aligned(16))) T sk[2][kKeys * D];
-    __shared__ __attribute__((aligned(16))) T sv[2][kKeys * D];
-    __shared__ int bad_tile;  // 1 + the last tile found to hold values that are not finite, of those checked
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    T8 q[D / 16];
+    f32x16 o[D / 32];
+    f32x16 s[2];
+    T8 p[4];
+    float m, l, scale;
+    int hf;
+    int at_k;           // keys: row i of a tile, chunk hf as it is turned (chunk 2n + hf is at_k ^ 16n)
+    int at_v[D / 32];   // values: row 4hf + (i % 16) / 4, the lane's four dims of dim tile d
+
+    // o += V^T P^T for the tile at vs; CLEAN: values that are not finite count as zero.
+    template <bool CLEAN>
+    __device__ __forceinline__ void values(const T* vs) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) {
+                // keys 16n + 4hf + 0..3 and + 8..11 of dim 32d + i
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) s16x4*)(vs + at_v[d] + 16 * n * D));
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) s16x4*)(vs + at_v[d] + (16 * n + 8) * D));
+                u32x4 v4 = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                if constexpr (CLEAN)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) v4[x] = finite_only<T>(v4[x]);
+                const T8 v8 = __builtin_bit_cast(T8, v4);
+                o[d] = mfma(v8, p[n], o[d]);
+            }
+    }
+
+    // s = K Q^T for the tile at ks.
+    __device__ __forceinline__ void scores(const T* ks) {
+#pragma unroll
+        for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const T8 k8 = *reinterpret_cast<const T8*>(ks + (at_k ^ 16 * n) + 32 * x * D);
+                s[x] = mfma(k8, q[n], n ? s[x] : f32x16{});
+            }
+    }
+
+    // Hides keys from `limit` on, in the tile from key k0.
+    __device__ __forceinline__ void mask(int k0, int limit) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (32 * x + 8 * (r / 4) + r % 4 >= limit - k0 - 4 * hf) s[x][r] = -INFINITY;
+    }
+
+    // The tile's weights from its scores.
+    __device__ __forceinline__ void weights() {
+        float top = s[0][0];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[x][r]);
+        top *= scale;
+        if (__any(top > m + kSlack)) {
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float m2 = fmaxf(m, top), c = exp2_(m - m2);
+            m = m2;
+            l *= c;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) o[d] *= c;
+        }
+        float sum[4] = {};
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float w = exp2_(__builtin_fmaf(s[x][r], scale, -m));
+                sum[r % 4] += w;
+                p[2 * x + r / 8][r % 8] = static_cast<T>(w);
+            }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    }
+};
+
+template <int D, typename T>
+__global__ __launch_bounds__(2 * kThreads, 1) void prompt_kernel(PromptArgs a, float scale_log2) {
+    typedef typename Vec8<T>::type T8;
+    constexpr int kQ = 32, kTileQ = kQ * kWaves, kTile = kKeys * D;
+    constexpr int kLoads = kTile * 2 / (16 * kThreads);  // loads a thread of a tile of keys or values
+    __shared__ __attribute__((aligned(16))) T sk[2][2][kTile];  // two tiles of keys for either group
+    __shared__ __attribute__((aligned(16))) T sv[2][2][kTile];  // and of values
+    const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64 % kWaves), lane = threadIdx.x & 63;
     const int i = lane & 31, hf = lane >> 5;
 
     // heads of one key head go to one XCD (workgroups go round the eight)
@@ -147,120 +282,158 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, float
     const bool live = qi < nq;
     const int limit = !live ? 0 : a.causal ? qi + nk - nq + 1 : nk;
     const int wave_first = q0 + wave * kQ;
-    const int wave_low = wave_first + kQ > nq ? 0 : a.causal ? wave_first + nk - nq + 1 : nk;  // seen by all its queries
+    const int wave_low = a.causal ? wave_first + nk - nq + 1 : nk;  // seen by all its queries
     const int wave_high = wave_first >= nq ? 0 : a.causal ? min(nk, min(wave_first + kQ, nq) + nk - nq) : nk;
-    const int block_low = a.causal ? q0 + nk - nq + 1 : nk;  // seen by all queries of the tile
     const int keys = a.causal ? min(nk, min(q0 + kTileQ, nq) + nk - nq) : nk;  // seen by any query of the tile
-    T8 q[D / 16];
+    Wave<D, T> w;
+    w.hf = hf;
+    w.at_k = i * D + (hf ^ turn_k<D>(i)) * 8;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) {
+        const int row = 4 * hf + (i & 15) / 4, dim = 32 * d + (i & 16) + 4 * (i & 3);
+        w.at_v[d] = row * D + ((dim / 8) ^ turn_v<D>(row)) * 8 + dim % 8;
+    }
+    w.scale = scale_log2;
+    w.m = -FLT_MAX;
+    w.l = 0.0f;
     {
         const T* x = static_cast<const T*>(a.q.p) + (q_first + min(qi, nq - 1)) * a.q.ts + head * a.q.hs + 8 * hf;
 #pragma unroll
-        for (int n = 0; n < D / 16; ++n) q[n] = *reinterpret_cast<const T8*>(x + 16 * n);
+        for (int n = 0; n < D / 16; ++n) w.q[n] = *reinterpret_cast<const T8*>(x + 16 * n);
     }
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) w.o[d] = f32x16{};
     const T* kp = static_cast<const T*>(a.k.p) + k_first * a.k.ts + kv * a.k.hs;
     const T* vp = static_cast<const T*>(a.v.p) + k_first * a.v.ts + kv * a.v.hs;
-
-    float m = -FLT_MAX, l = 0.0f;
-    f32x16 o[D / 32];
+    uint32_t off_k[kLoads], off_v[kLoads];
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d) o[d] = f32x16{};
-
-    if (threadIdx.x == 0) bad_tile = 0;
-    const int tiles = keys > 0 ? (keys + kKeys - 1) / kKeys : 0;
-    if (tiles > 0) {
-        load_tile<D, T, false>(kp, a.k.ts, min(kKeys, nk), sk[0], wave, lane);
-        load_tile<D, T, true>(vp, a.v.ts, min(kKeys, nk), sv[0], wave, lane);
+    for (int n = 0; n < kLoads; ++n) {
+        off_k[n] = load_offset<D, false>(n, threadIdx.x % kThreads, a.k.ts);
+        off_v[n] = load_offset<D, true>(n, threadIdx.x % kThreads, a.v.ts);
     }
-    for (int t = 0; t < tiles; ++t) {
-        __syncthreads();  // the tile is there, and its predecessor's buffer free
-        const int k0 = t * kKeys;
-        if (a.causal && k0 + kKeys > block_low) {  // queries see different keys
-            bool bad = false;
-            u32x4* w = reinterpret_cast<u32x4*>(sv[t & 1]) + threadIdx.x;
+    // the group's tile t is tile 2t + group of the keys
+    const auto load_k = [&](int t, T* to) __attribute__((always_inline)) {
+        const int k0 = min((2 * t + group) * kKeys, (nk - 1) / kKeys * kKeys);  // one past the end is not used
+        load_tile<D, T>(kp + k0 * a.k.ts, a.k.ts, min(kKeys, nk - k0), off_k, to, wave);
+    };
+    const auto load_v = [&](int t, T* to) __attribute__((always_inline)) {
+        const int k0 = min((2 * t + group) * kKeys, (nk - 1) / kKeys * kKeys);
+        load_tile<D, T>(vp + k0 * a.v.ts, a.v.ts, min(kKeys, nk - k0), off_v, to, wave);
+    };
+
+    // Tiles of the group: those before `whole` are seen whole by all the wave's
+    // queries, those from `over` on by none.
+    const int steps = keys > 0 ? ((keys + kKeys - 1) / kKeys + 1) / 2 : 0;
+    const int whole = (max(0, wave_low / kKeys - group) + 1) / 2;
+    const int over = (max(0, (max(0, wave_high) + kKeys - 1) / kKeys - group) + 1) / 2;
+
+    // of both groups, but for the last
+    const int block_low = a.causal ? q0 + nk - nq + 1 : nk;  // seen by all queries of the tile
+    const int plain = min(steps - 1, max(0, block_low / kKeys) / 2);
+    Spoiled spoiled{0, 0};
+
+    // The groups alternate: while one multiplies (the values of its last tile,
+    // the scores of its next), the other makes its weights, so that every
+    // SIMD, which has a wave of either, has work for its matrix core all the
+    // time.  Group 1 is a phase behind.  Keys come two tiles ahead, values one.
+    if (steps > 0) {
+        load_k(0, sk[group][0]);
+        load_v(0, sv[group][0]);
+        if (steps > 1) load_k(1, sk[group][1]);
+        wait_loads<0>();
+        // (the queries too: the compiler would go on waiting for them in the loop)
 #pragma unroll
-            for (int n = 0; n < kKeys * D / 8 / kThreads; ++n)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) bad |= not_finite<T>(w[n * kThreads][x]);
-            if (bad) bad_tile = t + 1;
-            __syncthreads();
-            if (bad_tile == t + 1) {
-                add_not_finite<D, T>(sv[t & 1], k0, limit, lane, o);
-                __syncthreads();
-#pragma unroll
-                for (int n = 0; n < kKeys * D / 8 / kThreads; ++n)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) w[n * kThreads][x] = finite_only<T>(w[n * kThreads][x]);
-                __syncthreads();
+        for (int n = 0; n < D / 16; ++n) asm volatile("" : "+v"(w.q[n]));
+        phase();
+        if (group) phase();
+        if (over > 0) w.scores(sk[group][0]);
+        phase();
+        int t = 0;
+        // tiles that all the workgroup's queries see whole
+        for (; t < plain; ++t) {
+            if (t + 2 < steps) load_k(t + 2, sk[group][t & 1]);
+            load_v(t + 1, sv[group][(t + 1) & 1]);
+            w.weights();
+            // the next tile's keys and this one's values have to be there
+            if (t + 2 < steps) wait_loads<2 * kLoads>();
+            else wait_loads<kLoads>();
+            phase();
+            __builtin_amdgcn_s_setprio(1);
+            w.template values<false>(sv[group][t & 1]);
+            w.scores(sk[group][(t + 1) & 1]);
+            schedule_products<D>();
+            __builtin_amdgcn_s_setprio(0);
+            phase();
+        }
+        // and the others
+        for (; t < steps; ++t) {
+            T* const v_now = sv[group][t & 1];
+            if (t + 2 < steps) load_k(t + 2, sk[group][t & 1]);
+            if (t + 1 < steps) load_v(t + 1, sv[group][(t + 1) & 1]);
+            const int k0 = (2 * t + group) * kKeys;
+            if (t < over) {
+                if (t >= whole) w.mask(k0, limit);
+                w.weights();
             }
-        }
-        if (t + 1 < tiles) {
-            const int k1 = (t + 1) * kKeys;
-            load_tile<D, T, false>(kp + k1 * a.k.ts, a.k.ts, min(kKeys, nk - k1), sk[(t + 1) & 1], wave, lane);
-            load_tile<D, T, true>(vp + k1 * a.v.ts, a.v.ts, min(kKeys, nk - k1), sv[(t + 1) & 1], wave, lane);
-        }
-        if (k0 >= wave_high) continue;
-        const T* ks = sk[t & 1];
-        const T* vs = sv[t & 1];
-        f32x16 s[2] = {};
-#pragma unroll
-        for (int n = 0; n < D / 16; ++n)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int row = 32 * x + i;
-                const T8 k8 = *reinterpret_cast<const T8*>(ks + row * D + ((2 * n + hf) ^ turn_k<D>(row)) * 8);
-                s[x] = mfma(k8, q[n], s[x]);
+            if (t + 2 < steps) wait_loads<2 * kLoads>();
+            else if (t + 1 < steps) wait_loads<kLoads>();
+            else wait_loads<0>();
+            phase();
+            if (t < over) {
+                if (a.causal && t >= whole && any_not_finite<D, T>(v_now, lane)) {
+                    mark_not_finite<D, T>(v_now, k0, limit, lane, spoiled);
+                    w.template values<true>(v_now);
+                } else {
+                    w.template values<false>(v_now);
+                }
             }
-        if (k0 + kKeys > wave_low) {
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (k0 + 32 * x + 8 * (r / 4) + 4 * hf + r % 4 >= limit) s[x][r] = -INFINITY;
+            if (t + 1 < over) w.scores(sk[group][(t + 1) & 1]);
+            phase();
         }
-        float top = s[0][0];
+        if (!group) phase();
+    }
+
+    if (__any((spoiled.up | spoiled.down) != 0)) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[x][r]);
-        top *= scale_log2;
-        if (__any(top > m + kSlack)) {
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float m2 = fmaxf(m, top), c = exp2_(m - m2);
-            m = m2;
-            l *= c;
-#pragma unroll
-            for (int d = 0; d < D / 32; ++d) o[d] *= c;
-        }
-        T8 p[4];
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int d = 0; d < D / 32; ++d)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const float w = exp2_(__builtin_fmaf(s[x][r], scale_log2, -m));
-                l += w;
-                p[2 * x + r / 8][r % 8] = static_cast<T>(w);
-            }
-#pragma unroll
-        for (int n = 0; n < 4; ++n)
-#pragma unroll
-            for (int d = 0; d < D / 32; ++d) {
-                // keys 16n + 4hf + 0..3 and + 8..11 of dim 32d + i
-                s16x4 part[2];
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int row = 16 * n + 8 * x + 4 * hf + (i & 15) / 4;
-                    const int dim = 32 * d + (i & 16) + 4 * (i & 3);
-                    const T* at = vs + row * D + ((dim / 8) ^ turn_v<D>(row)) * 8 + dim % 8;
-                    part[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
-                }
-                const T8 v8 = __builtin_bit_cast(T8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
-                o[d] = mfma(v8, p[n], o[d]);
+                const bool up = spoiled.up >> (16 * d + r) & 1, down = spoiled.down >> (16 * d + r) & 1;
+                w.o[d][r] += up && down ? __builtin_nanf("") : up ? INFINITY : down ? -INFINITY : 0.0f;
             }
     }
 
-    l += __shfl_xor(l, 32);
-    if (!live) return;
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    // group 1 hands its part over: every lane of group 0 has the same queries and dims as its twin
+    w.l += __shfl_xor(w.l, 32);
+    const int twin = threadIdx.x % kThreads;
+    float* half0 = reinterpret_cast<float*>(sk[0]);  // dims below D / 2
+    float* half1 = reinterpret_cast<float*>(sk[1]);
+    float* ml = reinterpret_cast<float*>(sv[0]);
+    if (steps > 0) {
+        if (group) {
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    (d < D / 64 ? half0 : half1)[(d % (D / 64) * 16 + r) * kThreads + twin] = w.o[d][r];
+            ml[twin] = w.m;
+            ml[kThreads + twin] = w.l;
+        }
+        __syncthreads();
+    }
+    if (group || !live) return;
+    if (steps > 0) {
+        const float m1 = ml[twin], l1 = ml[kThreads + twin], m2 = fmaxf(w.m, m1);
+        const float c0 = exp2_(w.m - m2), c1 = exp2_(m1 - m2);
+        w.m = m2;
+        w.l = w.l * c0 + l1 * c1;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                w.o[d][r] = w.o[d][r] * c0 + (d < D / 64 ? half0 : half1)[(d % (D / 64) * 16 + r) * kThreads + twin] * c1;
+    }
+    const float inv = w.l == 0.0f ? 0.0f : 1.0f / w.l;
     T* to = static_cast<T*>(a.out.p) + (q_first + qi) * a.out.ts + head * a.out.hs + 4 * hf;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
@@ -269,16 +442,16 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, float
             typedef T T4 __attribute__((ext_vector_type(4)));
             T4 v;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) v[x] = static_cast<T>(o[d][4 * r + x] * inv);
+            for (int x = 0; x < 4; ++x) v[x] = static_cast<T>(w.o[d][4 * r + x] * inv);
             *reinterpret_cast<T4*>(to + 32 * d + 8 * r) = v;
         }
-    if (a.lse && hf == 0) a.lse[(q_first + qi) * a.q_heads + head] = (m + log2f(l)) * kLn2;
+    if (a.lse && hf == 0) a.lse[(q_first + qi) * a.q_heads + head] = (w.m + log2f(w.l)) * kLn2;
 }
 
 template <int D, typename T>
 hipError_t run(const PromptArgs& a, hipStream_t s) {
     const int64_t tiles = a.q_tokens / 128 + a.sequences;
-    prompt_kernel<D, T><<<static_cast<uint32_t>(tiles * a.q_heads), kThreads, 0, s>>>(a, a.scale * kLog2e);
+    prompt_kernel<D, T><<<static_cast<uint32_t>(tiles * a.q_heads), 2 * kThreads, 0, s>>>(a, a.scale * kLog2e);
     return hipGetLastError();
 }
 
