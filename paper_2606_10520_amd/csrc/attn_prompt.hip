@@ -25,6 +25,7 @@ namespace {
 constexpr int kThreads = 256, kWaves = 4, kKeys = 64;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kSlack = 8.0f;
+constexpr uint32_t kResident = 512;  // workgroups that the GPU holds at once
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -227,20 +228,24 @@ struct Wave {
 };
 
 template <int D, typename T>
-__global__ __launch_bounds__(2 * kThreads, 1) void prompt_kernel(PromptArgs a, float scale_log2) {
+__global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, float scale_log2) {
     typedef typename Vec8<T>::type T8;
     constexpr int kQ = 32, kTileQ = kQ * kWaves, kTile = kKeys * D;
     constexpr int kLoads = kTile * 2 / (16 * kThreads);  // loads a thread of a tile of keys or values
-    __shared__ __attribute__((aligned(16))) T sk[2][2][kTile];  // two tiles of keys for either group
-    __shared__ __attribute__((aligned(16))) T sv[2][2][kTile];  // and of values
-    const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64 % kWaves), lane = threadIdx.x & 63;
+    __shared__ __attribute__((aligned(16))) T sk[2][kTile];  // two tiles of keys
+    __shared__ __attribute__((aligned(16))) T sv[2][kTile];  // and of values
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
     const int i = lane & 31, hf = lane >> 5;
 
     // heads of one key head go to one XCD (workgroups go round the eight)
     int head = blockIdx.x % a.q_heads;
     if (a.q_heads % 8 == 0) head = head % 8 * (a.q_heads / 8) + head / 8;
-    int64_t tile = gridDim.x / a.q_heads - 1 - blockIdx.x / a.q_heads;  // late tiles see most keys: first
+    // Late tiles see most keys, so they go first.  Where all workgroups are
+    // resident at once, two a CU, those that come second on a CU go from the
+    // fewest keys up, to share it with the most.
+    const int64_t rank = blockIdx.x / a.q_heads, count = gridDim.x / a.q_heads;
+    int64_t tile = count - 1 - rank;
+    if (gridDim.x <= kResident && rank >= (count + 1) / 2) tile = rank - (count + 1) / 2;
     // the sequence of the tile
     int b = 0;
     int64_t first = 0;
@@ -308,77 +313,62 @@ __global__ __launch_bounds__(2 * kThreads, 1) void prompt_kernel(PromptArgs a, f
     uint32_t off_k[kLoads], off_v[kLoads];
 #pragma unroll
     for (int n = 0; n < kLoads; ++n) {
-        off_k[n] = load_offset<D, false>(n, threadIdx.x % kThreads, a.k.ts);
-        off_v[n] = load_offset<D, true>(n, threadIdx.x % kThreads, a.v.ts);
+        off_k[n] = load_offset<D, false>(n, threadIdx.x, a.k.ts);
+        off_v[n] = load_offset<D, true>(n, threadIdx.x, a.v.ts);
     }
-    // the group's tile t is tile 2t + group of the keys
-    const auto load_k = [&](int t, T* to) __attribute__((always_inline)) {
-        const int k0 = min((2 * t + group) * kKeys, (nk - 1) / kKeys * kKeys);  // one past the end is not used
-        load_tile<D, T>(kp + k0 * a.k.ts, a.k.ts, min(kKeys, nk - k0), off_k, to, wave);
+    const auto load_k = [&](int t) __attribute__((always_inline)) {
+        const int k0 = t * kKeys;
+        load_tile<D, T>(kp + k0 * a.k.ts, a.k.ts, min(kKeys, nk - k0), off_k, sk[t & 1], wave);
     };
-    const auto load_v = [&](int t, T* to) __attribute__((always_inline)) {
-        const int k0 = min((2 * t + group) * kKeys, (nk - 1) / kKeys * kKeys);
-        load_tile<D, T>(vp + k0 * a.v.ts, a.v.ts, min(kKeys, nk - k0), off_v, to, wave);
+    const auto load_v = [&](int t) __attribute__((always_inline)) {
+        const int k0 = t * kKeys;
+        load_tile<D, T>(vp + k0 * a.v.ts, a.v.ts, min(kKeys, nk - k0), off_v, sv[t & 1], wave);
     };
 
-    // Tiles of the group: those before `whole` are seen whole by all the wave's
-    // queries, those from `over` on by none.
-    const int steps = keys > 0 ? ((keys + kKeys - 1) / kKeys + 1) / 2 : 0;
-    const int whole = (max(0, wave_low / kKeys - group) + 1) / 2;
-    const int over = (max(0, (max(0, wave_high) + kKeys - 1) / kKeys - group) + 1) / 2;
-
-    // of both groups, but for the last
-    const int block_low = a.causal ? q0 + nk - nq + 1 : nk;  // seen by all queries of the tile
-    const int plain = min(steps - 1, max(0, block_low / kKeys) / 2);
+    // Tiles: those before `plain` are seen whole by all the workgroup's
+    // queries (the last is not counted), before `whole` by the wave's, and
+    // those from `over` on by none of the wave's.
+    const int tiles = keys > 0 ? (keys + kKeys - 1) / kKeys : 0;
+    const int block_low = a.causal ? q0 + nk - nq + 1 : nk;
+    const int plain = min(tiles - 1, max(0, block_low) / kKeys);
+    const int whole = max(0, wave_low) / kKeys;
+    const int over = (max(0, wave_high) + kKeys - 1) / kKeys;
     Spoiled spoiled{0, 0};
 
-    // The groups alternate: while one multiplies (the values of its last tile,
-    // the scores of its next), the other makes its weights, so that every
-    // SIMD, which has a wave of either, has work for its matrix core all the
-    // time.  Group 1 is a phase behind.  Keys come two tiles ahead, values one.
-    if (steps > 0) {
-        load_k(0, sk[group][0]);
-        load_v(0, sv[group][0]);
-        if (steps > 1) load_k(1, sk[group][1]);
+    // Tile t's weights; then its values and the next tile's scores in one go,
+    // with the loads of the tiles after them: one barrier a tile.
+    if (tiles > 0) {
+        load_k(0);
+        load_v(0);
+        if (tiles > 1) load_k(1);
         wait_loads<0>();
         // (the queries too: the compiler would go on waiting for them in the loop)
 #pragma unroll
         for (int n = 0; n < D / 16; ++n) asm volatile("" : "+v"(w.q[n]));
         phase();
-        if (group) phase();
-        if (over > 0) w.scores(sk[group][0]);
-        phase();
+        if (over > 0) w.scores(sk[0]);
         int t = 0;
-        // tiles that all the workgroup's queries see whole
         for (; t < plain; ++t) {
-            if (t + 2 < steps) load_k(t + 2, sk[group][t & 1]);
-            load_v(t + 1, sv[group][(t + 1) & 1]);
             w.weights();
-            // the next tile's keys and this one's values have to be there
-            if (t + 2 < steps) wait_loads<2 * kLoads>();
-            else wait_loads<kLoads>();
-            phase();
-            __builtin_amdgcn_s_setprio(1);
-            w.template values<false>(sv[group][t & 1]);
-            w.scores(sk[group][(t + 1) & 1]);
+            wait_loads<0>();
+            phase();  // keys t + 1 and values t are there; keys t and values t - 1 are done with
+            if (t + 2 < tiles) load_k(t + 2);
+            load_v(t + 1);
+            w.template values<false>(sv[t & 1]);
+            w.scores(sk[(t + 1) & 1]);
             schedule_products<D>();
-            __builtin_amdgcn_s_setprio(0);
-            phase();
         }
-        // and the others
-        for (; t < steps; ++t) {
-            T* const v_now = sv[group][t & 1];
-            if (t + 2 < steps) load_k(t + 2, sk[group][t & 1]);
-            if (t + 1 < steps) load_v(t + 1, sv[group][(t + 1) & 1]);
-            const int k0 = (2 * t + group) * kKeys;
+        for (; t < tiles; ++t) {
+            const T* const v_now = sv[t & 1];
+            const int k0 = t * kKeys;
             if (t < over) {
                 if (t >= whole) w.mask(k0, limit);
                 w.weights();
             }
-            if (t + 2 < steps) wait_loads<2 * kLoads>();
-            else if (t + 1 < steps) wait_loads<kLoads>();
-            else wait_loads<0>();
+            wait_loads<0>();
             phase();
+            if (t + 2 < tiles) load_k(t + 2);
+            if (t + 1 < tiles) load_v(t + 1);
             if (t < over) {
                 if (a.causal && t >= whole && any_not_finite<D, T>(v_now, lane)) {
                     mark_not_finite<D, T>(v_now, k0, limit, lane, spoiled);
@@ -387,10 +377,8 @@ __global__ __launch_bounds__(2 * kThreads, 1) void prompt_kernel(PromptArgs a, f
                     w.template values<false>(v_now);
                 }
             }
-            if (t + 1 < over) w.scores(sk[group][(t + 1) & 1]);
-            phase();
+            if (t + 1 < over) w.scores(sk[(t + 1) & 1]);
         }
-        if (!group) phase();
     }
 
     if (__any((spoiled.up | spoiled.down) != 0)) {
@@ -403,36 +391,8 @@ __global__ __launch_bounds__(2 * kThreads, 1) void prompt_kernel(PromptArgs a, f
             }
     }
 
-    // group 1 hands its part over: every lane of group 0 has the same queries and dims as its twin
     w.l += __shfl_xor(w.l, 32);
-    const int twin = threadIdx.x % kThreads;
-    float* half0 = reinterpret_cast<float*>(sk[0]);  // dims below D / 2
-    float* half1 = reinterpret_cast<float*>(sk[1]);
-    float* ml = reinterpret_cast<float*>(sv[0]);
-    if (steps > 0) {
-        if (group) {
-#pragma unroll
-            for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    (d < D / 64 ? half0 : half1)[(d % (D / 64) * 16 + r) * kThreads + twin] = w.o[d][r];
-            ml[twin] = w.m;
-            ml[kThreads + twin] = w.l;
-        }
-        __syncthreads();
-    }
-    if (group || !live) return;
-    if (steps > 0) {
-        const float m1 = ml[twin], l1 = ml[kThreads + twin], m2 = fmaxf(w.m, m1);
-        const float c0 = exp2_(w.m - m2), c1 = exp2_(m1 - m2);
-        w.m = m2;
-        w.l = w.l * c0 + l1 * c1;
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                w.o[d][r] = w.o[d][r] * c0 + (d < D / 64 ? half0 : half1)[(d % (D / 64) * 16 + r) * kThreads + twin] * c1;
-    }
+    if (!live) return;
     const float inv = w.l == 0.0f ? 0.0f : 1.0f / w.l;
     T* to = static_cast<T*>(a.out.p) + (q_first + qi) * a.out.ts + head * a.out.hs + 4 * hf;
 #pragma unroll
@@ -450,8 +410,8 @@ __global__ __launch_bounds__(2 * kThreads, 1) void prompt_kernel(PromptArgs a, f
 
 template <int D, typename T>
 hipError_t run(const PromptArgs& a, hipStream_t s) {
-    const int64_t tiles = a.q_tokens / 128 + a.sequences;
-    prompt_kernel<D, T><<<static_cast<uint32_t>(tiles * a.q_heads), 2 * kThreads, 0, s>>>(a, a.scale * kLog2e);
+    const int64_t tiles = (a.q_tokens + 127 * a.sequences) / 128;  // at most, of sequences that fill their last one anyhow
+    prompt_kernel<D, T><<<static_cast<uint32_t>(tiles * a.q_heads), kThreads, 0, s>>>(a, a.scale * kLog2e);
     return hipGetLastError();
 }
 
