@@ -228,7 +228,8 @@ int unisvq_attn_prompt(int64_t sequences, int64_t q_tokens, int64_t k_tokens, co
     const int64_t wide = int64_t{1} << 22;
     if (k_token_stride < head_dim || k_token_stride > wide || v_token_stride < head_dim || v_token_stride > wide)
         return UNISVQ_EUNSUP;
-    if ((q_tokens / 64 + sequences) > kMost / q_heads) return UNISVQ_EUNSUP;
+    // rows and workgroups (of up to 32 parts) are counted in 32 bits
+    if (q_tokens > kMost / q_heads || q_tokens * q_heads / 128 + sequences * kv_heads > kMost / 2) return UNISVQ_EUNSUP;
     const size_t need = unisvq::prompt_workspace_bytes(sequences, q_tokens, k_tokens, static_cast<int>(q_heads),
                                                        static_cast<int>(kv_heads), static_cast<int>(head_dim));
     if (need) {

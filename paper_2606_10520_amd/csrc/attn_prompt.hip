@@ -15,6 +15,7 @@
 // So a query's maximum and sum need one exchange between the halves of a wave,
 // the maximum's only when a score exceeds it by 2^8 (the weights stay below
 // 2^8, so nothing overflows, and most tiles need no rescaling).
+#include <algorithm>
 #include <cfloat>
 
 #include "attn.hpp"
@@ -22,10 +23,10 @@
 namespace unisvq {
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4, kKeys = 64;
+constexpr int kThreads = 256, kWaves = 4, kKeys = 64, kTileQ = 128;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kSlack = 8.0f;
-constexpr uint32_t kResident = 512;  // workgroups that the GPU holds at once
+constexpr int64_t kResident = 512;  // workgroups that the GPU holds at once, two a CU
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -104,23 +105,51 @@ __device__ inline void mark_not_finite(const T* vs, int k0, int limit, int lane,
     }
 }
 
-// Whether the tile at `vs` holds a value that is not finite (the whole wave's answer).
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// Whether the wave's quarter of the tile at `vs` holds a value that is not finite.
 template <int D, typename T>
-__device__ inline bool any_not_finite(const T* vs, int lane) {
-    bool bad = false;
-#pragma unroll 4
-    for (int at = lane; at < kKeys * D / 8; at += 64) {
-        const u32x4 w = reinterpret_cast<const u32x4*>(vs)[at];
+__device__ inline bool any_not_finite(const T* vs, int wave, int lane) {
+    u16x2 top = {0, 0};  // largest magnitudes: exponents of all ones are above every finite one
+    const u32x4* at = reinterpret_cast<const u32x4*>(vs) + wave * (kKeys * D / 8 / kWaves) + lane;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) bad |= not_finite<T>(w[x]);
-    }
-    return __any(bad);
+    for (int n = 0; n < kKeys * D / 8 / kThreads; ++n)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, at[64 * n][x] & 0x7fff7fffu));
+    return __any(top[0] >= exponent_bits<T>() || top[1] >= exponent_bits<T>());
+}
+
+// Zeros in place of them.
+template <int D, typename T>
+__device__ inline void drop_not_finite(T* vs, int wave, int lane) {
+    u32x4* at = reinterpret_cast<u32x4*>(vs) + wave * (kKeys * D / 8 / kWaves) + lane;
+#pragma nounroll
+    for (int n = 0; n < kKeys * D / 8 / kThreads; ++n)
+        for (int x = 0; x < 4; ++x) at[64 * n][x] = finite_only<T>(at[64 * n][x]);
+}
+
+// Sum over the lanes up to this one.
+__device__ inline int scan64(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
 }
 
 // A barrier of all waves that waits for no loads in flight.
 __device__ inline void phase() {
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// One that waits for the wave's own reads and writes of LDS.
+__device__ inline void local_phase() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -157,8 +186,7 @@ struct Wave {
     int at_k;           // keys: row i of a tile, chunk hf as it is turned (chunk 2n + hf is at_k ^ 16n)
     int at_v[D / 32];   // values: row 4hf + (i % 16) / 4, the lane's four dims of dim tile d
 
-    // o += V^T P^T for the tile at vs; CLEAN: values that are not finite count as zero.
-    template <bool CLEAN>
+    // o += V^T P^T for the tile at vs.
     __device__ __forceinline__ void values(const T* vs) {
 #pragma unroll
         for (int n = 0; n < 4; ++n)
@@ -169,12 +197,7 @@ struct Wave {
                     (__attribute__((address_space(3))) s16x4*)(vs + at_v[d] + 16 * n * D));
                 const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                     (__attribute__((address_space(3))) s16x4*)(vs + at_v[d] + (16 * n + 8) * D));
-                u32x4 v4 = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-                if constexpr (CLEAN)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) v4[x] = finite_only<T>(v4[x]);
-                const T8 v8 = __builtin_bit_cast(T8, v4);
-                o[d] = mfma(v8, p[n], o[d]);
+                o[d] = mfma(__builtin_bit_cast(T8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)), p[n], o[d]);
             }
     }
 
@@ -227,157 +250,173 @@ struct Wave {
     }
 };
 
-template <int D, typename T>
-__global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, float scale_log2) {
+struct Prompt {
+    PromptArgs a;
+    float scale_log2;
+    int group;        // query heads of a key head
+    int splits;       // parts that a tile's keys are split into, a workgroup each
+    float* part;      // [query][head][splits][D] sums of the parts, where there are several
+    float2* part_ml;  // and their maximum (log2) and sum
+};
+
+// STAGES: tiles of keys and of values in LDS.  Two let two workgroups share a
+// CU, whose waves then cover each other's waits; three, for grids of no more
+// workgroups than CUs, bring a tile two steps ahead.
+template <int D, typename T, int STAGES>
+__global__ __launch_bounds__(kThreads, STAGES == 2 ? 2 : 1) void prompt_kernel(Prompt g) {
     typedef typename Vec8<T>::type T8;
-    constexpr int kQ = 32, kTileQ = kQ * kWaves, kTile = kKeys * D;
+    const PromptArgs& a = g.a;
+    constexpr int kQ = 32, kTile = kKeys * D, kChunks = D / 8;
     constexpr int kLoads = kTile * 2 / (16 * kThreads);  // loads a thread of a tile of keys or values
-    __shared__ __attribute__((aligned(16))) T sk[2][kTile];  // two tiles of keys
-    __shared__ __attribute__((aligned(16))) T sv[2][kTile];  // and of values
+    __shared__ __attribute__((aligned(16))) T sk[STAGES][kTile];
+    __shared__ __attribute__((aligned(16))) T sv[STAGES][kTile];
+    __shared__ int64_t row_at[kTileQ];
+    __shared__ int bad_tile;  // 1 + the last tile found to hold values that are not finite
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
     const int i = lane & 31, hf = lane >> 5;
 
-    // heads of one key head go to one XCD (workgroups go round the eight)
-    int head = blockIdx.x % a.q_heads;
-    if (a.q_heads % 8 == 0) head = head % 8 * (a.q_heads / 8) + head / 8;
+    // workgroups of a key head go to one XCD (they go round the eight)
+    const int parts = a.kv_heads * g.splits;
+    int kv = blockIdx.x % parts;
+    const int part = kv / a.kv_heads;
+    kv %= a.kv_heads;
+    if (a.kv_heads % 8 == 0) kv = kv % 8 * (a.kv_heads / 8) + kv / 8;
     // Late tiles see most keys, so they go first.  Where all workgroups are
     // resident at once, two a CU, those that come second on a CU go from the
     // fewest keys up, to share it with the most.
-    const int64_t rank = blockIdx.x / a.q_heads, count = gridDim.x / a.q_heads;
-    int64_t tile = count - 1 - rank;
-    if (gridDim.x <= kResident && rank >= (count + 1) / 2) tile = rank - (count + 1) / 2;
-    // the sequence of the tile
-    int b = 0;
-    int64_t first = 0;
-    bool found = false;
-    for (int base = 0; base < a.sequences && !found; base += 64) {
-        int tiles = 0;
+    const int rank = blockIdx.x / parts, count = gridDim.x / parts;
+    int tile = count - 1 - rank;
+    if (gridDim.x <= kResident && gridDim.x > kResident / 2 && rank >= (count + 1) / 2) tile = rank - (count + 1) / 2;
+    // the sequence of the tile: its tiles are its queries times the group's heads, 128 a tile
+    int first = 0, q_first = 0, nq = 0, k_first = 0, nk = 0;
+    for (int base = 0;; base += 64) {
+        if (base >= a.sequences) return;
+        int c0 = 0, c1 = 0, d0 = 0, d1 = 0;
         if (base + lane < a.sequences) {
-            const int64_t q0 = min(static_cast<int64_t>(max(0, a.cu_q[base + lane])), a.q_tokens);
-            const int64_t q1 = min(static_cast<int64_t>(max(0, a.cu_q[base + lane + 1])), a.q_tokens);
-            tiles = q1 > q0 ? static_cast<int>((q1 - q0 + kTileQ - 1) / kTileQ) : 0;
+            c0 = a.cu_q[base + lane], c1 = a.cu_q[base + lane + 1];
+            d0 = a.cu_k[base + lane], d1 = a.cu_k[base + lane + 1];
         }
-        int sum = tiles;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int up = __shfl_up(sum, d);
-            if (lane >= d) sum += up;
-        }
+        const int most_q = static_cast<int>(a.q_tokens), most_k = static_cast<int>(a.k_tokens);
+        c0 = min(max(c0, 0), most_q), c1 = min(max(c1, c0), most_q), d0 = min(max(d0, 0), most_k), d1 = min(max(d1, d0), most_k);
+        const int tiles = ((c1 - c0) * g.group + kTileQ - 1) / kTileQ;
+        const int sum = scan64(tiles);
         const uint64_t in = __ballot(tile < first + sum);
         if (in) {
             const int l = __ffsll(static_cast<unsigned long long>(in)) - 1;
-            b = base + l;
-            first += __shfl(sum - tiles, l);
-            found = true;
-        } else {
-            first += __shfl(sum, 63);
+            first += __builtin_amdgcn_readlane(sum - tiles, l);
+            q_first = __builtin_amdgcn_readlane(c0, l);
+            nq = __builtin_amdgcn_readlane(c1, l) - q_first;
+            k_first = __builtin_amdgcn_readlane(d0, l);
+            nk = __builtin_amdgcn_readlane(d1, l) - k_first;
+            break;
         }
+        first += __builtin_amdgcn_readlane(sum, 63);
     }
-    if (!found) return;
-    b = __builtin_amdgcn_readfirstlane(b);
-    const int64_t q_first = max(0, a.cu_q[b]);
-    const int nq = static_cast<int>(min(static_cast<int64_t>(a.cu_q[b + 1]), a.q_tokens) - q_first);
-    const int64_t k_first = min(static_cast<int64_t>(max(0, a.cu_k[b])), a.k_tokens);
-    const int nk = static_cast<int>(max(int64_t{0}, min(static_cast<int64_t>(a.cu_k[b + 1]), a.k_tokens) - k_first));
-    const int q0 = __builtin_amdgcn_readfirstlane(static_cast<int>(tile - first)) * kTileQ;
-    const int kv = head / (a.q_heads / a.kv_heads);
+    // rows are (query, head of the group)
+    const int rows = nq * g.group, row0 = (tile - first) * kTileQ, wave_row = row0 + wave * kQ;
+    const int row = min(wave_row + i, rows - 1);
+    const bool live = wave_row + i < rows;
+    const int qi = row / g.group, head = kv * g.group + row - qi * g.group;
 
-    // the lane's query: keys below `limit` are seen
-    const int qi = q0 + wave * kQ + i;
-    const bool live = qi < nq;
-    const int limit = !live ? 0 : a.causal ? qi + nk - nq + 1 : nk;
-    const int wave_first = q0 + wave * kQ;
-    const int wave_low = a.causal ? wave_first + nk - nq + 1 : nk;  // seen by all its queries
-    const int wave_high = wave_first >= nq ? 0 : a.causal ? min(nk, min(wave_first + kQ, nq) + nk - nq) : nk;
-    const int keys = a.causal ? min(nk, min(q0 + kTileQ, nq) + nk - nq) : nk;  // seen by any query of the tile
+    // the lane's row: keys below `limit` are seen
+    const int more = nk - nq + 1;
+    const int limit = !live ? 0 : a.causal ? qi + more : nk;
+    const int wave_low = a.causal ? wave_row / g.group + more : nk;  // seen by all its rows
+    const int block_low = a.causal ? row0 / g.group + more : nk;  // seen by all rows of the tile
+    const int keys = a.causal ? min(nk, (min(row0 + kTileQ, rows) - 1) / g.group + more) : nk;  // seen by any
     Wave<D, T> w;
     w.hf = hf;
     w.at_k = i * D + (hf ^ turn_k<D>(i)) * 8;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) {
-        const int row = 4 * hf + (i & 15) / 4, dim = 32 * d + (i & 16) + 4 * (i & 3);
-        w.at_v[d] = row * D + ((dim / 8) ^ turn_v<D>(row)) * 8 + dim % 8;
+        const int r = 4 * hf + (i & 15) / 4, dim = 32 * d + (i & 16) + 4 * (i & 3);
+        w.at_v[d] = r * D + ((dim / 8) ^ turn_v<D>(r)) * 8 + dim % 8;
     }
-    w.scale = scale_log2;
+    w.scale = g.scale_log2;
     w.m = -FLT_MAX;
     w.l = 0.0f;
     {
-        const T* x = static_cast<const T*>(a.q.p) + (q_first + min(qi, nq - 1)) * a.q.ts + head * a.q.hs + 8 * hf;
+        const T* x = static_cast<const T*>(a.q.p) + static_cast<int64_t>(q_first + qi) * a.q.ts + head * a.q.hs + 8 * hf;
 #pragma unroll
         for (int n = 0; n < D / 16; ++n) w.q[n] = *reinterpret_cast<const T8*>(x + 16 * n);
     }
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) w.o[d] = f32x16{};
-    const T* kp = static_cast<const T*>(a.k.p) + k_first * a.k.ts + kv * a.k.hs;
-    const T* vp = static_cast<const T*>(a.v.p) + k_first * a.v.ts + kv * a.v.hs;
+
+    // The part's tiles of keys: those before `plain` are seen whole by all the
+    // workgroup's rows, before `whole` by the wave's.
+    const int all_tiles = keys > 0 ? (keys + kKeys - 1) / kKeys : 0;
+    const int from = static_cast<int>(static_cast<int64_t>(all_tiles) * part / g.splits);
+    const int tiles = static_cast<int>(static_cast<int64_t>(all_tiles) * (part + 1) / g.splits) - from;
+    const int plain = max(0, block_low) / kKeys - from;
+    const int whole = max(0, wave_low) / kKeys - from;
+    const int key0 = from * kKeys;
+    const T* kp = static_cast<const T*>(a.k.p) + static_cast<int64_t>(k_first + key0) * a.k.ts + kv * a.k.hs;
+    const T* vp = static_cast<const T*>(a.v.p) + static_cast<int64_t>(k_first + key0) * a.v.ts + kv * a.v.hs;
     uint32_t off_k[kLoads], off_v[kLoads];
 #pragma unroll
     for (int n = 0; n < kLoads; ++n) {
         off_k[n] = load_offset<D, false>(n, threadIdx.x, a.k.ts);
         off_v[n] = load_offset<D, true>(n, threadIdx.x, a.v.ts);
     }
-    const auto load_k = [&](int t) __attribute__((always_inline)) {
-        const int k0 = t * kKeys;
-        load_tile<D, T>(kp + k0 * a.k.ts, a.k.ts, min(kKeys, nk - k0), off_k, sk[t & 1], wave);
+    // tiles are loaded in turn
+    int left_k = nk - key0, left_v = left_k;  // rows from the next tile on
+    const auto load_k = [&](int slot) __attribute__((always_inline)) {
+        load_tile<D, T>(kp, a.k.ts, min(kKeys, left_k), off_k, sk[slot], wave);
+        kp += kKeys * a.k.ts;
+        left_k -= kKeys;
     };
-    const auto load_v = [&](int t) __attribute__((always_inline)) {
-        const int k0 = t * kKeys;
-        load_tile<D, T>(vp + k0 * a.v.ts, a.v.ts, min(kKeys, nk - k0), off_v, sv[t & 1], wave);
+    const auto load_v = [&](int slot) __attribute__((always_inline)) {
+        load_tile<D, T>(vp, a.v.ts, min(kKeys, left_v), off_v, sv[slot], wave);
+        vp += kKeys * a.v.ts;
+        left_v -= kKeys;
     };
-
-    // Tiles: those before `plain` are seen whole by all the workgroup's
-    // queries (the last is not counted), before `whole` by the wave's, and
-    // those from `over` on by none of the wave's.
-    const int tiles = keys > 0 ? (keys + kKeys - 1) / kKeys : 0;
-    const int block_low = a.causal ? q0 + nk - nq + 1 : nk;
-    const int plain = min(tiles - 1, max(0, block_low) / kKeys);
-    const int whole = max(0, wave_low) / kKeys;
-    const int over = (max(0, wave_high) + kKeys - 1) / kKeys;
     Spoiled spoiled{0, 0};
+    if (threadIdx.x == 0) bad_tile = 0;
 
     // Tile t's weights; then its values and the next tile's scores in one go,
     // with the loads of the tiles after them: one barrier a tile.
     if (tiles > 0) {
-        load_k(0);
-        load_v(0);
-        if (tiles > 1) load_k(1);
+#pragma unroll
+        for (int n = 0; n < STAGES; ++n) {
+            if (n < tiles) load_k(n);
+            if (n < STAGES - 1 && n < tiles) load_v(n);
+        }
         wait_loads<0>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         // (the queries too: the compiler would go on waiting for them in the loop)
 #pragma unroll
         for (int n = 0; n < D / 16; ++n) asm volatile("" : "+v"(w.q[n]));
         phase();
-        if (over > 0) w.scores(sk[0]);
-        int t = 0;
-        for (; t < plain; ++t) {
+        w.scores(sk[0]);
+        int slot = 0;  // t % STAGES
+        for (int t = 0; t < tiles; ++t) {
+            if (t >= whole) w.mask(key0 + t * kKeys, limit);
             w.weights();
-            wait_loads<0>();
-            phase();  // keys t + 1 and values t are there; keys t and values t - 1 are done with
-            if (t + 2 < tiles) load_k(t + 2);
-            load_v(t + 1);
-            w.template values<false>(sv[t & 1]);
-            w.scores(sk[(t + 1) & 1]);
-            schedule_products<D>();
-        }
-        for (; t < tiles; ++t) {
-            const T* const v_now = sv[t & 1];
-            const int k0 = t * kKeys;
-            if (t < over) {
-                if (t >= whole) w.mask(k0, limit);
-                w.weights();
-            }
-            wait_loads<0>();
-            phase();
-            if (t + 2 < tiles) load_k(t + 2);
-            if (t + 1 < tiles) load_v(t + 1);
-            if (t < over) {
-                if (a.causal && t >= whole && any_not_finite<D, T>(v_now, lane)) {
-                    mark_not_finite<D, T>(v_now, k0, limit, lane, spoiled);
-                    w.template values<true>(v_now);
-                } else {
-                    w.template values<false>(v_now);
+            // Keys t + 1 and values t have to be there; what was loaded after
+            // the last barrier may be on its way still.
+            if (STAGES == 2) wait_loads<0>();
+            else if (t + 2 < tiles) wait_loads<2 * kLoads>();
+            else if (t + 1 < tiles) wait_loads<kLoads>();
+            else wait_loads<0>();
+            phase();  // and keys t and values t - 1 are done with
+            if (t + STAGES < tiles) load_k(slot);
+            if (t + STAGES - 1 < tiles) load_v(slot == 0 ? STAGES - 1 : slot - 1);
+            T* const v_now = sv[slot];
+            if (a.causal && t >= plain) {  // rows see different keys
+                if (any_not_finite<D, T>(v_now, wave, lane)) bad_tile = t + 1;
+                local_phase();
+                if (bad_tile == t + 1) {
+                    mark_not_finite<D, T>(v_now, key0 + t * kKeys, limit, lane, spoiled);
+                    local_phase();
+                    drop_not_finite<D, T>(v_now, wave, lane);
+                    local_phase();
                 }
             }
-            if (t + 1 < over) w.scores(sk[(t + 1) & 1]);
+            slot = slot + 1 == STAGES ? 0 : slot + 1;
+            w.values(v_now);
+            w.scores(sk[slot]);  // (after the last tile: of what was there before, and not used)
+            schedule_products<D>();
         }
     }
 
@@ -390,11 +429,26 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, float
                 w.o[d][r] += up && down ? __builtin_nanf("") : up ? INFINITY : down ? -INFINITY : 0.0f;
             }
     }
-
     w.l += __shfl_xor(w.l, 32);
-    if (!live) return;
+    const int64_t out_row = static_cast<int64_t>(q_first + qi) * a.q_heads + head;
+    if (g.splits > 1) {
+        if (!live) return;
+        float* to = g.part + (out_row * g.splits + part) * D + 4 * hf;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                *reinterpret_cast<f32x4*>(to + 32 * d + 8 * r) =
+                    f32x4{w.o[d][4 * r], w.o[d][4 * r + 1], w.o[d][4 * r + 2], w.o[d][4 * r + 3]};
+        if (hf == 0) g.part_ml[out_row * g.splits + part] = float2{w.m, w.l};
+        return;
+    }
+    // Results go out through LDS, so that a row leaves as a whole.
     const float inv = w.l == 0.0f ? 0.0f : 1.0f / w.l;
-    T* to = static_cast<T*>(a.out.p) + (q_first + qi) * a.out.ts + head * a.out.hs + 4 * hf;
+    if (a.lse && live && hf == 0) a.lse[out_row] = (w.m + log2f(w.l)) * kLn2;
+    phase();  // all waves are done with the tiles
+    T* mine = sk[0] + wave * kQ * D;
+    if (hf == 0) row_at[wave * kQ + i] = live ? static_cast<int64_t>(q_first + qi) * a.out.ts + head * a.out.hs : -1;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -403,25 +457,89 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, float
             T4 v;
 #pragma unroll
             for (int x = 0; x < 4; ++x) v[x] = static_cast<T>(w.o[d][4 * r + x] * inv);
-            *reinterpret_cast<T4*>(to + 32 * d + 8 * r) = v;
+            *reinterpret_cast<T4*>(mine + i * D + ((4 * d + r) ^ (i & (kChunks - 1))) * 8 + 4 * hf) = v;
         }
-    if (a.lse && hf == 0) a.lse[(q_first + qi) * a.q_heads + head] = (w.m + log2f(w.l)) * kLn2;
+    __builtin_amdgcn_wave_barrier();  // a wave reads its own rows only
+#pragma unroll
+    for (int n = 0; n < kQ * kChunks / 64; ++n) {
+        const int r = (n * 64 + lane) / kChunks, place = lane % kChunks;
+        const T8 v = *reinterpret_cast<const T8*>(mine + r * D + place * 8);
+        const int64_t at = row_at[wave * kQ + r];
+        if (at >= 0) *reinterpret_cast<T8*>(static_cast<T*>(a.out.p) + at + (place ^ (r & (kChunks - 1))) * 8) = v;
+    }
+}
+
+// Joins the parts of a row, in their order; one wave a row.
+template <int D, typename T>
+__global__ __launch_bounds__(kThreads) void prompt_join_kernel(Prompt g) {
+    const PromptArgs& a = g.a;
+    const int64_t r = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
+    const int64_t token = r / a.q_heads;
+    if (token >= min(a.q_tokens, static_cast<int64_t>(a.cu_q[a.sequences]))) return;
+    const int head = static_cast<int>(r - token * a.q_heads), lane = threadIdx.x & 63;
+    const float2* ml = g.part_ml + r * g.splits;
+    float m = -FLT_MAX, l = 0.0f, f[D / 64] = {};
+    for (int x = 0; x < g.splits; ++x) m = fmaxf(m, ml[x].x);
+    for (int x = 0; x < g.splits; ++x) {
+        if (ml[x].y == 0.0f) continue;
+        const float c = exp2_(ml[x].x - m);
+        l += c * ml[x].y;
+        const float* from = g.part + (r * g.splits + x) * D + lane * (D / 64);
+#pragma unroll
+        for (int y = 0; y < D / 64; ++y) f[y] += c * from[y];
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    T* to = static_cast<T*>(a.out.p) + token * a.out.ts + head * a.out.hs + lane * (D / 64);
+#pragma unroll
+    for (int y = 0; y < D / 64; ++y) to[y] = static_cast<T>(f[y] * inv);
+    if (a.lse && lane == 0) a.lse[r] = (m + log2f(l)) * kLn2;
+}
+
+// Workgroups without a split, at most (every sequence may end with a part of a tile).
+int64_t prompt_blocks(int64_t sequences, int64_t q_tokens, int q_heads, int kv_heads) {
+    return (q_tokens * (q_heads / kv_heads) + (kTileQ - 1) * sequences) / kTileQ * kv_heads;
+}
+
+// Few rows before many keys: the keys are split so that there are about two
+// workgroups a CU, of at least four tiles each were all keys one sequence's.
+int prompt_splits(int64_t sequences, int64_t q_tokens, int64_t k_tokens, int q_heads, int kv_heads) {
+    const int64_t blocks = prompt_blocks(sequences, q_tokens, q_heads, kv_heads);
+    const int64_t n = std::min(kResident / std::max<int64_t>(1, blocks), k_tokens / (4 * kKeys));
+    return static_cast<int>(std::min<int64_t>(std::max<int64_t>(1, n), 32));
 }
 
 template <int D, typename T>
-hipError_t run(const PromptArgs& a, hipStream_t s) {
-    const int64_t tiles = (a.q_tokens + 127 * a.sequences) / 128;  // at most, of sequences that fill their last one anyhow
-    prompt_kernel<D, T><<<static_cast<uint32_t>(tiles * a.q_heads), kThreads, 0, s>>>(a, a.scale * kLog2e);
+hipError_t run(const PromptArgs& a, void* workspace, hipStream_t s) {
+    Prompt g{a, a.scale * kLog2e, a.q_heads / a.kv_heads, prompt_splits(a.sequences, a.q_tokens, a.k_tokens, a.q_heads, a.kv_heads),
+             nullptr, nullptr};
+    const int64_t rows = a.q_tokens * a.q_heads;
+    if (g.splits > 1) {
+        g.part = static_cast<float*>(workspace);
+        g.part_ml = reinterpret_cast<float2*>(g.part + rows * g.splits * D);
+    }
+    const uint32_t blocks = static_cast<uint32_t>(prompt_blocks(a.sequences, a.q_tokens, a.q_heads, a.kv_heads) * g.splits);
+    if (blocks <= kResident / 2)
+        prompt_kernel<D, T, 3><<<blocks, kThreads, 0, s>>>(g);
+    else
+        prompt_kernel<D, T, 2><<<blocks, kThreads, 0, s>>>(g);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || g.splits == 1) return e;
+    prompt_join_kernel<D, T><<<static_cast<uint32_t>((rows + kWaves - 1) / kWaves), kThreads, 0, s>>>(g);
     return hipGetLastError();
 }
 
 }  // namespace
 
-size_t prompt_workspace_bytes(int64_t, int64_t, int64_t, int, int, int) { return 0; }
+size_t prompt_workspace_bytes(int64_t sequences, int64_t q_tokens, int64_t k_tokens, int q_heads, int kv_heads,
+                              int head_dim) {
+    const int n = prompt_splits(sequences, q_tokens, k_tokens, q_heads, kv_heads);
+    return n == 1 ? 0 : static_cast<size_t>(q_tokens * q_heads) * n * (head_dim + 2) * 4;
+}
 
-hipError_t launch_attn_prompt(const PromptArgs& a, void*, hipStream_t s) {
-    if (a.head_dim == 128) return a.dtype == UNISVQ_F16 ? run<128, _Float16>(a, s) : run<128, __bf16>(a, s);
-    return a.dtype == UNISVQ_F16 ? run<64, _Float16>(a, s) : run<64, __bf16>(a, s);
+hipError_t launch_attn_prompt(const PromptArgs& a, void* workspace, hipStream_t s) {
+    if (a.head_dim == 128)
+        return a.dtype == UNISVQ_F16 ? run<128, _Float16>(a, workspace, s) : run<128, __bf16>(a, workspace, s);
+    return a.dtype == UNISVQ_F16 ? run<64, _Float16>(a, workspace, s) : run<64, __bf16>(a, workspace, s);
 }
 
 }  // namespace unisvq
