@@ -28,7 +28,7 @@
 // f16), so most tiles need no exchange between lanes and no rescaling.
 #include <cfloat>
 
-#include "attn.hpp"
+#include "attn_join.hpp"
 
 namespace unisvq {
 namespace {
@@ -491,39 +491,6 @@ __global__ __launch_bounds__(kThreads) void decode_kernel(Decode a) {
     }
 }
 
-// Joins the parts of a row; one wave a row, in the order of the parts.
-template <int D, typename XT>
-__global__ __launch_bounds__(kThreads) void join_kernel(Decode a, int64_t rows) {
-    const int64_t r = static_cast<int64_t>(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
-    if (r >= rows) return;
-    const int lane = threadIdx.x & 63;
-    const int64_t token = r / a.q_heads;
-    const int hq = static_cast<int>(r - token * a.q_heads);
-    const int64_t room = a.c.width << a.c.page_shift;
-    int64_t len = max(0, a.lens[token / a.q_len]);
-    if (len > room) len = room;
-    const int n = static_cast<int>(min(static_cast<int64_t>(a.splits), max(int64_t{1}, (len + a.chunk - 1) / a.chunk)));
-    float mt = -FLT_MAX;
-    for (int x = lane; x < n; x += 64) mt = fmaxf(mt, a.part_ml[r * a.splits + x].x);
-#pragma unroll
-    for (int x = 1; x < 64; x *= 2) mt = fmaxf(mt, __shfl_xor(mt, x));
-    float lt = 0.0f, f[D / 64] = {};
-    for (int x = 0; x < n; ++x) {
-        const float2 ml = a.part_ml[r * a.splits + x];
-        if (ml.y == 0.0f) continue;
-        const float c = exp2_(ml.x - mt);
-        lt += c * ml.y;
-        const float* from = a.part + (r * a.splits + x) * D + lane * (D / 64);
-#pragma unroll
-        for (int y = 0; y < D / 64; ++y) f[y] += c * from[y];
-    }
-    const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
-    XT* to = static_cast<XT*>(a.out.p) + token * a.out.ts + hq * a.out.hs + lane * (D / 64);
-#pragma unroll
-    for (int y = 0; y < D / 64; ++y) to[y] = static_cast<XT>(f[y] * inv);
-    if (a.lse && lane == 0) a.lse[r] = (mt + log2f(lt)) * kLn2;
-}
-
 template <int D, typename XT>
 hipError_t run(const Decode& a, hipStream_t s) {
     const uint32_t blocks = static_cast<uint32_t>(a.c.sequences * a.c.heads * a.row_tiles * a.splits);
@@ -536,9 +503,18 @@ hipError_t run(const Decode& a, hipStream_t s) {
         decode_kernel<raw, D, XT><<<blocks, kThreads, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
-    const int64_t rows = a.c.sequences * a.q_len * a.q_heads;
-    join_kernel<D, XT><<<static_cast<uint32_t>((rows + 3) / 4), kThreads, 0, s>>>(a, rows);
-    return hipGetLastError();
+    Join j{};
+    j.part = a.part;
+    j.part_ml = a.part_ml;
+    j.rows = a.c.sequences * a.q_len * a.q_heads;
+    j.splits = a.splits;
+    j.q_heads = a.q_heads;
+    j.out = a.out;
+    j.lse = a.lse;
+    j.lens = a.lens;
+    j.q_len = a.q_len;
+    j.chunk = a.chunk;
+    return launch_join<D, XT>(j, s);
 }
 
 }  // namespace

@@ -18,7 +18,7 @@
 #include <algorithm>
 #include <cfloat>
 
-#include "attn.hpp"
+#include "attn_join.hpp"
 
 namespace unisvq {
 namespace {
@@ -56,17 +56,21 @@ __device__ inline uint32_t load_offset(int n, int i, int64_t ts) {
 // Bring the tile at `p` (of `rows` rows, ts elements apart) to LDS.  What is
 // past the last row is past the buffer's end, and becomes zeros.
 template <int D, typename T>
-__device__ __forceinline__ void load_tile(const T* p, int64_t ts, int rows, const uint32_t (&off)[kKeys * D / 8 / kThreads],
-                                          T* lds, int wave) {
-    const __amdgpu_buffer_rsrc_t r = make_rsrc(p, static_cast<uint32_t>((rows - 1) * ts * 2 + D * 2));
-#pragma unroll
-    for (int n = 0; n < kKeys * D / 8 / kThreads; ++n) {
-        const uint32_t to = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(
-            (__attribute__((address_space(3))) void*)(lds + (n * kThreads + wave * 64) * 8))));
-        // (the compiler would wait for a load that it knows of before any read of LDS that might be of its place)
-        asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off[n]), "s"(r) : "memory");
+struct TileLoad {
+    __amdgpu_buffer_rsrc_t r;
+    uint32_t to;
+
+    __device__ __forceinline__ TileLoad(const T* p, int64_t ts, int rows, T* lds, int wave)
+        : r(make_rsrc(p, rows > 0 ? static_cast<uint32_t>((rows - 1) * ts * 2 + D * 2) : 0u)),
+          to(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(
+              reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)(lds + wave * 64 * 8))))) {}
+
+    // Its n-th load.  (The compiler would wait for a load that it knows of
+    // before any read of LDS that might be of its place.)
+    __device__ __forceinline__ void issue(int n, uint32_t off) const {
+        asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + n * kThreads * 16), "v"(off), "s"(r));
     }
-}
+};
 
 // Which of a lane's sums have met +inf or NaN, and which -inf or NaN (bit 16 d + r: o[d][r]).
 struct Spoiled {
@@ -179,7 +183,6 @@ struct Wave {
     typedef typename Vec8<T>::type T8;
     T8 q[D / 16];
     f32x16 o[D / 32];
-    f32x16 s[2];
     T8 p[4];
     float m, l, scale;
     int hf;
@@ -202,7 +205,7 @@ struct Wave {
     }
 
     // s = K Q^T for the tile at ks.
-    __device__ __forceinline__ void scores(const T* ks) {
+    __device__ __forceinline__ void scores(const T* ks, f32x16 (&s)[2]) const {
 #pragma unroll
         for (int n = 0; n < D / 16; ++n)
 #pragma unroll
@@ -213,7 +216,7 @@ struct Wave {
     }
 
     // Hides keys from `limit` on, in the tile from key k0.
-    __device__ __forceinline__ void mask(int k0, int limit) {
+    __device__ __forceinline__ void mask(f32x16 (&s)[2], int k0, int limit) const {
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -221,22 +224,25 @@ struct Wave {
                 if (32 * x + 8 * (r / 4) + r % 4 >= limit - k0 - 4 * hf) s[x][r] = -INFINITY;
     }
 
-    // The tile's weights from its scores.
-    __device__ __forceinline__ void weights() {
+    // Raises the maximum m where scores of the tile exceed it by 2^kSlack.
+    __device__ __forceinline__ void raise(const f32x16 (&s)[2]) {
         float top = s[0][0];
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, s[x][r]);
         top *= scale;
-        if (__any(top > m + kSlack)) {
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float m2 = fmaxf(m, top), c = exp2_(m - m2);
-            m = m2;
-            l *= c;
+        if (!__any(top > m + kSlack)) return;
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m2 = fmaxf(m, top), c = exp2_(m - m2);
+        m = m2;
+        l *= c;
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d) o[d] *= c;
-        }
+        for (int d = 0; d < D / 32; ++d) o[d] *= c;
+    }
+
+    // The tile's weights from its scores.
+    __device__ __forceinline__ void weights(const f32x16 (&s)[2]) {
         float sum[4] = {};
 #pragma unroll
         for (int x = 0; x < 2; ++x)
@@ -259,17 +265,14 @@ struct Prompt {
     float2* part_ml;  // and their maximum (log2) and sum
 };
 
-// STAGES: tiles of keys and of values in LDS.  Two let two workgroups share a
-// CU, whose waves then cover each other's waits; three, for grids of no more
-// workgroups than CUs, bring a tile two steps ahead.
-template <int D, typename T, int STAGES>
-__global__ __launch_bounds__(kThreads, STAGES == 2 ? 2 : 1) void prompt_kernel(Prompt g) {
+template <int D, typename T>
+__global__ __launch_bounds__(kThreads, 2) void prompt_kernel(Prompt g) {
     typedef typename Vec8<T>::type T8;
     const PromptArgs& a = g.a;
     constexpr int kQ = 32, kTile = kKeys * D, kChunks = D / 8;
     constexpr int kLoads = kTile * 2 / (16 * kThreads);  // loads a thread of a tile of keys or values
-    __shared__ __attribute__((aligned(16))) T sk[STAGES][kTile];
-    __shared__ __attribute__((aligned(16))) T sv[STAGES][kTile];
+    __shared__ __attribute__((aligned(16))) T sk[2][kTile];
+    __shared__ __attribute__((aligned(16))) T sv[2][kTile];
     __shared__ int64_t row_at[kTileQ];
     __shared__ int bad_tile;  // 1 + the last tile found to hold values that are not finite
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
@@ -281,12 +284,10 @@ __global__ __launch_bounds__(kThreads, STAGES == 2 ? 2 : 1) void prompt_kernel(P
     const int part = kv / a.kv_heads;
     kv %= a.kv_heads;
     if (a.kv_heads % 8 == 0) kv = kv % 8 * (a.kv_heads / 8) + kv / 8;
-    // Late tiles see most keys, so they go first.  Where all workgroups are
-    // resident at once, two a CU, those that come second on a CU go from the
-    // fewest keys up, to share it with the most.
-    const int rank = blockIdx.x / parts, count = gridDim.x / parts;
-    int tile = count - 1 - rank;
-    if (gridDim.x <= kResident && gridDim.x > kResident / 2 && rank >= (count + 1) / 2) tile = rank - (count + 1) / 2;
+    // Tiles go in the order of their work, most first: sequences with most
+    // keys first (of 64 at a time), and of a sequence the late tiles, which
+    // see most.
+    int tile = blockIdx.x / parts;
     // the sequence of the tile: its tiles are its queries times the group's heads, 128 a tile
     int first = 0, q_first = 0, nq = 0, k_first = 0, nk = 0;
     for (int base = 0;; base += 64) {
@@ -298,12 +299,23 @@ __global__ __launch_bounds__(kThreads, STAGES == 2 ? 2 : 1) void prompt_kernel(P
         }
         const int most_q = static_cast<int>(a.q_tokens), most_k = static_cast<int>(a.k_tokens);
         c0 = min(max(c0, 0), most_q), c1 = min(max(c1, c0), most_q), d0 = min(max(d0, 0), most_k), d1 = min(max(d1, d0), most_k);
+        if (a.sequences > 1) {
+            const int many = min(64, static_cast<int>(a.sequences) - base);
+            int before = 0;  // sequences that go before the lane's
+            for (int j = 0; j < many; ++j) {
+                const int other = __builtin_amdgcn_readlane(d1 - d0, j);
+                before += other > d1 - d0 || (other == d1 - d0 && j < lane);
+            }
+            if (lane >= many) before = lane;
+            c0 = __builtin_amdgcn_ds_permute(4 * before, c0), c1 = __builtin_amdgcn_ds_permute(4 * before, c1);
+            d0 = __builtin_amdgcn_ds_permute(4 * before, d0), d1 = __builtin_amdgcn_ds_permute(4 * before, d1);
+        }
         const int tiles = ((c1 - c0) * g.group + kTileQ - 1) / kTileQ;
         const int sum = scan64(tiles);
         const uint64_t in = __ballot(tile < first + sum);
         if (in) {
             const int l = __ffsll(static_cast<unsigned long long>(in)) - 1;
-            first += __builtin_amdgcn_readlane(sum - tiles, l);
+            tile = first + __builtin_amdgcn_readlane(sum, l) - 1 - tile;
             q_first = __builtin_amdgcn_readlane(c0, l);
             nq = __builtin_amdgcn_readlane(c1, l) - q_first;
             k_first = __builtin_amdgcn_readlane(d0, l);
@@ -313,7 +325,7 @@ __global__ __launch_bounds__(kThreads, STAGES == 2 ? 2 : 1) void prompt_kernel(P
         first += __builtin_amdgcn_readlane(sum, 63);
     }
     // rows are (query, head of the group)
-    const int rows = nq * g.group, row0 = (tile - first) * kTileQ, wave_row = row0 + wave * kQ;
+    const int rows = nq * g.group, row0 = tile * kTileQ, wave_row = row0 + wave * kQ;
     const int row = min(wave_row + i, rows - 1);
     const bool live = wave_row + i < rows;
     const int qi = row / g.group, head = kv * g.group + row - qi * g.group;
@@ -359,65 +371,69 @@ __global__ __launch_bounds__(kThreads, STAGES == 2 ? 2 : 1) void prompt_kernel(P
         off_k[n] = load_offset<D, false>(n, threadIdx.x, a.k.ts);
         off_v[n] = load_offset<D, true>(n, threadIdx.x, a.v.ts);
     }
-    // tiles are loaded in turn
+    // tiles are loaded in turn; past the end, zeros
     int left_k = nk - key0, left_v = left_k;  // rows from the next tile on
-    const auto load_k = [&](int slot) __attribute__((always_inline)) {
-        load_tile<D, T>(kp, a.k.ts, min(kKeys, left_k), off_k, sk[slot], wave);
+    const auto next_k = [&](int slot) __attribute__((always_inline)) {
+        const TileLoad<D, T> l(kp, a.k.ts, min(kKeys, left_k), sk[slot], wave);
         kp += kKeys * a.k.ts;
         left_k -= kKeys;
+        return l;
     };
-    const auto load_v = [&](int slot) __attribute__((always_inline)) {
-        load_tile<D, T>(vp, a.v.ts, min(kKeys, left_v), off_v, sv[slot], wave);
+    const auto next_v = [&](int slot) __attribute__((always_inline)) {
+        const TileLoad<D, T> l(vp, a.v.ts, min(kKeys, left_v), sv[slot], wave);
         vp += kKeys * a.v.ts;
         left_v -= kKeys;
+        return l;
     };
     Spoiled spoiled{0, 0};
     if (threadIdx.x == 0) bad_tile = 0;
 
-    // Tile t's weights; then its values and the next tile's scores in one go,
-    // with the loads of the tiles after them: one barrier a tile.
-    if (tiles > 0) {
-#pragma unroll
-        for (int n = 0; n < STAGES; ++n) {
-            if (n < tiles) load_k(n);
-            if (n < STAGES - 1 && n < tiles) load_v(n);
+    f32x16 s[2];
+    // Before the values of tile t: where rows see different keys, those that
+    // are not finite are taken out and marked.
+    const auto check_values = [&](int t, T* vs) __attribute__((always_inline)) {
+        if (!a.causal || t < plain) return;
+        if (any_not_finite<D, T>(vs, wave, lane)) bad_tile = t + 1;
+        local_phase();
+        if (bad_tile == t + 1) {
+            mark_not_finite<D, T>(vs, key0 + t * kKeys, limit, lane, spoiled);
+            local_phase();
+            drop_not_finite<D, T>(vs, wave, lane);
+            local_phase();
         }
+    };
+    const auto issue = [&](const TileLoad<D, T>& l, const uint32_t (&off)[kLoads]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) l.issue(n, off[n]);
+    };
+    // Tile t's weights; then its values and the next tile's scores in one run
+    // of products, with the loads of the tiles after them: one barrier a tile.
+    if (tiles > 0) {
+        issue(next_k(0), off_k);
+        issue(next_v(0), off_v);
+        issue(next_k(1), off_k);
         wait_loads<0>();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         // (the queries too: the compiler would go on waiting for them in the loop)
 #pragma unroll
         for (int n = 0; n < D / 16; ++n) asm volatile("" : "+v"(w.q[n]));
         phase();
-        w.scores(sk[0]);
-        int slot = 0;  // t % STAGES
+        w.scores(sk[0], s);
         for (int t = 0; t < tiles; ++t) {
-            if (t >= whole) w.mask(key0 + t * kKeys, limit);
-            w.weights();
-            // Keys t + 1 and values t have to be there; what was loaded after
-            // the last barrier may be on its way still.
-            if (STAGES == 2) wait_loads<0>();
-            else if (t + 2 < tiles) wait_loads<2 * kLoads>();
-            else if (t + 1 < tiles) wait_loads<kLoads>();
-            else wait_loads<0>();
-            phase();  // and keys t and values t - 1 are done with
-            if (t + STAGES < tiles) load_k(slot);
-            if (t + STAGES - 1 < tiles) load_v(slot == 0 ? STAGES - 1 : slot - 1);
-            T* const v_now = sv[slot];
-            if (a.causal && t >= plain) {  // rows see different keys
-                if (any_not_finite<D, T>(v_now, wave, lane)) bad_tile = t + 1;
-                local_phase();
-                if (bad_tile == t + 1) {
-                    mark_not_finite<D, T>(v_now, key0 + t * kKeys, limit, lane, spoiled);
-                    local_phase();
-                    drop_not_finite<D, T>(v_now, wave, lane);
-                    local_phase();
-                }
-            }
-            slot = slot + 1 == STAGES ? 0 : slot + 1;
-            w.values(v_now);
-            w.scores(sk[slot]);  // (after the last tile: of what was there before, and not used)
+            const int slot = t & 1;
+            if (t >= whole) w.mask(s, key0 + t * kKeys, limit);
+            w.raise(s);
+            w.weights(s);
+            wait_loads<0>();
+            phase();  // keys t + 1 and values t are there; keys t and values t - 1 are done with
+            issue(next_k(slot), off_k);
+            issue(next_v(slot ^ 1), off_v);
+            check_values(t, sv[slot]);
+            w.values(sv[slot]);
+            w.scores(sk[slot ^ 1], s);  // (after the last tile: zeros or what was there, and not used)
             schedule_products<D>();
         }
+        wait_loads<0>();  // none may come to LDS after this
     }
 
     if (__any((spoiled.up | spoiled.down) != 0)) {
@@ -469,48 +485,33 @@ __global__ __launch_bounds__(kThreads, STAGES == 2 ? 2 : 1) void prompt_kernel(P
     }
 }
 
-// Joins the parts of a row, in their order; one wave a row.
-template <int D, typename T>
-__global__ __launch_bounds__(kThreads) void prompt_join_kernel(Prompt g) {
-    const PromptArgs& a = g.a;
-    const int64_t r = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
-    const int64_t token = r / a.q_heads;
-    if (token >= min(a.q_tokens, static_cast<int64_t>(a.cu_q[a.sequences]))) return;
-    const int head = static_cast<int>(r - token * a.q_heads), lane = threadIdx.x & 63;
-    const float2* ml = g.part_ml + r * g.splits;
-    float m = -FLT_MAX, l = 0.0f, f[D / 64] = {};
-    for (int x = 0; x < g.splits; ++x) m = fmaxf(m, ml[x].x);
-    for (int x = 0; x < g.splits; ++x) {
-        if (ml[x].y == 0.0f) continue;
-        const float c = exp2_(ml[x].x - m);
-        l += c * ml[x].y;
-        const float* from = g.part + (r * g.splits + x) * D + lane * (D / 64);
-#pragma unroll
-        for (int y = 0; y < D / 64; ++y) f[y] += c * from[y];
-    }
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    T* to = static_cast<T*>(a.out.p) + token * a.out.ts + head * a.out.hs + lane * (D / 64);
-#pragma unroll
-    for (int y = 0; y < D / 64; ++y) to[y] = static_cast<T>(f[y] * inv);
-    if (a.lse && lane == 0) a.lse[r] = (m + log2f(l)) * kLn2;
-}
-
 // Workgroups without a split, at most (every sequence may end with a part of a tile).
 int64_t prompt_blocks(int64_t sequences, int64_t q_tokens, int q_heads, int kv_heads) {
     return (q_tokens * (q_heads / kv_heads) + (kTileQ - 1) * sequences) / kTileQ * kv_heads;
 }
 
-// Few rows before many keys: the keys are split so that there are about two
-// workgroups a CU, of at least four tiles each were all keys one sequence's.
-int prompt_splits(int64_t sequences, int64_t q_tokens, int64_t k_tokens, int q_heads, int kv_heads) {
-    const int64_t blocks = prompt_blocks(sequences, q_tokens, q_heads, kv_heads);
-    const int64_t n = std::min(kResident / std::max<int64_t>(1, blocks), k_tokens / (4 * kKeys));
-    return static_cast<int>(std::min<int64_t>(std::max<int64_t>(1, n), 32));
+// Few rows before many keys: the keys are split, so that there are up to two
+// workgroups a CU, if that is expected to take less time than it costs.  A tile
+// of keys takes a workgroup about 1.1 us, the launch that joins the parts 5 us
+// and what their sums (written and read) take at 3.5 TB/s.  Of a batch's
+// lengths only the mean is known here: its longest sequence is taken to have
+// twice that.
+int prompt_splits(int64_t sequences, int64_t q_tokens, int64_t k_tokens, int q_heads, int kv_heads, int head_dim) {
+    const int64_t blocks = std::max<int64_t>(1, prompt_blocks(sequences, q_tokens, q_heads, kv_heads));
+    const double tiles = static_cast<double>(std::min(k_tokens, 2 * k_tokens / sequences)) / kKeys;
+    const double sums = 8e-6 / 3.5 * static_cast<double>(q_tokens) * q_heads * head_dim;  // us a part
+    int best = 1;
+    double least = 1.1 * tiles;
+    for (int n = 2; n <= 32 && n * blocks <= kResident && n * 2 <= tiles; ++n) {
+        const double us = 1.1 * tiles / n + 5.0 + sums * n;
+        if (us < least) least = us, best = n;
+    }
+    return best;
 }
 
 template <int D, typename T>
 hipError_t run(const PromptArgs& a, void* workspace, hipStream_t s) {
-    Prompt g{a, a.scale * kLog2e, a.q_heads / a.kv_heads, prompt_splits(a.sequences, a.q_tokens, a.k_tokens, a.q_heads, a.kv_heads),
+    Prompt g{a, a.scale * kLog2e, a.q_heads / a.kv_heads, prompt_splits(a.sequences, a.q_tokens, a.k_tokens, a.q_heads, a.kv_heads, D),
              nullptr, nullptr};
     const int64_t rows = a.q_tokens * a.q_heads;
     if (g.splits > 1) {
@@ -518,21 +519,26 @@ hipError_t run(const PromptArgs& a, void* workspace, hipStream_t s) {
         g.part_ml = reinterpret_cast<float2*>(g.part + rows * g.splits * D);
     }
     const uint32_t blocks = static_cast<uint32_t>(prompt_blocks(a.sequences, a.q_tokens, a.q_heads, a.kv_heads) * g.splits);
-    if (blocks <= kResident / 2)
-        prompt_kernel<D, T, 3><<<blocks, kThreads, 0, s>>>(g);
-    else
-        prompt_kernel<D, T, 2><<<blocks, kThreads, 0, s>>>(g);
+    prompt_kernel<D, T><<<blocks, kThreads, 0, s>>>(g);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || g.splits == 1) return e;
-    prompt_join_kernel<D, T><<<static_cast<uint32_t>((rows + kWaves - 1) / kWaves), kThreads, 0, s>>>(g);
-    return hipGetLastError();
+    Join j{};
+    j.part = g.part;
+    j.part_ml = g.part_ml;
+    j.rows = rows;
+    j.splits = g.splits;
+    j.q_heads = a.q_heads;
+    j.out = a.out;
+    j.lse = a.lse;
+    j.tokens = a.cu_q + a.sequences;
+    return launch_join<D, T>(j, s);
 }
 
 }  // namespace
 
 size_t prompt_workspace_bytes(int64_t sequences, int64_t q_tokens, int64_t k_tokens, int q_heads, int kv_heads,
                               int head_dim) {
-    const int n = prompt_splits(sequences, q_tokens, k_tokens, q_heads, kv_heads);
+    const int n = prompt_splits(sequences, q_tokens, k_tokens, q_heads, kv_heads, head_dim);
     return n == 1 ? 0 : static_cast<size_t>(q_tokens * q_heads) * n * (head_dim + 2) * 4;
 }
 
