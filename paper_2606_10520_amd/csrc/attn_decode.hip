@@ -18,14 +18,28 @@
 //                 consecutive dims a lane; row i of dim tile e is dim (D/16) i + e,
 //                 and pairs of tokens are put together by byte permutes.
 // Query rows are the q_len tokens of the q_heads / kv_heads heads that share a
-// key head.  Codes become f16 integers exactly; the keys' scales multiply the
-// scores and the values' scales the softmax weights, both in fp32.
+// key head.
+//
+// Codes.  A byte u in the low bits of an f16 is the (subnormal) number u 2^-24,
+// a nibble in bits 6 to 9 u 2^-18, exactly, and the matrix cores multiply
+// subnormals too.  So codes become operands with a mask or a byte permute each,
+// without arithmetic: u = code + 128 (i8, the sign bit turned) or code + 8
+// (i4).  The bias is taken off sums, not elements: the scores start from -bias
+// sum(q), and the values' sums lose bias sum(p), which one more product with a
+// constant keeps.  (A sum's last bit is that of its largest product as if its
+// subnormal factor had all its bits: what is lost of 24 bits are the zeros
+// before u, two or three for bytes, one for nibbles; with nibbles in bits 0 to
+// 3, one operation a word less, seven were, and it showed in the results.)  The keys' scales multiply the scores and the
+// values' scales the weights, both in fp32; queries are scaled by a power of
+// two into f16's range.
 //
 // A workgroup's four waves take every fourth 32-token tile of the workgroup's
-// part of the sequence, each with its own running maximum m, sum and outputs,
-// joined through LDS; parts are joined by a second launch.  m is raised only
-// when a score exceeds it by 2^8 (the weights then stay below 2^8, well inside
-// f16), so most tiles need no exchange between lanes and no rescaling.
+// part of the sequence, the next tile's loads under way while one is computed,
+// each with its own running maximum m, sum and outputs, joined through LDS;
+// parts are joined by a second launch.  m is raised only when a score exceeds
+// it by 2^8 (the weights then stay below 2^8, well inside f16), so most tiles
+// need no exchange between lanes and no rescaling.
+#include <algorithm>
 #include <cfloat>
 
 #include "attn_join.hpp"
@@ -55,25 +69,11 @@ __device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amd
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 __device__ inline uint32_t perm(uint32_t hi, uint32_t lo, uint32_t sel) { return __builtin_amdgcn_perm(hi, lo, sel); }
-__device__ inline f16x2 as_f16x2(uint32_t v) { return __builtin_bit_cast(f16x2, v); }
-__device__ inline uint32_t as_u32(f16x2 v) { return __builtin_bit_cast(uint32_t, v); }
 
-// 1024 + u in both halves (u a byte or a nibble in the low bits) minus `bias`.
-__device__ inline uint32_t minus(uint32_t v, float bias) {
-    const _Float16 b = static_cast<_Float16>(-bias);
-    return as_u32(as_f16x2(v) + f16x2{b, b});
-}
-// 1024 + 16 u in both halves: u - 8.
-__device__ inline uint32_t minus8_of16(uint32_t v) {
-    const _Float16 r = static_cast<_Float16>(0.0625f), b = static_cast<_Float16>(-72.0f);
-    return as_u32(__builtin_elementwise_fma(as_f16x2(v), f16x2{r, r}, f16x2{b, b}));
-}
-
-// Eight nibbles + 8 of w as f16 integers in the order 0 4 1 5 2 6 3 7.
+// Nibbles of w in the order 0 4 1 5 2 6 3 7, as u 2^-18.
 __device__ inline u32x4 nibbles(uint32_t w) {
-    const uint32_t x = w >> 8;
-    return u32x4{minus((w & 0x000f000fu) | 0x64006400u, 1032.0f), minus8_of16((w & 0x00f000f0u) | 0x64006400u),
-                 minus((x & 0x000f000fu) | 0x64006400u, 1032.0f), minus8_of16((x & 0x00f000f0u) | 0x64006400u)};
+    const uint32_t m = 0x03c003c0u;
+    return u32x4{w << 6 & m, w << 2 & m, w >> 2 & m, w >> 6 & m};
 }
 
 // What a lane reads of 16 tokens' keys (K) and of one token's values (V).
@@ -87,6 +87,8 @@ struct Geometry {
     static constexpr int kloads = row / (4 * kword);
     static constexpr bool scaled = bits < 16;
     static constexpr int halves = bits == 4 ? 2 : 1;  // scales of a head
+    static constexpr uint32_t bias = bits == 4 ? 8 << 6 : 128;  // as an operand's bits
+    static constexpr float unit = bits == 4 ? 0x1p18f : 0x1p24f;  // what operands are to be times for their codes
 };
 
 template <int BYTES>
@@ -101,22 +103,31 @@ struct TileRegs {
     typedef Geometry<KIND, D> G;
     typename Word<G::kword>::type k[2][G::kloads];
     typename Word<G::vbytes>::type v[2][4];
-    f32x4 ks[2], vs[2];  // the scale words of tokens 4g .. 4g + 3
+    u32x4 ks[2], vs[2];  // the scale words of tokens 4g .. 4g + 3
     bool there[2];       // whether the 16 tokens have a page (the same in all lanes)
 };
 
 template <typename T>
 __device__ inline T load_stream(const uint8_t* p) { return __builtin_nontemporal_load(reinterpret_cast<const T*>(p)); }
 
+// The pages of the 16 tokens from p and from p + 16 on, -1 where there is none.
+struct Pages {
+    int at[2];
+};
+__device__ inline Pages look_up(const Decode& a, const int32_t* row, int p, int len) {
+    Pages r;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) r.at[t] = p + 16 * t < len ? row[(p + 16 * t) >> a.c.page_shift] : -1;
+    return r;
+}
+
 template <int KIND, int D>
-__device__ inline void load_tile(const Decode& a, int64_t table_row, int h, int pos, int len, int i, int g,
-                                 TileRegs<KIND, D>& r) {
+__device__ __forceinline__ void load_tile(const Decode& a, const Pages& pages, int h, int pos, int i, int g, TileRegs<KIND, D>& r) {
     typedef Geometry<KIND, D> G;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         const int p = pos + 16 * t;
-        int64_t page = -1;
-        if (p < len) page = a.c.table[table_row + (p >> a.c.page_shift)];
+        int64_t page = pages.at[t];
         r.there[t] = page >= 0 && page < a.c.pages;
         if (!r.there[t]) page = 0;
         const int64_t e = ((page * a.c.heads + h) << a.c.page_shift) + (p & ((1 << a.c.page_shift) - 1));
@@ -125,13 +136,11 @@ __device__ inline void load_tile(const Decode& a, int64_t table_row, int h, int 
 #pragma unroll
         for (int n = 0; n < G::kloads; ++n)
             r.k[t][n] = load_stream<typename Word<G::kword>::type>(kp + (i * G::row + n * 4 * G::kword + g * G::kword));
+        if constexpr (G::scaled) r.ks[t] = *reinterpret_cast<const u32x4*>(a.c.ks + e + 4 * g);
 #pragma unroll
         for (int n = 0; n < 4; ++n)
             r.v[t][n] = load_stream<typename Word<G::vbytes>::type>(vp + ((4 * g + n) * G::row + i * G::vbytes));
-        if constexpr (G::scaled) {
-            r.ks[t] = *reinterpret_cast<const f32x4*>(a.c.ks + e + 4 * g);
-            r.vs[t] = *reinterpret_cast<const f32x4*>(a.c.vs + e + 4 * g);
-        }
+        if constexpr (G::scaled) r.vs[t] = *reinterpret_cast<const u32x4*>(a.c.vs + e + 4 * g);
     }
 }
 
@@ -144,19 +153,18 @@ __device__ inline int query_dim(int n, int g) {
     return 32 * n + 8 * g;
 }
 
-// Scores of 16 tokens (unscaled; one sum for each half of the head where the
-// scales differ).
+// Scores of 16 tokens (without scales; one sum for each half of the head where
+// the scales differ), from `start`.
 template <int KIND, int D, typename C8>
-__device__ inline void scores16(const TileRegs<KIND, D>& r, int t, const C8 (&q)[D / 32], f32x4 (&s)[Geometry<KIND, D>::halves]) {
+__device__ __forceinline__ void scores16(const TileRegs<KIND, D>& r, int t, const C8 (&q)[D / 32],
+                                         const float (&start)[Geometry<KIND, D>::halves], f32x4 (&s)[Geometry<KIND, D>::halves]) {
 #pragma unroll
-    for (int h = 0; h < Geometry<KIND, D>::halves; ++h) s[h] = f32x4{0, 0, 0, 0};
+    for (int h = 0; h < Geometry<KIND, D>::halves; ++h) s[h] = f32x4{start[h], start[h], start[h], start[h]};
     if constexpr (KIND == UNISVQ_CACHE_I8) {
 #pragma unroll
         for (int n = 0; n < D / 32; ++n) {
             const uint32_t w0 = r.k[t][n / 2][2 * (n % 2)] ^ 0x80808080u, w1 = r.k[t][n / 2][2 * (n % 2) + 1] ^ 0x80808080u;
-            const uint32_t magic = 0x64646464u;
-            const u32x4 a = {minus(perm(magic, w0, 0x04010400u), 1152.0f), minus(perm(magic, w0, 0x04030402u), 1152.0f),
-                             minus(perm(magic, w1, 0x04010400u), 1152.0f), minus(perm(magic, w1, 0x04030402u), 1152.0f)};
+            const u32x4 a = {perm(0, w0, 0x0c010c00u), perm(0, w0, 0x0c030c02u), perm(0, w1, 0x0c010c00u), perm(0, w1, 0x0c030c02u)};
             s[0] = mfma(__builtin_bit_cast(C8, a), q[n], s[0]);
         }
     } else if constexpr (KIND == UNISVQ_CACHE_I4) {
@@ -183,7 +191,7 @@ __device__ inline uint32_t vword(const TileRegs<KIND, D>& r, int t, int n, int w
 
 // The A operand of dim tile e: dim (D/16) i + e of the lane's eight tokens.
 template <int KIND, int D, typename C8>
-__device__ inline void value_operands(const TileRegs<KIND, D>& r, C8 (&v)[D / 16]) {
+__device__ __forceinline__ void value_operands(const TileRegs<KIND, D>& r, C8 (&v)[D / 16]) {
     constexpr int E = D / 16;
     uint32_t w[E][4];  // [dim][token pair]
 #pragma unroll
@@ -195,10 +203,10 @@ __device__ inline void value_operands(const TileRegs<KIND, D>& r, C8 (&v)[D / 16
 #pragma unroll
                 for (int x = 0; x < E / 4; ++x) {
                     const uint32_t a = vword<KIND, D>(r, t, n, x) ^ 0x80808080u, b = vword<KIND, D>(r, t, n + 1, x) ^ 0x80808080u;
-                    w[4 * x + 0][pair] = minus(perm(b, a, 0x0c040c00u) | 0x64006400u, 1152.0f);
-                    w[4 * x + 1][pair] = minus(perm(b, a, 0x0c050c01u) | 0x64006400u, 1152.0f);
-                    w[4 * x + 2][pair] = minus(perm(b, a, 0x0c060c02u) | 0x64006400u, 1152.0f);
-                    w[4 * x + 3][pair] = minus(perm(b, a, 0x0c070c03u) | 0x64006400u, 1152.0f);
+                    w[4 * x + 0][pair] = perm(b, a, 0x0c040c00u);
+                    w[4 * x + 1][pair] = perm(b, a, 0x0c050c01u);
+                    w[4 * x + 2][pair] = perm(b, a, 0x0c060c02u);
+                    w[4 * x + 3][pair] = perm(b, a, 0x0c070c03u);
                 }
             } else if constexpr (KIND == UNISVQ_CACHE_I4) {
                 const uint32_t a = vword<KIND, D>(r, t, n, 0), b = vword<KIND, D>(r, t, n + 1, 0);
@@ -257,19 +265,153 @@ __device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // The scale of a token in half h of the head.
 template <int KIND>
-__device__ inline float scale_of(float word, int h) {
-    if constexpr (KIND == UNISVQ_CACHE_I4) {
-        const uint32_t w = __float_as_uint(word);
-        return __uint_as_float(h ? w & 0xffff0000u : w << 16);
-    }
+__device__ inline float scale_of(uint32_t word, int h) {
+    if constexpr (KIND == UNISVQ_CACHE_I4) return __uint_as_float(h ? word & 0xffff0000u : word << 16);
+    return __uint_as_float(word);
+}
+
+// The larger of two scale words (of both halves of them), and the largest of a
+// word as bits of fp32.  Scales are not negative, so they are ordered as their
+// bits are, with NaN above all.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+template <int KIND>
+__device__ inline uint32_t larger(uint32_t a, uint32_t b) {
+    if constexpr (KIND == UNISVQ_CACHE_I4)
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+    return max(a, b);
+}
+template <int KIND>
+__device__ inline uint32_t largest_bits(uint32_t word) {
+    if constexpr (KIND == UNISVQ_CACHE_I4) return max(word << 16, word & 0xffff0000u);
     return word;
 }
 
+// One wave's running result: weights are 2^(s - m + unit_log), sums l of them
+// and o of their products with the values' codes.
+template <int KIND, int D, typename CT>
+struct Running {
+    typedef typename Vec8<CT>::type C8;
+    static constexpr int E = D / 16, HV = Geometry<KIND, D>::halves;
+    C8 q[D / 32];
+    float start[HV];       // of the scores
+    float qscale;          // of the scores to log2 units
+    float m, l;
+    float unit_log;        // log2 of the unit that the values' scales are taken in
+    uint32_t most_bits;    // the largest scale that this unit takes (fp32 bits)
+    f32x4 o[HV][E], b[HV];  // b: sums of the weights times the bias
+    int limit;             // tokens below it are seen by the lane's row
+};
+
+template <int KIND, int D, typename CT>
+__device__ __forceinline__ void attend(const Decode& a, TileRegs<KIND, D>& r, int pos, int len, int g, Running<KIND, D, CT>& w) {
+    typedef Geometry<KIND, D> G;
+    typedef typename Vec8<CT>::type C8;
+    constexpr int E = G::E, HV = G::halves;
+    float s[2][4];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        f32x4 acc[HV];
+        scores16<KIND, D>(r, t, w.q, w.start, acc);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            if constexpr (KIND == UNISVQ_CACHE_I4)
+                s[t][n] = acc[0][n] * scale_of<KIND>(r.ks[t][n], 0) + acc[HV - 1][n] * scale_of<KIND>(r.ks[t][n], 1);
+            else if constexpr (KIND == UNISVQ_CACHE_I8)
+                s[t][n] = acc[0][n] * scale_of<KIND>(r.ks[t][n], 0);
+            else
+                s[t][n] = acc[0][n];
+        }
+    }
+    // whether all 32 tokens are seen by all rows
+    const bool full = pos + kTile <= len - a.q_len + 1 && r.there[0] && r.there[1];
+    if (!full) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const int p = pos + 16 * t + 4 * g + n;
+                if (!(p < w.limit && r.there[t])) s[t][n] = -INFINITY;
+                // what no row sees may hold anything
+                if (!(p < len && r.there[t])) {
+                    if constexpr (G::scaled) r.vs[t][n] = 0;
+                    else r.v[t][n] = {};
+                }
+            }
+    }
+    float top = s[0][0];
+    uint32_t vtop = 0;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            top = fmaxf(top, s[t][n]);
+            if constexpr (G::scaled) vtop = larger<KIND>(vtop, r.vs[t][n]);
+        }
+    top *= w.qscale;
+    if constexpr (G::scaled) vtop = largest_bits<KIND>(vtop);
+    if (__any(top > w.m + kSlack || (G::scaled && vtop > w.most_bits))) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m2 = fmaxf(w.m, top);
+        float c = exp2_(w.m - m2);
+        w.m = m2;
+        if constexpr (G::scaled) {
+            vtop = max(vtop, static_cast<uint32_t>(__shfl_xor(static_cast<int>(vtop), 16)));
+            vtop = max(vtop, static_cast<uint32_t>(__shfl_xor(static_cast<int>(vtop), 32)));
+            if (vtop > w.most_bits && vtop < 0x7f800000u) {
+                // the unit: the power of two below the largest scale; scales of up to 2^7 of it are taken
+                const int exponent = max(1, static_cast<int>(vtop >> 23));
+                const float unit = static_cast<float>(127 - exponent);
+                c *= exp2_(unit - w.unit_log);
+                w.unit_log = unit;
+                w.most_bits = static_cast<uint32_t>(min(exponent + 7, 254)) << 23;
+            }
+        }
+        w.l *= c;
+#pragma unroll
+        for (int x = 0; x < HV; ++x) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) w.o[x][e] *= c;
+            if constexpr (G::scaled) w.b[x] *= c;
+        }
+    }
+    C8 p[HV];
+    const float m = w.m - w.unit_log;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            const float v = exp2_(__builtin_fmaf(s[t][n], w.qscale, -m));
+            w.l += v;
+#pragma unroll
+            for (int x = 0; x < HV; ++x)
+                // (a weight of zero stays one where the scale is NaN, for rows that do not see the token)
+                p[x][4 * t + n] = static_cast<CT>(!G::scaled ? v
+                                                  : full || s[t][n] > -INFINITY || s[t][n] != s[t][n]
+                                                      ? v * scale_of<KIND>(r.vs[t][n], x)
+                                                      : 0.0f);
+        }
+    if constexpr (!G::scaled) {  // codes are finite, and a scale that is not is the weight's matter
+        if (!full && a.q_len > 1) only_where_seen<KIND, D, CT>(r, pos, w.limit, g, w.o[0]);
+    }
+    C8 v[E];
+    value_operands<KIND, D>(r, v);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+        for (int x = 0; x < HV; ++x) w.o[x][e] = mfma(v[e], p[x], w.o[x][e]);
+    if constexpr (G::scaled) {
+        constexpr uint32_t bias = G::bias | G::bias << 16;
+        const C8 ones = __builtin_bit_cast(C8, u32x4{bias, bias, bias, bias});
+#pragma unroll
+        for (int x = 0; x < HV; ++x) w.b[x] = mfma(ones, p[x], w.b[x]);
+    }
+}
+
 template <int KIND, int D, typename XT>
-__global__ __launch_bounds__(kThreads) void decode_kernel(Decode a) {
+__global__ __launch_bounds__(kThreads, 2) void decode_kernel(Decode a) {
     typedef Geometry<KIND, D> G;
     typedef std::conditional_t<G::scaled, _Float16, XT> CT;
-    typedef typename Vec8<CT>::type C8;
     constexpr int E = G::E, HV = G::halves, kPad = 4;
     const int split = blockIdx.x % a.splits;
     const int hr = blockIdx.x / a.splits % (a.c.heads * a.row_tiles);
@@ -284,15 +426,26 @@ __global__ __launch_bounds__(kThreads) void decode_kernel(Decode a) {
     const int end = split == a.splits - 1 ? len : min(len, begin + a.chunk);  // past max_len the last goes on
     if (split > 0 && begin >= len) return;  // the joining launch goes by the length too
 
+    // the first tiles are on their way while the queries are made ready
+    const int32_t* row_pages = a.c.table + static_cast<int64_t>(b) * a.c.width;
+    constexpr int kStep = kWaves * kTile;
+    TileRegs<KIND, D> r0, r1;
+    int pos = begin + wave * kTile;
+    Pages pages = look_up(a, row_pages, pos, end);
+    if (pos < end) load_tile<KIND, D>(a, pages, h, pos, i, g, r0);
+    pages = look_up(a, row_pages, pos + kStep, end);
+
     // the lane's query row: token j, head hq of the group
     const int rows = a.q_len * a.group;
     const int row = row0 + i;
     const bool live = row < rows;
     const int j = live ? row / a.group : 0, hq = h * a.group + (live ? row % a.group : 0);
     const int64_t token = static_cast<int64_t>(b) * a.q_len + j;
-    const int limit = live ? len - a.q_len + 1 + j : 0;
-    C8 q[D / 32];
-    float qscale = a.scale;
+    Running<KIND, D, CT> w;
+    w.limit = live ? len - a.q_len + 1 + j : 0;
+    w.qscale = a.scale;
+#pragma unroll
+    for (int x = 0; x < HV; ++x) w.start[x] = 0.0f;
     {
         const XT* x = static_cast<const XT*>(a.q.p) + token * a.q.ts + hq * a.q.hs;
         typename Vec8<XT>::type raw[D / 32];
@@ -302,163 +455,82 @@ __global__ __launch_bounds__(kThreads) void decode_kernel(Decode a) {
             if (!live)
 #pragma unroll
                 for (int y = 0; y < 8; ++y) raw[n][y] = static_cast<XT>(0.0f);
-            if constexpr (KIND == UNISVQ_CACHE_I4) {
-                const auto v = raw[n];
-#pragma unroll
-                for (int y = 0; y < 4; ++y) raw[n][2 * y] = v[y], raw[n][2 * y + 1] = v[4 + y];
-            }
         }
-        if constexpr (std::is_same_v<CT, XT>) {
+        if constexpr (!G::scaled) {
 #pragma unroll
-            for (int n = 0; n < D / 32; ++n) q[n] = raw[n];
+            for (int n = 0; n < D / 32; ++n) w.q[n] = raw[n];
         } else {
-            // bf16 queries as f16: times a power of two that brings the row's largest into [2^14, 2^15)
-            uint32_t m = 0;
+            // times a power of two that brings the row's largest into [2^14,
+            // 2^15): exact for what is within 2^28 of it
+            uint32_t most = 0;
 #pragma unroll
             for (int n = 0; n < D / 32; ++n)
 #pragma unroll
-                for (int y = 0; y < 8; ++y) m = max(m, __float_as_uint(static_cast<float>(raw[n][y])) & 0x7fffffffu);
-            m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16)));
-            m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 32)));
-            const int exponent = static_cast<int>(m >> 23) - 127;
-            const int up = m == 0 || exponent == 128 ? 0 : 14 - exponent;
+                for (int y = 0; y < 8; ++y) most = max(most, __float_as_uint(static_cast<float>(raw[n][y])) & 0x7fffffffu);
+            most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 16)));
+            most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 32)));
+            const int exponent = static_cast<int>(most >> 23) - 127;
+            const int up = most == 0 || exponent == 128 ? 0 : 14 - exponent;
+            constexpr bool nibble = KIND == UNISVQ_CACHE_I4;
 #pragma unroll
             for (int n = 0; n < D / 32; ++n)
 #pragma unroll
-                for (int y = 0; y < 8; ++y) q[n][y] = static_cast<CT>(ldexpf(static_cast<float>(raw[n][y]), up));
-            qscale = ldexpf(qscale, -up);
+                for (int y = 0; y < 8; ++y) {
+                    const float v = ldexpf(static_cast<float>(raw[n][nibble ? y / 2 + y % 2 * 4 : y]), up);
+                    w.start[n / (D / 32 / HV)] += v;
+                    w.q[n][y] = static_cast<CT>(v);
+                }
+#pragma unroll
+            for (int n = 0; n < HV; ++n) {
+                w.start[n] += __shfl_xor(w.start[n], 16);
+                w.start[n] += __shfl_xor(w.start[n], 32);
+                w.start[n] *= -static_cast<float>(G::bias) * 0x1p-24f;
+            }
+            w.qscale = ldexpf(w.qscale, -up) * G::unit;
         }
     }
+    w.m = -FLT_MAX;
+    w.l = 0.0f;
+    w.unit_log = 0.0f;
+    w.most_bits = 0;
+#pragma unroll
+    for (int x = 0; x < HV; ++x) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) w.o[x][e] = f32x4{0, 0, 0, 0};
+        w.b[x] = f32x4{0, 0, 0, 0};
+    }
 
-    float m = -FLT_MAX, l = 0.0f;
-    float vunit = 1.0f;  // power of two that the values' scales are taken in (scaled kinds)
-    f32x4 o[HV][E];
-#pragma unroll
-    for (int x = 0; x < HV; ++x)
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[x][e] = f32x4{0, 0, 0, 0};
-
-    const int64_t table_row = static_cast<int64_t>(b) * a.c.width;
-    TileRegs<KIND, D> r;
-    int pos = begin + wave * kTile;
-    bool first = true;
-    for (; pos < end; pos += kWaves * kTile) {
-        load_tile<KIND, D>(a, table_row, h, pos, len, i, g, r);
-        // scores, log2 units
-        float s[2][4];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            f32x4 acc[HV];
-            scores16<KIND, D>(r, t, q, acc);
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                float v;
-                if constexpr (KIND == UNISVQ_CACHE_I4)
-                    v = acc[0][n] * scale_of<KIND>(r.ks[t][n], 0) + acc[HV - 1][n] * scale_of<KIND>(r.ks[t][n], 1);
-                else if constexpr (KIND == UNISVQ_CACHE_I8)
-                    v = acc[0][n] * r.ks[t][n];
-                else
-                    v = acc[0][n];
-                s[t][n] = v * qscale;
-            }
-        }
-        // whether all 32 tokens are seen by all rows
-        const bool full = pos + kTile <= len - a.q_len + 1 && r.there[0] && r.there[1];
-        if (!full) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    const int p = pos + 16 * t + 4 * g + n;
-                    if (!(p < limit && r.there[t])) s[t][n] = -INFINITY;
-                    // what no row sees may hold anything
-                    if (!(p < len && r.there[t])) {
-                        if constexpr (G::scaled) r.vs[t][n] = 0.0f;
-                        else r.v[t][n] = {};
-                    }
-                }
-        }
-        float top = s[0][0];
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int n = 0; n < 4; ++n) top = fmaxf(top, s[t][n]);
-        bool raise = top > m + kSlack;
-        float vtop = 0.0f;
-        if constexpr (G::scaled) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int n = 0; n < 4; ++n)
-#pragma unroll
-                    for (int x = 0; x < HV; ++x) vtop = fmaxf(vtop, scale_of<KIND>(r.vs[t][n], x));
-            raise |= first || vtop * vunit > 128.0f;
-        }
-        if (__any(raise)) {
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float m2 = fmaxf(m, top);
-            float c = exp2_(m - m2);
-            l *= c;
-            m = m2;
-            if constexpr (G::scaled) {
-                vtop = fmaxf(vtop, __shfl_xor(vtop, 16));
-                vtop = fmaxf(vtop, __shfl_xor(vtop, 32));
-                if (vtop > 0.0f && vtop < INFINITY && (first || vtop * vunit > 128.0f)) {
-                    // 2^-exponent of the largest scale
-                    const float unit = ldexpf(1.0f, 127 - static_cast<int>(__float_as_uint(vtop) >> 23));
-                    if (!first) c *= unit / vunit;
-                    vunit = unit;
-                    first = false;
-                }
-            }
-#pragma unroll
-            for (int x = 0; x < HV; ++x)
-#pragma unroll
-                for (int e = 0; e < E; ++e) o[x][e] *= c;
-        }
-        C8 p[HV];
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const float w = exp2_(s[t][n] - m);
-                l += w;
-#pragma unroll
-                for (int x = 0; x < HV; ++x)
-                    // (a weight of zero stays one where the scale is NaN, for rows that do not see the token)
-                    p[x][4 * t + n] = static_cast<CT>(!G::scaled ? w
-                                                      : full || s[t][n] > -INFINITY || s[t][n] != s[t][n]
-                                                          ? w * (scale_of<KIND>(r.vs[t][n], x) * vunit)
-                                                          : 0.0f);
-            }
-        if constexpr (!G::scaled) {  // codes are finite, and a scale that is not is the weight's matter
-            if (!full && a.q_len > 1) only_where_seen<KIND, D, CT>(r, pos, limit, g, o[0]);
-        }
-        C8 v[E];
-        value_operands<KIND, D>(r, v);
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-#pragma unroll
-            for (int x = 0; x < HV; ++x) o[x][e] = mfma(v[e], p[x], o[x][e]);
+    while (pos < end) {
+        if (pos + kStep < end) load_tile<KIND, D>(a, pages, h, pos + kStep, i, g, r1);
+        pages = look_up(a, row_pages, pos + 2 * kStep, end);
+        attend<KIND, D, CT>(a, r0, pos, len, g, w);
+        pos += kStep;
+        if (pos >= end) break;
+        if (pos + kStep < end) load_tile<KIND, D>(a, pages, h, pos + kStep, i, g, r0);
+        pages = look_up(a, row_pages, pos + 2 * kStep, end);
+        attend<KIND, D, CT>(a, r1, pos, len, g, w);
+        pos += kStep;
     }
 
     // join the waves: dim E (4g + n) + e of query i
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
+    w.l += __shfl_xor(w.l, 16);
+    w.l += __shfl_xor(w.l, 32);
     __shared__ float so[kWaves][kRows][D + kPad];
     __shared__ float sm[kWaves][kRows], sl[kWaves][kRows];
     if (live) {
-        const float back = G::scaled ? 1.0f / vunit : 1.0f;
+        const float unit = G::scaled ? exp2_(-w.unit_log) : 1.0f;  // of the weights
 #pragma unroll
         for (int n = 0; n < 4; ++n)
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                float v = o[0][e][n];
-                if constexpr (HV == 2) v = g < 2 ? v : o[HV - 1][e][n];
-                so[wave][i][E * (4 * g + n) + e] = v * back;
+                float v = HV == 2 && g >= 2 ? w.o[HV - 1][e][n] : w.o[0][e][n];
+                if constexpr (G::scaled) {
+                    const float bias = HV == 2 && g >= 2 ? w.b[HV - 1][n] : w.b[0][n];
+                    v = (v - bias) * G::unit * unit;
+                }
+                so[wave][i][E * (4 * g + n) + e] = v;
             }
-        if (g == 0) sm[wave][i] = m, sl[wave][i] = l;
+        if (g == 0) sm[wave][i] = w.m, sl[wave][i] = w.l * unit;
     }
     __syncthreads();
     const int y = threadIdx.x / (D / 8), d = threadIdx.x % (D / 8) * 8;
@@ -519,13 +591,16 @@ hipError_t run(const Decode& a, hipStream_t s) {
 
 }  // namespace
 
-// Splits: about 1024 workgroups (four a CU), of at least one tile a wave.
+// Splits: about 2048 workgroups of at least two tiles a wave if all sequences
+// were the longest (a ragged batch has its work in few of them), else about 512
+// of at least one.
 int decode_splits(int64_t sequences, int q_len, int q_heads, int kv_heads, int64_t max_len) {
     const int64_t base = sequences * kv_heads * ((q_len * (q_heads / kv_heads) + kRows - 1) / kRows);
-    const int64_t most = (max_len + kWaves * kTile - 1) / (kWaves * kTile);
-    int64_t n = 1024 / base;
-    n = n > most ? most : n;
-    return static_cast<int>(n < 1 ? 1 : n > 128 ? 128 : n);
+    const auto parts = [&](int64_t tokens) { return (max_len + tokens - 1) / tokens; };
+    constexpr int64_t step = kWaves * kTile;
+    int64_t n = std::min(2048 / base, parts(2 * step));
+    if (base * n < 512) n = std::min(std::max<int64_t>(1, 512 / base), parts(step));
+    return static_cast<int>(std::min<int64_t>(std::max<int64_t>(1, n), 256));
 }
 
 size_t decode_workspace_bytes(int64_t sequences, int q_len, int q_heads, int head_dim, int splits) {
