@@ -48,11 +48,11 @@ hipError_t launch_cache_append(const CacheView& c, int64_t tokens, const int32_t
 hipError_t launch_cache_read(const CacheView& c, const int32_t* starts, const int32_t* cu, int64_t tokens, Rows k,
                              Rows v, int dtype, hipStream_t s);
 
-// Attention over the cache.  splits: workgroups along a sequence.
-int decode_splits(int64_t sequences, int q_len, int q_heads, int kv_heads, int64_t max_len);
-size_t decode_workspace_bytes(int64_t sequences, int q_len, int q_heads, int head_dim, int splits);
-hipError_t launch_attn_decode(const CacheView& c, const int32_t* lens, int64_t max_len, int splits, int q_len, int q_heads, Rows q,
-                              int x_dtype, float scale, Rows out, float* lse, void* workspace, hipStream_t s);
+// Attention over the cache.  slots: parts that a row's work can be split into.
+int decode_slots(int64_t sequences, int q_len, int q_heads, int kv_heads, int64_t max_len);
+size_t decode_workspace_bytes(int64_t sequences, int q_len, int q_heads, int head_dim, int slots);
+hipError_t launch_attn_decode(const CacheView& c, const int32_t* lens, int64_t max_len, int slots, int q_len, int q_heads,
+                              Rows q, int x_dtype, float scale, Rows out, float* lse, void* workspace, hipStream_t s);
 
 struct PromptArgs {
     const int32_t *cu_q, *cu_k;
@@ -171,6 +171,27 @@ __device__ inline uint32_t finite_only(uint32_t w) {
     if ((w >> 16 & e) == e) w &= 0xffffu;
     return w;
 }
+
+// A word that no kernel running now writes, from an address that is the same in
+// all lanes: by a scalar load, also where the compiler cannot see that the
+// kernel's own stores leave it alone.
+__device__ inline int32_t load_uniform(const int32_t* p) {
+    return *(const __attribute__((address_space(4))) int32_t*)reinterpret_cast<uintptr_t>(p);
+}
+
+// Sum, or the largest (of what is not negative), over the lanes up to this one.
+template <typename F>
+__device__ inline int scan64(int x, F op) {
+    x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));  // row_shr
+    x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+    x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+    x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+    x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));  // row_bcast
+    x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
+    return x;
+}
+__device__ inline int scan64(int x) { return scan64(x, [](int a, int b) { return a + b; }); }
+__device__ inline int scan64_max(int x) { return scan64(x, [](int a, int b) { return max(a, b); }); }
 
 // The sequence that packed row r belongs to: the last b with cu[b] <= r, found
 // by a whole wave together (64 entries a step; r is the same in all lanes).

@@ -157,10 +157,10 @@ bool decode_shape_ok(int64_t sequences, int64_t q_len, int64_t q_heads, int64_t 
 size_t unisvq_attn_decode_workspace_bytes(int64_t sequences, int64_t q_len, int64_t q_heads, int64_t kv_heads,
                                           int64_t head_dim, int64_t max_len) {
     if (!decode_shape_ok(sequences, q_len, q_heads, kv_heads, head_dim, max_len) || sequences == 0) return 0;
-    const int splits = unisvq::decode_splits(sequences, static_cast<int>(q_len), static_cast<int>(q_heads),
+    const int slots = unisvq::decode_slots(sequences, static_cast<int>(q_len), static_cast<int>(q_heads),
                                              static_cast<int>(kv_heads), max_len);
     return unisvq::decode_workspace_bytes(sequences, static_cast<int>(q_len), static_cast<int>(q_heads),
-                                          static_cast<int>(head_dim), splits);
+                                          static_cast<int>(head_dim), slots);
 }
 
 int unisvq_attn_decode(const unisvq_cache* cache, const int32_t* page_table, int64_t sequences, int64_t table_width,
@@ -182,18 +182,20 @@ int unisvq_attn_decode(const unisvq_cache* cache, const int32_t* page_table, int
     if (!rows_aligned(q, q_token_stride, q_head_stride) || !rows_aligned(out, out_token_stride, out_head_stride) ||
         !aligned(lens, 4) || !aligned(lse, 4))
         return UNISVQ_EALIGN;
-    const int splits = unisvq::decode_splits(sequences, static_cast<int>(q_len), static_cast<int>(q_heads), c.heads,
+    const int slots = unisvq::decode_slots(sequences, static_cast<int>(q_len), static_cast<int>(q_heads), c.heads,
                                              max_len);
-    // one workgroup for each key head, sixteen rows and split
+    // workgroups and units of work are counted in 32 bits
     const int64_t row_tiles = (q_len * (q_heads / c.heads) + 15) / 16;
-    if (sequences > kMost / (c.heads * row_tiles * splits)) return UNISVQ_EUNSUP;
+    if (c.heads * row_tiles > kMost / 2 / (room / 128 + 1) ||
+        sequences > kMost / 2 / (c.heads * row_tiles * (room / 128 + 1)))
+        return UNISVQ_EUNSUP;
     const size_t need = unisvq::decode_workspace_bytes(sequences, static_cast<int>(q_len), static_cast<int>(q_heads),
-                                                       c.head_dim, splits);
+                                                       c.head_dim, slots);
     if (need) {
         if (!workspace || workspace_bytes < need) return UNISVQ_EWORKSPACE;
         if (!aligned(workspace, 16)) return UNISVQ_EALIGN;
     }
-    return status(unisvq::launch_attn_decode(c, lens, max_len, splits, static_cast<int>(q_len),
+    return status(unisvq::launch_attn_decode(c, lens, max_len, slots, static_cast<int>(q_len),
                                              static_cast<int>(q_heads), rows(q, q_token_stride, q_head_stride),
                                              x_dtype, scale, rows(out, out_token_stride, out_head_stride), lse,
                                              workspace, static_cast<hipStream_t>(stream)));

@@ -33,10 +33,20 @@
 // values' scales the weights, both in fp32; queries are scaled by a power of
 // two into f16's range.
 //
-// A workgroup's four waves take every fourth 32-token tile of the workgroup's
-// part of the sequence, the next tile's loads under way while one is computed,
-// each with its own running maximum m, sum and outputs, joined through LDS;
-// parts are joined by a second launch.  m is raised only when a score exceeds
+// Work.  An item is a sequence's rows on one key head (sixteen of them), in
+// units of 128 tokens.  The units of all items are dealt out evenly, so that a
+// ragged batch loads the GPU as evenly as one of equal lengths; the lengths are
+// on the device, so every workgroup finds its share by a scan over them.  Up to
+// 2048 units a share is what 512 workgroups (two a CU) make of them, up to
+// 4096 four units, above that what 1024 workgroups make of them: a workgroup
+// costs about what two units do, and two rounds of them even out what CUs
+// differ by (16 x 8192 tokens of 8-bit cache, 8 heads: 1024 workgroups 62 us,
+// 2048 72 us; 16 ragged sequences up to 8192 tokens: 25 us, 43 us where each
+// sequence was cut into as many parts).  A share may begin and end within items: an item
+// within one share is finished there, others are joined by a second launch.
+// A workgroup's four waves take every fourth 32-token tile of its part of an
+// item, the next tile's loads under way while one is computed, each with its
+// own running maximum m, sum and outputs, joined through LDS.  m is raised only when a score exceeds
 // it by 2^8 (the weights then stay below 2^8, well inside f16), so most tiles
 // need no exchange between lanes and no rescaling.
 #include <algorithm>
@@ -48,6 +58,10 @@ namespace unisvq {
 namespace {
 
 constexpr int kThreads = 256, kWaves = 4, kTile = 32, kRows = 16;
+constexpr int kUnit = kWaves * kTile;  // tokens
+constexpr int kResident = 512;         // workgroups that the GPU holds at once: two a CU
+constexpr int kGrid = 2 * kResident;   // workgroups at most
+constexpr int kSlots = 66;             // parts of a row at most, of which two are not whole shares
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kSlack = 8.0f;  // log2 of how far scores may exceed the running maximum
 
@@ -56,11 +70,12 @@ struct Decode {
     const int32_t* lens;
     Rows q, out;
     float* lse;
-    float* part;   // [rows][splits][D] sums, null when splits == 1
-    float2* part_ml;  // [rows][splits] maximum (log2) and sum
-    int splits, chunk;  // tokens of a split, a multiple of kTile
+    float* part;      // [rows][slots][D] sums, where slots > 1
+    float2* part_ml;  // [rows][slots] maximum (log2) and sum
+    int32_t* before;  // [sequences + 1] units of an item of the sequences before, and the share after them
+    int slots;        // parts a row can have; 1: a workgroup has an item
     int q_len, q_heads, group, row_tiles;
-    float scale;  // of the scores, times log2 e
+    float scale;      // of the scores, times log2 e
 };
 
 __device__ inline f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -117,7 +132,7 @@ struct Pages {
 __device__ inline Pages look_up(const Decode& a, const int32_t* row, int p, int len) {
     Pages r;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) r.at[t] = p + 16 * t < len ? row[(p + 16 * t) >> a.c.page_shift] : -1;
+    for (int t = 0; t < 2; ++t) r.at[t] = p + 16 * t < len ? load_uniform(row + ((p + 16 * t) >> a.c.page_shift)) : -1;
     return r;
 }
 
@@ -349,6 +364,7 @@ __device__ __forceinline__ void attend(const Decode& a, TileRegs<KIND, D>& r, in
         }
     top *= w.qscale;
     if constexpr (G::scaled) vtop = largest_bits<KIND>(vtop);
+    const uint32_t vmost = vtop;  // the lane's
     if (__any(top > w.m + kSlack || (G::scaled && vtop > w.most_bits))) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
@@ -385,12 +401,19 @@ __device__ __forceinline__ void attend(const Decode& a, TileRegs<KIND, D>& r, in
             w.l += v;
 #pragma unroll
             for (int x = 0; x < HV; ++x)
-                // (a weight of zero stays one where the scale is NaN, for rows that do not see the token)
-                p[x][4 * t + n] = static_cast<CT>(!G::scaled ? v
-                                                  : full || s[t][n] > -INFINITY || s[t][n] != s[t][n]
-                                                      ? v * scale_of<KIND>(r.vs[t][n], x)
-                                                      : 0.0f);
+                p[x][4 * t + n] = static_cast<CT>(G::scaled ? v * scale_of<KIND>(r.vs[t][n], x) : v);
         }
+    if constexpr (G::scaled) {
+        // rows that do not see a token have no part of a scale that is not finite
+        if (!full && __any(vmost >= 0x7f800000u))
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+                    if (s[t][n] == -INFINITY)
+#pragma unroll
+                        for (int x = 0; x < HV; ++x) p[x][4 * t + n] = static_cast<CT>(0.0f);
+    }
     if constexpr (!G::scaled) {  // codes are finite, and a scale that is not is the weight's matter
         if (!full && a.q_len > 1) only_where_seen<KIND, D, CT>(r, pos, w.limit, g, w.o[0]);
     }
@@ -408,32 +431,33 @@ __device__ __forceinline__ void attend(const Decode& a, TileRegs<KIND, D>& r, in
     }
 }
 
+// Units of a sequence's items: one also where there is nothing to see (its rows
+// are to become zeros).
+__device__ inline int units_of(int len) { return max(1, (len + kUnit - 1) / kUnit); }
+
+__device__ inline int length_of(const Decode& a, int64_t b) {
+    const int64_t room = a.c.width << a.c.page_shift;
+    return static_cast<int>(min(static_cast<int64_t>(max(0, a.lens[b])), room));
+}
+
+// Units begin .. end - 1 of item (b, hr), for sequences of length len.  `slot`:
+// of the part, or -1 where the item is all here.
 template <int KIND, int D, typename XT>
-__global__ __launch_bounds__(kThreads, 2) void decode_kernel(Decode a) {
+__device__ __forceinline__ void attend_item(const Decode& a, int b, int hr, int len, int begin, int end, int slot, int wave, int lane) {
     typedef Geometry<KIND, D> G;
     typedef std::conditional_t<G::scaled, _Float16, XT> CT;
     constexpr int E = G::E, HV = G::halves, kPad = 4;
-    const int split = blockIdx.x % a.splits;
-    const int hr = blockIdx.x / a.splits % (a.c.heads * a.row_tiles);
-    const int b = blockIdx.x / a.splits / (a.c.heads * a.row_tiles);
     const int h = hr / a.row_tiles, row0 = hr % a.row_tiles * kRows;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int i = lane & 15, g = lane >> 4;
-    const int64_t room = a.c.width << a.c.page_shift;
-    int len = max(0, a.lens[b]);
-    if (len > room) len = static_cast<int>(room);
-    const int begin = split * a.chunk;
-    const int end = split == a.splits - 1 ? len : min(len, begin + a.chunk);  // past max_len the last goes on
-    if (split > 0 && begin >= len) return;  // the joining launch goes by the length too
+    end = min(len, end * kUnit);
 
     // the first tiles are on their way while the queries are made ready
     const int32_t* row_pages = a.c.table + static_cast<int64_t>(b) * a.c.width;
-    constexpr int kStep = kWaves * kTile;
     TileRegs<KIND, D> r0, r1;
-    int pos = begin + wave * kTile;
+    int pos = begin * kUnit + wave * kTile;
     Pages pages = look_up(a, row_pages, pos, end);
     if (pos < end) load_tile<KIND, D>(a, pages, h, pos, i, g, r0);
-    pages = look_up(a, row_pages, pos + kStep, end);
+    pages = look_up(a, row_pages, pos + kUnit, end);
 
     // the lane's query row: token j, head hq of the group
     const int rows = a.q_len * a.group;
@@ -501,15 +525,15 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(Decode a) {
     }
 
     while (pos < end) {
-        if (pos + kStep < end) load_tile<KIND, D>(a, pages, h, pos + kStep, i, g, r1);
-        pages = look_up(a, row_pages, pos + 2 * kStep, end);
+        if (pos + kUnit < end) load_tile<KIND, D>(a, pages, h, pos + kUnit, i, g, r1);
+        pages = look_up(a, row_pages, pos + 2 * kUnit, end);
         attend<KIND, D, CT>(a, r0, pos, len, g, w);
-        pos += kStep;
+        pos += kUnit;
         if (pos >= end) break;
-        if (pos + kStep < end) load_tile<KIND, D>(a, pages, h, pos + kStep, i, g, r0);
-        pages = look_up(a, row_pages, pos + 2 * kStep, end);
+        if (pos + kUnit < end) load_tile<KIND, D>(a, pages, h, pos + kUnit, i, g, r0);
+        pages = look_up(a, row_pages, pos + 2 * kUnit, end);
         attend<KIND, D, CT>(a, r1, pos, len, g, w);
-        pos += kStep;
+        pos += kUnit;
     }
 
     // join the waves: dim E (4g + n) + e of query i
@@ -549,23 +573,87 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(Decode a) {
     }
     const int jy = (row0 + y) / a.group, hy = h * a.group + (row0 + y) % a.group;
     const int64_t ty = static_cast<int64_t>(b) * a.q_len + jy, r_out = ty * a.q_heads + hy;
-    if (a.splits == 1) {
+    if (slot < 0) {
         const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
 #pragma unroll
         for (int n = 0; n < 8; ++n) f[n] *= inv;
         store8(static_cast<XT*>(a.out.p) + ty * a.out.ts + hy * a.out.hs + d, f);
         if (a.lse && d == 0) a.lse[r_out] = (mt + log2f(lt)) * kLn2;
     } else {
-        float* to = a.part + (r_out * a.splits + split) * D + d;
+        float* to = a.part + (r_out * a.slots + slot) * D + d;
         *reinterpret_cast<f32x4*>(to) = f32x4{f[0], f[1], f[2], f[3]};
         *reinterpret_cast<f32x4*>(to + 4) = f32x4{f[4], f[5], f[6], f[7]};
-        if (d == 0) a.part_ml[r_out * a.splits + split] = float2{mt, lt};
+        if (d == 0) a.part_ml[r_out * a.slots + slot] = float2{mt, lt};
     }
 }
 
+template <int KIND, int D, typename XT>
+__global__ __launch_bounds__(kThreads, 2) void decode_kernel(Decode a) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int items = a.c.heads * a.row_tiles, sequences = static_cast<int>(a.c.sequences);
+    int first = 0, unit, last;  // units of the sequences before b, and those of this workgroup
+    int b = 0, share;
+    if (a.slots == 1) {  // an item, whatever its length
+        b = blockIdx.x / items;
+        share = units_of(length_of(a, b));
+        unit = blockIdx.x % items * share;
+        last = unit + share;
+    } else {
+        int all = 0, most = 0;
+        for (int base = 0; base < sequences; base += 64) {
+            const int units = base + lane < sequences ? units_of(length_of(a, base + lane)) : 0;
+            const int sum = scan64(units);
+            if (blockIdx.x == 0 && wave == 0 && base + lane < sequences) a.before[base + lane] = all + sum - units;
+            all += __builtin_amdgcn_readlane(sum, 63);
+            most = max(most, __builtin_amdgcn_readlane(scan64_max(units), 63));
+        }
+        const int n = all * items;
+        const auto dealt = [n](int workgroups) { return (n + workgroups - 1) / workgroups; };
+        share = max(dealt(kGrid), min(4, dealt(kResident)));
+        // what the launch has workgroups and rows have slots for, whatever the lengths
+        share = max(max(share, dealt(gridDim.x)), (most + a.slots - 3) / (a.slots - 2));
+        if (blockIdx.x == 0 && wave == 0 && lane == 0) a.before[sequences] = all, a.before[sequences + 1] = share;
+        if (static_cast<int64_t>(blockIdx.x) * share >= n) return;
+        unit = blockIdx.x * share;
+        last = min(unit + share, n);
+        for (int base = 0;; base += 64) {
+            const int units = base + lane < sequences ? units_of(length_of(a, base + lane)) : 0;
+            const int sum = scan64(units);
+            const uint64_t in = __ballot(unit < (first + sum) * items);
+            if (in) {
+                const int l = __ffsll(static_cast<unsigned long long>(in)) - 1;
+                b = base + l;
+                first += __builtin_amdgcn_readlane(sum - units, l);
+                break;
+            }
+            first += __builtin_amdgcn_readlane(sum, 63);
+        }
+    }
+    while (unit < last) {
+        const int64_t room = a.c.width << a.c.page_shift;
+        const int len = static_cast<int>(min(static_cast<int64_t>(max(0, load_uniform(a.lens + b))), room)), n = units_of(len);
+        const int hr = (unit - first * items) / n, item = first * items + hr * n;
+        const int begin = unit - item, end = min(n, last - item);
+        const Shares s = shares_of(item, n, share);
+        attend_item<KIND, D, XT>(a, b, hr, len, begin, end, s.count == 1 ? -1 : static_cast<int>(blockIdx.x) - s.first, wave, lane);
+        unit += end - begin;
+        if (hr == items - 1 && end == n) first += n, ++b;
+        __syncthreads();  // (LDS is used again)
+    }
+}
+
+// Workgroups: as many as there are units if all sequences have max_len tokens.
+int decode_grid(int64_t sequences, int items, int64_t max_len) {
+    const int64_t units = std::max<int64_t>(1, (max_len + kUnit - 1) / kUnit) * sequences * items;
+    return static_cast<int>(std::min<int64_t>(units, kGrid));
+}
+
+int row_tiles_of(int q_len, int q_heads, int kv_heads) { return (q_len * (q_heads / kv_heads) + kRows - 1) / kRows; }
+
 template <int D, typename XT>
-hipError_t run(const Decode& a, hipStream_t s) {
-    const uint32_t blocks = static_cast<uint32_t>(a.c.sequences * a.c.heads * a.row_tiles * a.splits);
+hipError_t run(const Decode& a, int64_t max_len, hipStream_t s) {
+    const int items = a.c.heads * a.row_tiles;
+    const uint32_t blocks = a.slots == 1 ? static_cast<uint32_t>(a.c.sequences * items) : decode_grid(a.c.sequences, items, max_len);
     constexpr int raw = std::is_same_v<XT, _Float16> ? UNISVQ_CACHE_F16 : UNISVQ_CACHE_BF16;
     if (a.c.kind == UNISVQ_CACHE_I8)
         decode_kernel<UNISVQ_CACHE_I8, D, XT><<<blocks, kThreads, 0, s>>>(a);
@@ -573,62 +661,63 @@ hipError_t run(const Decode& a, hipStream_t s) {
         decode_kernel<UNISVQ_CACHE_I4, D, XT><<<blocks, kThreads, 0, s>>>(a);
     else
         decode_kernel<raw, D, XT><<<blocks, kThreads, 0, s>>>(a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.splits == 1) return e;
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.slots == 1) return e;
     Join j{};
     j.part = a.part;
     j.part_ml = a.part_ml;
     j.rows = a.c.sequences * a.q_len * a.q_heads;
-    j.splits = a.splits;
+    j.slots = a.slots;
     j.q_heads = a.q_heads;
     j.out = a.out;
     j.lse = a.lse;
-    j.lens = a.lens;
+    j.before = a.before;
+    j.share = a.before + a.c.sequences + 1;
     j.q_len = a.q_len;
-    j.chunk = a.chunk;
+    j.group = a.group;
+    j.items = items;
+    j.row_tiles = a.row_tiles;
+    j.tile = kRows;
     return launch_join<D, XT>(j, s);
 }
 
 }  // namespace
 
-// Splits: about 2048 workgroups of at least two tiles a wave if all sequences
-// were the longest (a ragged batch has its work in few of them), else about 512
-// of at least one.
-int decode_splits(int64_t sequences, int q_len, int q_heads, int kv_heads, int64_t max_len) {
-    const int64_t base = sequences * kv_heads * ((q_len * (q_heads / kv_heads) + kRows - 1) / kRows);
-    const auto parts = [&](int64_t tokens) { return (max_len + tokens - 1) / tokens; };
-    constexpr int64_t step = kWaves * kTile;
-    int64_t n = std::min(2048 / base, parts(2 * step));
-    if (base * n < 512) n = std::min(std::max<int64_t>(1, 512 / base), parts(step));
-    return static_cast<int>(std::min<int64_t>(std::max<int64_t>(1, n), 256));
+// Parts a row can have (a share is made large enough for it): one where no
+// sequence is to have more than a unit; then workgroups have whole items.
+int decode_slots(int64_t sequences, int q_len, int q_heads, int kv_heads, int64_t max_len) {
+    if (max_len <= kUnit) return 1;
+    const int items = kv_heads * row_tiles_of(q_len, q_heads, kv_heads);
+    return std::min(kSlots, decode_grid(sequences, items, max_len) / items + 2);
 }
 
-size_t decode_workspace_bytes(int64_t sequences, int q_len, int q_heads, int head_dim, int splits) {
-    if (splits == 1) return 0;
-    return static_cast<size_t>(sequences * q_len * q_heads) * splits * (head_dim + 2) * 4;
+size_t decode_workspace_bytes(int64_t sequences, int q_len, int q_heads, int head_dim, int slots) {
+    if (slots == 1) return 0;
+    return static_cast<size_t>(sequences * q_len * q_heads) * slots * (head_dim + 2) * 4 + static_cast<size_t>(sequences + 2) * 4;
 }
 
-hipError_t launch_attn_decode(const CacheView& c, const int32_t* lens, int64_t max_len, int splits, int q_len, int q_heads, Rows q,
-                              int x_dtype, float scale, Rows out, float* lse, void* workspace, hipStream_t s) {
+hipError_t launch_attn_decode(const CacheView& c, const int32_t* lens, int64_t max_len, int slots, int q_len, int q_heads,
+                              Rows q, int x_dtype, float scale, Rows out, float* lse, void* workspace, hipStream_t s) {
     Decode a{};
     a.c = c;
     a.lens = lens;
     a.q = q;
     a.out = out;
     a.lse = lse;
-    a.splits = splits;
-    a.chunk = static_cast<int>(((max_len + splits - 1) / splits + kTile - 1) / kTile * kTile);
+    a.slots = slots;
     a.q_len = q_len;
     a.q_heads = q_heads;
     a.group = q_heads / c.heads;
-    a.row_tiles = (q_len * a.group + kRows - 1) / kRows;
+    a.row_tiles = row_tiles_of(q_len, q_heads, c.heads);
     a.scale = scale * kLog2e;
-    if (splits > 1) {
+    if (slots > 1) {
+        const int64_t parts = c.sequences * q_len * q_heads * slots;
         a.part = static_cast<float*>(workspace);
-        a.part_ml = reinterpret_cast<float2*>(a.part + c.sequences * q_len * q_heads * splits * c.head_dim);
+        a.part_ml = reinterpret_cast<float2*>(a.part + parts * c.head_dim);
+        a.before = reinterpret_cast<int32_t*>(a.part_ml + parts);
     }
-    if (c.head_dim == 128) return x_dtype == UNISVQ_F16 ? run<128, _Float16>(a, s) : run<128, __bf16>(a, s);
-    return x_dtype == UNISVQ_F16 ? run<64, _Float16>(a, s) : run<64, __bf16>(a, s);
+    if (c.head_dim == 128) return x_dtype == UNISVQ_F16 ? run<128, _Float16>(a, max_len, s) : run<128, __bf16>(a, max_len, s);
+    return x_dtype == UNISVQ_F16 ? run<64, _Float16>(a, max_len, s) : run<64, __bf16>(a, max_len, s);
 }
 
 }  // namespace unisvq

@@ -1,8 +1,10 @@
 // Joining the parts of split attention rows: every part has a maximum m_p
 // (log2), a sum l_p and the sums o_p of its weighted values, and
 //   m = max m_p,  l = sum 2^(m_p - m) l_p,  out = sum 2^(m_p - m) o_p / l.
-// Bound by reading the parts.  Sixteen lanes have a row (eight or four dims
-// each), in the order of the parts, so a result does not depend on timing.
+// Bound by reading the parts.  Sixteen lanes have a part of a row (eight or
+// four dims each).  Few rows have many parts: then sixteen such groups share a
+// row, every sixteenth part each, and are joined through LDS.  The order goes
+// by the parts alone, so a result does not depend on timing.
 #pragma once
 
 #include <cfloat>
@@ -12,43 +14,62 @@
 namespace unisvq {
 
 struct Join {
-    const float* part;      // [rows][splits][D]
-    const float2* part_ml;  // [rows][splits]
+    const float* part;      // [rows][slots][D]
+    const float2* part_ml;  // [rows][slots]
     int64_t rows;           // tokens * q_heads
-    int splits, q_heads;
+    int slots, q_heads;
     Rows out;
     float* lse;             // [rows] or null
     const int32_t* tokens;  // rows of tokens from *tokens on are left alone; null: there are none
-    // Parts that there are of a row: those that begin before the length of its
-    // sequence (of q_len tokens); null: all.
-    const int32_t* lens;
-    int q_len, chunk;
+    // Where rows have different numbers of parts (else null, and all slots are
+    // theirs): before[b] counts the units of work of an item of sequences 0 ..
+    // b - 1, and an item is the q_len tokens' `tile` rows of one of `items`
+    // (key heads times row tiles).  Units are dealt out `share` a workgroup, in
+    // order; an item within one share needs no joining.
+    const int32_t* before;
+    const int32_t* share;
+    int q_len, group, items, row_tiles, tile;
 };
+
+// The shares that units first .. first + n - 1 lie in: the first, and how many.
+struct Shares {
+    int first, count;
+};
+__device__ inline Shares shares_of(int first, int n, int share) {
+    const int a = first / share;
+    return Shares{a, (first + n - 1) / share - a + 1};
+}
 
 namespace {
 
 constexpr float kJoinLn2 = 0.69314718055994530942f;
 
-template <int D, typename T>
+template <int D, typename T, int GROUPS>
 __global__ __launch_bounds__(256) void join_kernel(Join j) {
     constexpr int kDims = D / 16;
-    const int64_t r = static_cast<int64_t>(blockIdx.x) * 16 + threadIdx.x / 16;
-    if (r >= j.rows) return;
-    const int at = threadIdx.x % 16;
+    const int64_t r = static_cast<int64_t>(blockIdx.x) * (16 / GROUPS) + threadIdx.x / (16 * GROUPS);
+    const int group = threadIdx.x / 16 % GROUPS, at = threadIdx.x % 16;
+    if (r >= j.rows) return;  // (with GROUPS > 1 a block has one row)
     const int64_t token = r / j.q_heads;
     const int head = static_cast<int>(r - token * j.q_heads);
     if (j.tokens && token >= *j.tokens) return;
-    int n = j.splits;
-    if (j.lens) n = min(n, max(0, j.lens[token / j.q_len] - 1) / j.chunk + 1);
-    const float2* ml = j.part_ml + r * j.splits;
+    int n = j.slots;
+    if (j.before) {
+        const int64_t b = token / j.q_len;
+        const int units = j.before[b + 1] - j.before[b];
+        const int item = head / j.group * j.row_tiles + (static_cast<int>(token - b * j.q_len) * j.group + head % j.group) / j.tile;
+        n = shares_of(j.before[b] * j.items + item * units, units, *j.share).count;
+        if (n == 1) return;
+    }
+    const float2* ml = j.part_ml + r * j.slots;
     float m = -FLT_MAX;
     for (int x = at; x < n; x += 16) m = fmaxf(m, ml[x].x);
 #pragma unroll
     for (int d = 1; d < 16; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
-    const float* part = j.part + r * j.splits * D + at * kDims;
+    const float* part = j.part + r * j.slots * D + at * kDims;
     float l = 0.0f, f[kDims] = {};
 #pragma unroll 4
-    for (int x = 0; x < n; ++x) {
+    for (int x = group; x < n; x += GROUPS) {
         const float2 here = ml[x];
         float v[kDims];
 #pragma unroll
@@ -57,12 +78,24 @@ __global__ __launch_bounds__(256) void join_kernel(Join j) {
 #pragma unroll
             for (int z = 0; z < 4; ++z) v[y + z] = q[z];
         }
-        // (a part that saw nothing has written no sums)
-        const bool some = here.y != 0.0f;
-        const float c = some ? __builtin_amdgcn_exp2f(here.x - m) : 0.0f;
+        const float c = __builtin_amdgcn_exp2f(here.x - m);
         l += c * here.y;
 #pragma unroll
-        for (int y = 0; y < kDims; ++y) f[y] += some ? c * v[y] : 0.0f;
+        for (int y = 0; y < kDims; ++y) f[y] += c * v[y];
+    }
+    if constexpr (GROUPS > 1) {
+        __shared__ float so[GROUPS][16][kDims + 1];
+#pragma unroll
+        for (int y = 0; y < kDims; ++y) so[group][at][y] = f[y];
+        so[group][at][kDims] = l;
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int x = 1; x < GROUPS; ++x) {
+#pragma unroll
+            for (int y = 0; y < kDims; ++y) f[y] += so[x][at][y];
+            l += so[x][at][kDims];
+        }
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     typedef T TN __attribute__((ext_vector_type(kDims)));
@@ -75,7 +108,10 @@ __global__ __launch_bounds__(256) void join_kernel(Join j) {
 
 template <int D, typename T>
 hipError_t launch_join(const Join& j, hipStream_t s) {
-    join_kernel<D, T><<<static_cast<uint32_t>((j.rows + 15) / 16), 256, 0, s>>>(j);
+    if (j.rows <= 4096 && j.slots > 4)
+        join_kernel<D, T, 16><<<static_cast<uint32_t>(j.rows), 256, 0, s>>>(j);
+    else
+        join_kernel<D, T, 1><<<static_cast<uint32_t>((j.rows + 15) / 16), 256, 0, s>>>(j);
     return hipGetLastError();
 }
 

@@ -132,17 +132,6 @@ __device__ inline void drop_not_finite(T* vs, int wave, int lane) {
         for (int x = 0; x < 4; ++x) at[64 * n][x] = finite_only<T>(at[64 * n][x]);
 }
 
-// Sum over the lanes up to this one.
-__device__ inline int scan64(int x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
-    return x;
-}
-
 // A barrier of all waves that waits for no loads in flight.
 __device__ inline void phase() {
     __builtin_amdgcn_sched_barrier(0);
@@ -526,7 +515,7 @@ hipError_t run(const PromptArgs& a, void* workspace, hipStream_t s) {
     j.part = g.part;
     j.part_ml = g.part_ml;
     j.rows = rows;
-    j.splits = g.splits;
+    j.slots = g.splits;
     j.q_heads = a.q_heads;
     j.out = a.out;
     j.lse = a.lse;

@@ -9,6 +9,7 @@ library has not been built the first call raises ``UniSVQLibraryMissing``.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -843,43 +844,81 @@ def read_bytes(buffers, store: bool = True, sink=None, stream=None):
 
 # ---- the attention block ----
 
-def _rows(t, what: str, heads: int | None = None, head_dim: int | None = None, tokens: int | None = None, dtype=None):
-    """A [tokens][heads][head_dim] fp16/bf16 tensor, its last axis contiguous, any strides of the other two (the C
-    entry refuses those that are not multiples of 8): checked, and as (pointer, token stride, head stride)."""
-    torch = _torch()
-    shape = t.shape
-    if len(shape) != 3:
-        raise ValueError(f"{what} must be [tokens][heads][head_dim], got {tuple(shape)}")
+_HALVES = {}  # the 16-bit dtypes and their codes, once torch is there
+
+
+def _halves():
+    if not _HALVES:
+        torch = _torch()
+        _HALVES.update({torch.float16: F16, torch.bfloat16: BF16})
+    return _HALVES
+
+
+_current_stream = None  # of a device's index, as a handle
+
+
+def _raw_stream(stream, t) -> int:
+    """The stream's handle; None: the current one of t's device."""
+    global _current_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _current_stream is None:
+        torch = _torch()
+        # (torch's own way to the handle without a Stream object around it, where it has one)
+        _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                                  lambda device: torch.cuda.current_stream(device).cuda_stream)
+    return _current_stream(t.get_device())
+
+
+def _rows(t, what: str, heads=None, head_dim=None, tokens=None, dtype=None):
+    """A [tokens][heads][head_dim] fp16/bf16 device tensor, its last axis contiguous, any strides of the other two (the
+    C entry refuses those that are not multiples of 8): checked, and as (pointer, token stride, head stride)."""
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 3 or strides[2] != 1:
+        raise ValueError(f"{what} must be [tokens][heads][head_dim] with contiguous dims, got {tuple(shape)}, strides {strides}")
     if not t.is_cuda:
         raise ValueError("libunisvq takes device tensors only")
-    if dtype is not None and t.dtype != dtype:
-        raise TypeError(f"{what} is {t.dtype}, expected {dtype}")
-    if t.dtype not in (torch.float16, torch.bfloat16):
-        raise TypeError(f"{what} must be fp16 or bf16, got {t.dtype}")
+    if t.dtype is not dtype and (dtype is not None or t.dtype not in _halves()):
+        raise TypeError(f"{what} is {t.dtype}, expected {'fp16 or bf16' if dtype is None else dtype}")
     if (tokens is not None and shape[0] != tokens) or (heads is not None and shape[1] != heads) or \
             (head_dim is not None and shape[2] != head_dim):
         raise ValueError(f"{what} is {tuple(shape)}, expected {(tokens, heads, head_dim)}")
-    strides = t.stride()
-    if strides[2] != 1:
-        raise ValueError(f"the dims of {what}'s heads must be contiguous")
     return t.data_ptr(), strides[0], strides[1]
 
 
-def _ints(t, count: int, what: str):
-    """A contiguous int32 device tensor of `count` elements, as a pointer."""
-    torch = _torch()
-    if t.dtype != torch.int32 or t.numel() != count or not t.is_contiguous():
-        raise ValueError(f"{what} must hold {count} contiguous int32, got {t.dtype} {tuple(t.shape)}")
-    if not t.is_cuda:
-        raise ValueError("libunisvq takes device tensors only")
+def _words(t, count: int, what: str, dtype):
+    """A contiguous device tensor of `count` elements of dtype, as a pointer (None: None)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != count or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{what} must hold {count} contiguous {dtype} on the device, got {t.dtype} {tuple(t.shape)}")
     return t.data_ptr()
 
 
 def _out_rows(out, like, tokens: int, heads: int, head_dim: int, what: str = "out"):
     """The caller's out (checked) or a new tensor, and its rows."""
     if out is None:
-        out = _torch().empty((tokens, heads, head_dim), dtype=like.dtype, device=like.device)
+        out = like.new_empty((tokens, heads, head_dim))
     return out, _rows(out, what, heads, head_dim, tokens, like.dtype)
+
+
+@functools.lru_cache(maxsize=4096)
+def _workspace_size(name: str, *shape) -> int:
+    return getattr(load(), name)(*shape)
+
+
+def _scratch(workspace, need: int, like, stream):
+    """(tensor, pointer, bytes) of the caller's workspace or of a new one, which stays the stream's until its work there
+    is done."""
+    if workspace is None:
+        if not need:
+            return None, None, 0
+        workspace = like.new_empty(need, dtype=_torch().uint8)
+        if stream is not None:
+            workspace.record_stream(stream)
+    else:
+        workspace, need = _workspace(workspace, need, like)
+    return workspace, workspace.data_ptr(), need
 
 
 def rope_table(positions: int, rot: int, theta: float = 10000.0, factor: float = 1.0, low: float = 1.0,
@@ -895,12 +934,9 @@ def rope_table(positions: int, rot: int, theta: float = 10000.0, factor: float =
 
 def _rope_rows(table):
     """(pointer, positions, rot) of a table of rope_table's."""
-    torch = _torch()
     shape = table.shape
-    if table.dtype != torch.float32 or len(shape) != 3 or shape[1] != 2 or not table.is_contiguous():
-        raise ValueError("the rope table must be contiguous fp32 [positions][2][rot / 2]")
-    if not table.is_cuda:
-        raise ValueError("libunisvq takes device tensors only")
+    if table.dtype is not _torch().float32 or len(shape) != 3 or shape[1] != 2 or not table.is_contiguous() or not table.is_cuda:
+        raise ValueError("the rope table must be contiguous fp32 [positions][2][rot / 2] on the device")
     return table.data_ptr(), shape[0], 2 * shape[2]
 
 
@@ -908,13 +944,15 @@ def rope(x, positions, table, interleaved: bool = False, inverse: bool = False, 
     """x [tokens][heads][head_dim] rotated to int32 positions [tokens]: the first rot = 2 * table.shape[2] dims of
     every head, in pairs (i, i + rot / 2) or, interleaved, (2i, 2i + 1); inverse: the transpose (the gradient).
     out may be x (in place) or a view with its own strides."""
-    tokens, heads, head_dim = x.shape
     xr = _rows(x, "x")
+    tokens, heads, head_dim = x.shape
     out, yr = _out_rows(out, x, tokens, heads, head_dim)
     tp, n, rot = _rope_rows(table)
-    _check("unisvq_rope", load().unisvq_rope(tokens, heads, head_dim, rot, interleaved, inverse, *xr,
-                                             _ints(positions, tokens, "positions"), tp, n, *yr, _dtype_code(x.dtype),
-                                             _stream(stream)))
+    st = load().unisvq_rope(tokens, heads, head_dim, rot, interleaved, inverse, *xr,
+                            _words(positions, tokens, "positions", _torch().int32), tp, n, *yr, _halves()[x.dtype],
+                            _raw_stream(stream, x))
+    if st:
+        raise UniSVQError("unisvq_rope", st)
     return out
 
 
@@ -936,40 +974,42 @@ def new_cache(pages: int, kv_heads: int, page_tokens: int, head_dim: int, kind: 
     return (*pools, *scales)
 
 
+_KINDS = {}  # dtype of the pools -> (kind, dims an element holds, dtype of the scales)
+
+
 def _cache(cache):
     """The C description of a cache tuple (k, v, k_scales, v_scales), checked; the kind is the pools' dtype's."""
-    torch = _torch()
+    if not _KINDS:
+        torch = _torch()
+        _KINDS.update({torch.float16: (CACHE_F16, 1, None), torch.bfloat16: (CACHE_BF16, 1, None),
+                       torch.int8: (CACHE_I8, 1, torch.float32), torch.uint8: (CACHE_I4, 2, torch.bfloat16)})
     k, v, ks, vs = cache
     dt, shape = k.dtype, k.shape
-    if dt == torch.int8:
-        kind, head_dim = CACHE_I8, shape[-1]
-    elif dt == torch.uint8:
-        kind, head_dim = CACHE_I4, 2 * shape[-1]
-    elif dt == torch.float16:
-        kind, head_dim = CACHE_F16, shape[-1]
-    elif dt == torch.bfloat16:
-        kind, head_dim = CACHE_BF16, shape[-1]
-    else:
+    if dt not in _KINDS:
         raise TypeError(f"a cache's pools are fp16, bf16, int8 or uint8 (4-bit codes), got {dt}")
-    if len(shape) != 4 or v.shape != shape or v.dtype != dt or not (k.is_contiguous() and v.is_contiguous()):
+    kind, dims, scale_type = _KINDS[dt]
+    if len(shape) != 4 or v.shape != shape or v.dtype is not dt or not (k.is_contiguous() and v.is_contiguous()):
         raise ValueError("k and v pools must be contiguous [pages][kv_heads][page_tokens][..] of one dtype")
     if not (k.is_cuda and v.is_cuda):
         raise ValueError("libunisvq takes device tensors only")
-    if kind >= CACHE_I8:
-        want = (torch.float32, shape[:3]) if kind == CACHE_I8 else (torch.bfloat16, (*shape[:3], 2))
-        for t in (ks, vs):
-            if t is None or t.dtype != want[0] or t.shape != want[1] or not t.is_contiguous() or not t.is_cuda:
-                raise ValueError(f"scales must be contiguous {want[0]} {tuple(want[1])} on the device")
-        return Cache(shape[0], shape[2], shape[1], head_dim, kind, k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr())
-    return Cache(shape[0], shape[2], shape[1], head_dim, kind, k.data_ptr(), v.data_ptr(), None, None)
+    pages, kv_heads, page_tokens, last = shape
+    ksp = vsp = None
+    if scale_type is not None:
+        if ks is None or vs is None:
+            raise ValueError("codes come with scales")
+        count = pages * kv_heads * page_tokens * dims
+        ksp, vsp = _words(ks, count, "k_scales", scale_type), _words(vs, count, "v_scales", scale_type)
+    return Cache(pages, page_tokens, kv_heads, last * dims, kind, k.data_ptr(), v.data_ptr(), ksp, vsp)
 
 
 def _page_table(table):
-    torch = _torch()
     shape = table.shape
-    if table.dtype != torch.int32 or len(shape) != 2 or not table.is_contiguous() or not table.is_cuda:
+    if table.dtype is not _torch().int32 or len(shape) != 2 or not table.is_contiguous() or not table.is_cuda:
         raise ValueError("the page table must be contiguous int32 [sequences][pages of a sequence] on the device")
     return table.data_ptr(), shape[0], shape[1]
+
+
+_NO_ROWS = (None, 0, 0)
 
 
 def cache_append(cache, page_table, seqs, positions, k, v, q=None, rope_table=None, interleaved: bool = False,
@@ -978,19 +1018,21 @@ def cache_append(cache, page_table, seqs, positions, k, v, q=None, rope_table=No
     int32 positions [tokens] of sequences seqs [tokens] (None: token t is sequence t's).  q [tokens][q_heads][head_dim]
     is rotated in the same launch and returned (q_out, which may be q, or a new tensor; None where q is None)."""
     c = _cache(cache)
+    int32, kv_heads, head_dim, dt = _torch().int32, c.kv_heads, c.head_dim, k.dtype
+    kr = _rows(k, "k", kv_heads, head_dim)
     tokens = k.shape[0]
-    kr = _rows(k, "k", c.kv_heads, c.head_dim)
-    vr = _rows(v, "v", c.kv_heads, c.head_dim, tokens, k.dtype)
-    q_heads, qr, qor = 0, (None, 0, 0), (None, 0, 0)
+    vr = _rows(v, "v", kv_heads, head_dim, tokens, dt)
+    q_heads, qr, qor = 0, _NO_ROWS, _NO_ROWS
     if q is not None:
+        qr = _rows(q, "q", None, head_dim, tokens, dt)
         q_heads = q.shape[1]
-        qr = _rows(q, "q", q_heads, c.head_dim, tokens, k.dtype)
-        q_out, qor = _out_rows(q_out, q, tokens, q_heads, c.head_dim, "q_out")
-    rr = (None, 0, 0) if rope_table is None else _rope_rows(rope_table)
-    _check("unisvq_cache_append", load().unisvq_cache_append(
-        c, *_page_table(page_table), tokens, None if seqs is None else _ints(seqs, tokens, "seqs"),
-        _ints(positions, tokens, "positions"), *kr, *vr, qr[0], q_heads, qr[1], qr[2], *qor, _dtype_code(k.dtype), *rr,
-        interleaved, _stream(stream)))
+        q_out, qor = _out_rows(q_out, q, tokens, q_heads, head_dim, "q_out")
+    st = load().unisvq_cache_append(
+        c, *_page_table(page_table), tokens, _words(seqs, tokens, "seqs", int32),
+        _words(positions, tokens, "positions", int32), *kr, *vr, qr[0], q_heads, qr[1], qr[2], *qor, _halves()[dt],
+        *(_NO_ROWS if rope_table is None else _rope_rows(rope_table)), interleaved, _raw_stream(stream, k))
+    if st:
+        raise UniSVQError("unisvq_cache_append", st)
     return q_out if q is not None else None
 
 
@@ -1003,23 +1045,16 @@ def cache_read(cache, page_table, starts, cu, tokens: int, out=None, out_dtype=N
     pt = _page_table(page_table)
     if out is None:
         dt = out_dtype or (cache[0].dtype if cache[0].dtype.is_floating_point else torch.float16)
-        out = tuple(torch.empty((tokens, c.kv_heads, c.head_dim), dtype=dt, device=cache[0].device) for _ in range(2))
+        out = tuple(cache[0].new_empty((tokens, c.kv_heads, c.head_dim), dtype=dt) for _ in range(2))
     k, v = out
     kr = _rows(k, "out k", c.kv_heads, c.head_dim, tokens)
     vr = _rows(v, "out v", c.kv_heads, c.head_dim, tokens, k.dtype)
-    _check("unisvq_cache_read", load().unisvq_cache_read(
-        c, *pt, None if starts is None else _ints(starts, pt[1], "starts"), _ints(cu, pt[1] + 1, "cu"), tokens, *kr,
-        *vr, _dtype_code(k.dtype), _stream(stream)))
+    st = load().unisvq_cache_read(c, *pt, _words(starts, pt[1], "starts", torch.int32),
+                                  _words(cu, pt[1] + 1, "cu", torch.int32), tokens, *kr, *vr, _halves()[k.dtype],
+                                  _raw_stream(stream, k))
+    if st:
+        raise UniSVQError("unisvq_cache_read", st)
     return k, v
-
-
-def _lse(lse, count: int):
-    if lse is None:
-        return None
-    torch = _torch()
-    if lse.dtype != torch.float32 or lse.numel() != count or not lse.is_contiguous() or not lse.is_cuda:
-        raise ValueError(f"lse must hold {count} contiguous fp32 on the device")
-    return lse.data_ptr()
 
 
 def attn_decode_workspace_bytes(sequences: int, q_len: int, q_heads: int, kv_heads: int, head_dim: int,
@@ -1033,30 +1068,32 @@ def attn_decode(q, cache, page_table, lens, scale: float | None = None, max_len:
     the cache, which holds their keys and values already; lens int32 [sequences] counts them too.  scale: of the
     scores (None: head_dim ** -0.5).  max_len: what the lengths are at most (0: the page table's width).  lse: fp32
     tensor for the log of the sum of exponentials, or None.  workspace: as gemm's."""
+    torch = _torch()
     c = _cache(cache)
     pt = _page_table(page_table)
-    if q.dim() not in (3, 4):
-        raise ValueError("q must be [sequences][q_heads][head_dim] or [sequences][q_len][q_heads][head_dim]")
-    shape = q.shape
+    shape, head_dim = q.shape, c.head_dim
+    if len(shape) not in (3, 4) or shape[0] != pt[1]:
+        raise ValueError(f"q must be [sequences][q_heads][head_dim] or [sequences][q_len][q_heads][head_dim] of the page "
+                         f"table's {pt[1]} sequences, got {tuple(shape)}")
     sequences, q_len, q_heads = shape[0], shape[1] if len(shape) == 4 else 1, shape[-2]
-    if sequences != pt[1]:
-        raise ValueError(f"q has {sequences} sequences, the page table {pt[1]}")
     tokens = sequences * q_len
-    q3 = q if len(shape) == 3 else q.view(tokens, q_heads, shape[3])
-    qr = _rows(q3, "q", q_heads, c.head_dim)
     if out is None:
-        out = _torch().empty(shape, dtype=q.dtype, device=q.device)
+        out = torch.empty(shape, dtype=q.dtype, device=q.device)
     elif out.shape != shape:
         raise ValueError(f"out is {tuple(out.shape)}, q {tuple(shape)}")
-    orr = _rows(out if len(shape) == 3 else out.view(tokens, q_heads, shape[3]), "out", dtype=q.dtype)
+    q3, out3 = (q, out) if len(shape) == 3 else (q.view(tokens, q_heads, shape[3]), out.view(tokens, q_heads, shape[3]))
+    qr = _rows(q3, "q", None, head_dim)
+    orr = _rows(out3, "out", None, None, None, q.dtype)
     room = pt[2] * c.page_tokens
-    need = attn_decode_workspace_bytes(sequences, q_len, q_heads, c.kv_heads, c.head_dim,
-                                       min(max_len, room) if max_len else room)
-    ws, size = _workspace(workspace, need, q)
-    _check("unisvq_attn_decode", load().unisvq_attn_decode(
-        c, *pt, _ints(lens, sequences, "lens"), max_len, q_len, q_heads, *qr, _dtype_code(q.dtype),
-        c.head_dim ** -0.5 if scale is None else scale, *orr, _lse(lse, tokens * q_heads), _ptr(ws),
-        size, _stream(stream)))
+    need = _workspace_size("unisvq_attn_decode_workspace_bytes", sequences, q_len, q_heads, c.kv_heads, head_dim,
+                           min(max_len, room) if max_len else room)
+    ws, wp, size = _scratch(workspace, need, q, stream)
+    st = load().unisvq_attn_decode(
+        c, *pt, _words(lens, sequences, "lens", torch.int32), max_len, q_len, q_heads, *qr, _halves()[q.dtype],
+        head_dim ** -0.5 if scale is None else scale, *orr, _words(lse, tokens * q_heads, "lse", torch.float32), wp,
+        size, _raw_stream(stream, q))
+    if st:
+        raise UniSVQError("unisvq_attn_decode", st)
     return out
 
 
@@ -1071,18 +1108,21 @@ def attn_prompt(q, k, v, cu_q, cu_k, causal: bool = True, scale: float | None = 
     strides (parts of one fused row, say); sequence b has queries cu_q[b] .. cu_q[b + 1] - 1 and keys cu_k[b] .. (int32
     [sequences + 1]).  Causal: the last query of a sequence sees all its keys, each one before it one key less.  scale,
     lse, workspace: as attn_decode's."""
-    tokens, q_heads, head_dim = q.shape
-    k_tokens, kv_heads = k.shape[0], k.shape[1]
+    torch = _torch()
     qr = _rows(q, "q")
-    kr = _rows(k, "k", kv_heads, head_dim, k_tokens, q.dtype)
+    tokens, q_heads, head_dim = q.shape
+    kr = _rows(k, "k", None, head_dim, None, q.dtype)
+    k_tokens, kv_heads = k.shape[0], k.shape[1]
     vr = _rows(v, "v", kv_heads, head_dim, k_tokens, q.dtype)
     out, orr = _out_rows(out, q, tokens, q_heads, head_dim)
     sequences = cu_q.numel() - 1
-    need = attn_prompt_workspace_bytes(sequences, tokens, k_tokens, q_heads, kv_heads, head_dim)
-    ws, size = _workspace(workspace, need, q)
-    _check("unisvq_attn_prompt", load().unisvq_attn_prompt(
-        sequences, tokens, k_tokens, _ints(cu_q, sequences + 1, "cu_q"), _ints(cu_k, sequences + 1, "cu_k"), q_heads,
-        kv_heads, head_dim, *qr, *kr, *vr, _dtype_code(q.dtype), causal,
-        head_dim ** -0.5 if scale is None else scale, *orr, _lse(lse, tokens * q_heads), _ptr(ws),
-        size, _stream(stream)))
+    need = _workspace_size("unisvq_attn_prompt_workspace_bytes", sequences, tokens, k_tokens, q_heads, kv_heads, head_dim)
+    ws, wp, size = _scratch(workspace, need, q, stream)
+    st = load().unisvq_attn_prompt(
+        sequences, tokens, k_tokens, _words(cu_q, sequences + 1, "cu_q", torch.int32),
+        _words(cu_k, sequences + 1, "cu_k", torch.int32), q_heads, kv_heads, head_dim, *qr, *kr, *vr,
+        _halves()[q.dtype], causal, head_dim ** -0.5 if scale is None else scale, *orr,
+        _words(lse, tokens * q_heads, "lse", torch.float32), wp, size, _raw_stream(stream, q))
+    if st:
+        raise UniSVQError("unisvq_attn_prompt", st)
     return out
