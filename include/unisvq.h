@@ -595,7 +595,8 @@ int unisvq_rope_table(int64_t positions, int64_t rot, double theta, double facto
  * `inverse` turns the other way (s -> -s): the transpose of the rotation and
  * so its gradient.
  *   tokens >= 0, heads >= 1; head_dim a multiple of 16 to 1024; rot a
- *   multiple of 16, 16..head_dim (UNISVQ_EUNSUP otherwise)
+ *   multiple of 16, 16..head_dim; tokens * heads * head_dim below 2^35
+ *   (UNISVQ_EUNSUP otherwise)
  *   positions  device int32 [tokens]; a token whose position is outside
  *              [0, table_positions) gets NaN in its rotated dims
  *   table      device fp32 [table_positions][2][rot / 2], 16-byte aligned
@@ -651,8 +652,9 @@ typedef struct {
  *               NULL: nothing is rotated (then q is copied)
  * Keys are rotated in fp32 as by unisvq_rope and quantised without rounding
  * in between; 16-bit kinds round once.  x_dtype F16 or BF16; a 16-bit kind
- * has to be x_dtype's (UNISVQ_EUNSUP).  Two tokens of one call with the same
- * place: either is stored, or a mix of both. */
+ * has to be x_dtype's, and tokens * (q_heads + 2 kv_heads) * head_dim below
+ * 2^35 (UNISVQ_EUNSUP).  Two tokens of one call with the same place: either is
+ * stored, or a mix of both. */
 int unisvq_cache_append(const unisvq_cache* cache, const int32_t* page_table, int64_t sequences, int64_t table_width,
                         int64_t tokens, const int32_t* seqs, const int32_t* positions, const void* k,
                         int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
@@ -667,7 +669,8 @@ int unisvq_cache_append(const unisvq_cache* cache, const int32_t* page_table, in
  *   starts  device int32 [sequences], or NULL: 0
  *   cu      device int32 [sequences + 1], not decreasing, cu[0] = 0
  *   tokens  rows of k_out and v_out; rows from cu[sequences] on are left as
- *           they are, rows of places without a page become NaN
+ *           they are, rows of places without a page become NaN; tokens *
+ *           kv_heads * head_dim below 2^35 (UNISVQ_EUNSUP otherwise)
  *   k_out, v_out  device [tokens][kv_heads][head_dim] of dtype F16 or BF16 */
 int unisvq_cache_read(const unisvq_cache* cache, const int32_t* page_table, int64_t sequences, int64_t table_width,
                       const int32_t* starts, const int32_t* cu, int64_t tokens, void* k_out, int64_t k_token_stride,
@@ -686,7 +689,10 @@ int unisvq_cache_read(const unisvq_cache* cache, const int32_t* page_table, int6
  *   max_len    what the lengths are at most, which sets how the cache is split
  *              over the GPU; 0: the page table's whole width.  Longer
  *              sequences are served all the same
- *   q_len      1..16; q_heads a multiple of kv_heads
+ *   q_len      1..16; q_heads a multiple of kv_heads.  With items = sequences
+ *              * kv_heads * ceil(q_len * q_heads / kv_heads / 16): items below
+ *              2^24 and items * (table_width * page_tokens / 128 + 1) to 2^30
+ *              (UNISVQ_EUNSUP otherwise)
  *   q, out     device [sequences * q_len][q_heads][head_dim], x_dtype; a
  *              16-bit kind has to be x_dtype's (UNISVQ_EUNSUP)
  *   lse        device fp32 [sequences * q_len][q_heads] or NULL: the log of
@@ -717,7 +723,9 @@ int unisvq_attn_decode(const unisvq_cache* cache, const int32_t* page_table, int
  *               from cu_q[sequences] on are left as they are
  *   q, out      device [q_tokens][q_heads][head_dim]; k, v [k_tokens][kv_heads][head_dim]
  *   head_dim    64 or 128; q_heads a multiple of kv_heads; token strides of k
- *               and v from head_dim to 2^22 (UNISVQ_EUNSUP otherwise)
+ *               and v from head_dim to 2^22; q_tokens * q_heads below 2^31
+ *               and q_tokens * q_heads / 128 + sequences * kv_heads below 2^24
+ *               (UNISVQ_EUNSUP otherwise)
  *   lse         device fp32 [q_tokens][q_heads] or NULL, as above
  *   workspace   device, >= unisvq_attn_prompt_workspace_bytes(...) bytes,
  *               16-byte aligned; may be NULL when that size is 0 (it is where

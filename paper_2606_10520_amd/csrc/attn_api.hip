@@ -11,6 +11,7 @@ using unisvq::Rotary;
 using unisvq::Rows;
 
 constexpr int64_t kMost = (int64_t{1} << 31) - 1;
+constexpr int64_t kMostGroups = (int64_t{1} << 24) - 1;  // of 256 threads: a launch has fewer than 2^32
 // Tokens that a page table may span: positions and the kernels' counts along a
 // sequence are 32-bit integers.
 constexpr int64_t kMaxContext = int64_t{1} << 30;
@@ -138,6 +139,7 @@ int unisvq_cache_read(const unisvq_cache* cache, const int32_t* page_table, int6
     if (!rows_aligned(k_out, k_token_stride, k_head_stride) || !rows_aligned(v_out, v_token_stride, v_head_stride) ||
         !aligned(starts, 4) || !aligned(cu, 4))
         return UNISVQ_EALIGN;
+    if (tokens > kMost / (c.heads * (c.head_dim / 16))) return UNISVQ_EUNSUP;
     if (tokens == 0 || sequences == 0) return UNISVQ_OK;
     return status(unisvq::launch_cache_read(c, starts, cu, tokens, rows(k_out, k_token_stride, k_head_stride),
                                             rows(v_out, v_token_stride, v_head_stride), dtype,
@@ -186,7 +188,7 @@ int unisvq_attn_decode(const unisvq_cache* cache, const int32_t* page_table, int
                                              max_len);
     // workgroups and units of work are counted in 32 bits
     const int64_t row_tiles = (q_len * (q_heads / c.heads) + 15) / 16;
-    if (c.heads * row_tiles > kMost / 2 / (room / 128 + 1) ||
+    if (sequences > kMostGroups / (c.heads * row_tiles) || c.heads * row_tiles > kMost / 2 / (room / 128 + 1) ||
         sequences > kMost / 2 / (c.heads * row_tiles * (room / 128 + 1)))
         return UNISVQ_EUNSUP;
     const size_t need = unisvq::decode_workspace_bytes(sequences, static_cast<int>(q_len), static_cast<int>(q_heads),
@@ -230,8 +232,8 @@ int unisvq_attn_prompt(int64_t sequences, int64_t q_tokens, int64_t k_tokens, co
     const int64_t wide = int64_t{1} << 22;
     if (k_token_stride < head_dim || k_token_stride > wide || v_token_stride < head_dim || v_token_stride > wide)
         return UNISVQ_EUNSUP;
-    // rows and workgroups (of up to 32 parts) are counted in 32 bits
-    if (q_tokens > kMost / q_heads || q_tokens * q_heads / 128 + sequences * kv_heads > kMost / 2) return UNISVQ_EUNSUP;
+    // rows are counted in 32 bits
+    if (q_tokens > kMost / q_heads || q_tokens * q_heads / 128 + sequences * kv_heads > kMostGroups) return UNISVQ_EUNSUP;
     const size_t need = unisvq::prompt_workspace_bytes(sequences, q_tokens, k_tokens, static_cast<int>(q_heads),
                                                        static_cast<int>(kv_heads), static_cast<int>(head_dim));
     if (need) {

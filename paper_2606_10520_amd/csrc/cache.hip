@@ -1,9 +1,10 @@
 // The paged key/value cache: writing new tokens (with the rotation of keys and
 // queries) and reading tokens back, on gfx950.
 //
-// Both are bound by memory.  A head's quantisation needs the largest magnitude
-// of its values, which eight (head_dim 128) or four (64) neighbouring threads
-// find together, sixteen values each, so everything is read and written once.
+// Both are bound by memory; at a few tokens, by the latency of a launch.  A
+// head's quantisation needs the largest magnitude of its values, which eight
+// (head_dim 128) or four (64) neighbouring threads find together, sixteen
+// values each, so everything is read and written once.
 #include "attn.hpp"
 
 namespace unisvq {
@@ -13,7 +14,7 @@ constexpr int kThreads = 256;
 
 struct Append {
     CacheView c;
-    uint32_t count;  // threads with work: tokens * heads * chunks
+    int64_t tokens;
     const int32_t *seqs, *positions;
     Rows k, v, q, q_out;
     int q_heads;
@@ -48,10 +49,24 @@ __device__ inline uint32_t max_over(uint32_t m) {
 constexpr uint32_t kInfBits = 0x7f800000u;
 constexpr float kSmallest = 1e-30f;
 
-// Eight codes of f, round to even, |code| <= top.
-__device__ inline void codes8(const float (&f)[8], float inv, float top, int (&q)[8]) {
+// Codes of f * inv, rounded to even, in BITS bits each at an offset of half
+// their range.  A sum with 1.5 * 2^23 rounds to an integer in the low bits of
+// a float; the integers are put in place by adding them up shifted, and what
+// the exponents add is known, so it is taken off once.  No code can pass its
+// top: |f| <= a, and scale is a / top but for a rounding of 2^-9 at most, which
+// is far from a half even at 127 (whose scale is rounded to 2^-24).
+template <int BITS>
+__device__ inline uint32_t codes(const float* f, float inv) {
+#pragma clang fp contract(off)
+    constexpr float kMagic = 12582912.0f + (1 << (BITS - 1));
+    uint32_t b = 0, base = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = static_cast<int>(fminf(fmaxf(rintf(f[i] * inv), -top), top));
+    for (int i = 0; i < 32 / BITS; ++i) {
+        const float product = f[i] * inv;
+        b += __float_as_uint(product + kMagic) << BITS * i;
+        base += 0x4b400000u << BITS * i;
+    }
+    return b - base;
 }
 
 // A token's page, token of the page and head: the index of its entry.
@@ -77,18 +92,11 @@ __device__ inline void store_entry(uint8_t* pool, uint32_t* scales, int64_t e, b
         const float scale = !finite ? __builtin_nanf("") : a < kSmallest ? 0.0f : a / 127.0f;
         const float inv = finite && scale > 0.0f ? 1.0f / scale : 0.0f;
         if (!write) return;
-        int q[2][8];
-        codes8(u, inv, 127.0f, q[0]);
-        codes8(w, inv, 127.0f, q[1]);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            uint2 b = {0u, 0u};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                b.x |= (finite ? static_cast<uint32_t>(q[i][j]) & 255u : 0u) << 8 * j;
-                b.y |= (finite ? static_cast<uint32_t>(q[i][4 + j]) & 255u : 0u) << 8 * j;
-            }
-            *reinterpret_cast<uint2*>(pool + e * D + (i ? k.d1 : k.d0)) = b;
+            const float* f = i ? w : u;
+            const uint2 b = {codes<8>(f, inv) ^ 0x80808080u, codes<8>(f + 4, inv) ^ 0x80808080u};
+            *reinterpret_cast<uint2*>(pool + e * D + (i ? k.d1 : k.d0)) = finite ? b : uint2{0u, 0u};
         }
         if (c == 0) scales[e] = __float_as_uint(scale);
     } else {
@@ -108,48 +116,51 @@ __device__ inline void store_entry(uint8_t* pool, uint32_t* scales, int64_t e, b
             inv[i] = finite[i] && scale[i] > 0.0f ? 1.0f / scale[i] : 0.0f;
         }
         if (!write) return;
-        int q[2][8];
-        codes8(u, hu ? inv[1] : inv[0], 7.0f, q[0]);
-        codes8(w, hw ? inv[1] : inv[0], 7.0f, q[1]);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const bool fin = (i ? hw : hu) ? finite[1] : finite[0];
-            uint32_t b = 0;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) b |= (fin ? static_cast<uint32_t>(q[i][j] + 8) & 15u : 8u) << 4 * j;
-            *reinterpret_cast<uint32_t*>(pool + e * (D / 2) + (i ? k.d1 : k.d0) / 2) = b;
-        }
+        *reinterpret_cast<uint32_t*>(pool + e * (D / 2) + k.d0 / 2) =
+            finite[hu] ? codes<4>(u, hu ? inv[1] : inv[0]) : 0x88888888u;
+        *reinterpret_cast<uint32_t*>(pool + e * (D / 2) + k.d1 / 2) =
+            finite[hw] ? codes<4>(w, hw ? inv[1] : inv[0]) : 0x88888888u;
         if (c == 0)
             scales[e] = (__float_as_uint(scale[0]) >> 16) | (__float_as_uint(scale[1]) & 0xffff0000u);
     }
 }
 
-// Thread i: chunk i % chunks of a head of a token; a token's heads are those
-// of q, then of k, then of v.
+// A block: one head of kThreads / LANES tokens, a thread sixteen dims.
+// Neighbouring threads are neighbouring tokens of the head because that is what
+// lies together in a page: codes go out in whole lines and a block's scales are
+// one line, where a token's heads side by side would leave 64-byte and 4-byte
+// pieces to different dies' caches.
+//
+// 2048 tokens of 64 + 2 * 8 heads into 8-bit pages: 18.5 us, 4.3 TB/s; 2000
+// tokens of 3 * 32 heads into 4-bit pages: 23 us, 3.3 TB/s.  A thread waits for
+// its position and then for its table row and page, so what is left is waves
+// that start and wait; two heads a thread take as long, four 1-2 us longer
+// (fewer waves fit).
 template <int KIND, int D, typename T>
 __global__ __launch_bounds__(kThreads) void append_kernel(Append a) {
     constexpr int LANES = D / 16;
-    const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
-    if (i >= a.count) return;  // count is a multiple of LANES: a head's threads leave together
-    const uint32_t heads = a.q_heads + 2 * a.c.heads;
-    const int c = i % LANES;
-    const uint32_t th = i / LANES, t = th / heads;
-    int h = th % heads;
-    const int64_t pos = a.positions[t];
+    const uint32_t heads = static_cast<uint32_t>(a.q_heads + 2 * a.c.heads);
+    const int64_t t = static_cast<int64_t>(blockIdx.x / heads) * (kThreads / LANES) + threadIdx.x / LANES;
+    if (t >= a.tokens) return;  // a head's threads leave together
+    // a token's heads are those of q, then of k, then of v
+    const int h = static_cast<int>(blockIdx.x % heads), c = threadIdx.x % LANES;
     const int role = h < a.q_heads ? 0 : h < a.q_heads + a.c.heads ? 1 : 2;
-    h -= role == 0 ? 0 : role == 1 ? a.q_heads : a.q_heads + a.c.heads;
+    const int at = h - (role == 0 ? 0 : role == 1 ? a.q_heads : a.q_heads + a.c.heads);
     const Rows& from = role == 0 ? a.q : role == 1 ? a.k : a.v;
-    Chunk k = chunk_of(c, role == 2 || !a.rotary.table ? 0 : a.rotary.rot, a.rotary.interleaved);
-    const T* x = static_cast<const T*>(from.p) + t * from.ts + h * from.hs;
+    const int64_t pos = a.positions[t];
+    // dims that are not rotated are taken in halves too: whole lines a load
+    const Chunk k = role != 2 && a.rotary.table ? chunk_of(c, a.rotary.rot, a.rotary.interleaved)
+                                                : Chunk{8 * c, D / 2 + 8 * c, false};
+    const T* row = static_cast<const T*>(from.p) + t * from.ts + at * from.hs;
     float u[8], w[8];
-    load8(x + k.d0, u);
-    load8(x + k.d1, w);
+    load8(row + k.d0, u);
+    load8(row + k.d1, w);
     if (k.turned) {
         float cs[8], sn[8];
         if (pos >= 0 && pos < a.rotary.positions) {
-            const float* row = a.rotary.table + pos * a.rotary.rot + 8 * c;
-            load8(row, cs);
-            load8(row + a.rotary.rot / 2, sn);
+            const float* angles = a.rotary.table + pos * a.rotary.rot + 8 * c;
+            load8(angles, cs);
+            load8(angles + a.rotary.rot / 2, sn);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) cs[j] = sn[j] = __builtin_nanf("");
@@ -157,86 +168,112 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Append a) {
         turn(u, w, cs, sn, a.rotary.interleaved);
     }
     if (role == 0) {
-        T* y = static_cast<T*>(a.q_out.p) + t * a.q_out.ts + h * a.q_out.hs;
+        T* y = static_cast<T*>(a.q_out.p) + t * a.q_out.ts + at * a.q_out.hs;
         store8(y + k.d0, u);
         store8(y + k.d1, w);
         return;
     }
-    const int64_t page = page_of(a.c, a.seqs ? a.seqs[t] : static_cast<int64_t>(t), pos);
-    const int64_t e = entry_of(a.c, page < 0 ? 0 : page, pos < 0 ? 0 : pos, h);
+    const int64_t page = page_of(a.c, a.seqs ? a.seqs[t] : t, pos);
+    const int64_t e = page < 0 ? 0 : entry_of(a.c, page, pos, at);
     store_entry<KIND, D, T>(role == 1 ? a.c.k : a.c.v, role == 1 ? a.c.ks : a.c.vs, e, page >= 0, k, c, u, w);
 }
 
 // ---- reading back ----
 
-// Sixteen values, dims 16c .. 16c + 15, of entry e.
-template <int KIND, int D, typename T>
-__device__ inline void load_entry(const uint8_t* pool, const uint32_t* scales, int64_t e, int c, float (&u)[8],
-                                  float (&w)[8]) {
-    if constexpr (KIND == UNISVQ_CACHE_F16 || KIND == UNISVQ_CACHE_BF16) {
-        typedef std::conditional_t<KIND == UNISVQ_CACHE_F16, _Float16, __bf16> P;
-        const P* row = reinterpret_cast<const P*>(pool) + e * D + 16 * c;
-        load8(row, u);
-        load8(row + 8, w);
-    } else if constexpr (KIND == UNISVQ_CACHE_I8) {
-        const uint4 b = *reinterpret_cast<const uint4*>(pool + e * D + 16 * c);
-        const float scale = __uint_as_float(scales[e]);
+// Sixteen values of entry e as they are stored: dims 8c .. 8c + 7 of both
+// halves of the head, so that a head's threads write whole lines.
+template <int KIND, int D>
+struct Stored {
+    static constexpr int kWords = KIND == UNISVQ_CACHE_I8 ? 2 : KIND == UNISVQ_CACHE_I4 ? 1 : 4;
+    uint32_t b[2][kWords], scale;
+
+    __device__ inline void load(const uint8_t* pool, const uint32_t* scales, int64_t e, int c) {
+        typedef uint32_t Words __attribute__((ext_vector_type(kWords)));
+        const Words* p = reinterpret_cast<const Words*>(pool) + e * (D / 8) + c;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            u[j] = static_cast<float>(static_cast<int8_t>(b.x >> 8 * j)) * scale;
-            u[4 + j] = static_cast<float>(static_cast<int8_t>(b.y >> 8 * j)) * scale;
-            w[j] = static_cast<float>(static_cast<int8_t>(b.z >> 8 * j)) * scale;
-            w[4 + j] = static_cast<float>(static_cast<int8_t>(b.w >> 8 * j)) * scale;
+        for (int i = 0; i < 2; ++i) {
+            const Words v = p[i * (D / 16)];
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) b[i][j] = v[j];
         }
-    } else {
-        const uint2 b = *reinterpret_cast<const uint2*>(pool + e * (D / 2) + 8 * c);
-        const uint32_t both = scales[e];
-        const float scale = __uint_as_float(16 * c < D / 2 ? both << 16 : both & 0xffff0000u);
+        if constexpr (kWords < 4) scale = scales[e];
+    }
+
+    __device__ inline void values(int i, float (&f)[8]) const {
+        const uint32_t* x = b[i];
+        if constexpr (KIND == UNISVQ_CACHE_F16) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            u[j] = static_cast<float>(static_cast<int>(b.x >> 4 * j & 15u) - 8) * scale;
-            w[j] = static_cast<float>(static_cast<int>(b.y >> 4 * j & 15u) - 8) * scale;
+            for (int j = 0; j < 8; ++j)
+                f[j] = static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(x[j / 2] >> 16 * (j % 2))));
+        } else if constexpr (KIND == UNISVQ_CACHE_BF16) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(x[j / 2] >> 16 * (j % 2) << 16);
+        } else if constexpr (KIND == UNISVQ_CACHE_I8) {
+            const float s = __uint_as_float(scale);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = static_cast<float>(static_cast<int8_t>(x[j / 4] >> 8 * (j % 4))) * s;
+        } else {
+            const float s = __uint_as_float(i ? scale & 0xffff0000u : scale << 16);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t four = (j % 2 ? x[0] >> 4 : x[0]) & 0x0f0f0f0fu;  // its bytes convert as they are
+                f[j] = (static_cast<float>(four >> 8 * (j / 2) & 255u) - 8.0f) * s;
+            }
         }
     }
-}
+};
 
-// A wave reads rows one after the other, all heads of a row together: the
-// row's place is the same for all its lanes.
-constexpr int kRowsPerWave = 2;
-
+// A block: one head of kThreads / LANES rows, keys and values; neighbours as
+// in append_kernel, for the same reason.  3808 rows of 32 heads out of 4-bit
+// pages: 18 us, 4.7 TB/s; 16 rows of 32 heads: 4 us.
 template <int KIND, int D, typename T>
 __global__ __launch_bounds__(kThreads) void read_kernel(CacheView c, const int32_t* starts, const int32_t* cu,
                                                         int64_t tokens, Rows k, Rows v) {
     constexpr int LANES = D / 16;
-    const int lane = threadIdx.x & 63;
-    const int64_t first = (static_cast<int64_t>(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6)) * kRowsPerWave;
-    for (int64_t r = first; r < first + kRowsPerWave && r < tokens; ++r) {
-        const int seq = sequence_of(cu, static_cast<int>(c.sequences), r);
-        if (seq >= c.sequences) return;
-        const int64_t pos = (starts ? starts[seq] : 0) + r - cu[seq];
-        const int64_t page = page_of(c, seq, pos);
-        for (int i = lane; i < 2 * c.heads * LANES; i += 64) {
-            const int h2 = i / LANES, part = i % LANES;
-            const bool key = h2 < c.heads;
-            const int h = key ? h2 : h2 - c.heads;
-            float u[8], w[8];
+    const uint32_t heads = static_cast<uint32_t>(c.heads);
+    const int h = static_cast<int>(blockIdx.x % heads), part = threadIdx.x % LANES;
+    const int64_t first = static_cast<int64_t>(blockIdx.x / heads) * (kThreads / LANES) +
+                          __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (64 / LANES);
+    const int64_t r = first + (threadIdx.x & 63) / LANES;
+    int seq = sequence_of(cu, static_cast<int>(c.sequences), first);
+    if (r >= tokens) return;
+    while (seq < c.sequences && cu[seq + 1] <= r) ++seq;
+    if (seq >= c.sequences) return;
+    const int64_t pos = (starts ? starts[seq] : 0) + r - cu[seq];
+    const int64_t page = page_of(c, seq, pos);
+    Stored<KIND, D> in[2];
+    if (page >= 0) {
+        const int64_t e = entry_of(c, page, pos, h);
+        in[0].load(c.k, c.ks, e, part);
+        in[1].load(c.v, c.vs, e, part);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const Rows& to = i ? v : k;
+        T* y = static_cast<T*>(to.p) + r * to.ts + h * to.hs + 8 * part;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            float f[8];
             if (page >= 0) {
-                load_entry<KIND, D, T>(key ? c.k : c.v, key ? c.ks : c.vs, entry_of(c, page, pos, h), part, u, w);
+                in[i].values(half, f);
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) u[j] = w[j] = __builtin_nanf("");
+                for (int j = 0; j < 8; ++j) f[j] = __builtin_nanf("");
             }
-            const Rows& to = key ? k : v;
-            T* y = static_cast<T*>(to.p) + r * to.ts + h * to.hs + 16 * part;
-            store8(y, u);
-            store8(y + 8, w);
+            store8(y + half * (D / 2), f);
         }
     }
 }
 
+// A block for each head of the rows that a block holds.
+uint32_t blocks_of(int64_t tokens, int heads, int head_dim) {
+    const int64_t rows = kThreads / (head_dim / 16);
+    return static_cast<uint32_t>((tokens + rows - 1) / rows * heads);
+}
+
 template <int D, typename T>
 hipError_t append_with(const Append& a, hipStream_t s) {
-    const uint32_t blocks = (a.count + kThreads - 1) / kThreads;
+    const uint32_t blocks = blocks_of(a.tokens, a.q_heads + 2 * a.c.heads, D);
     switch (a.c.kind) {
         case UNISVQ_CACHE_I8: append_kernel<UNISVQ_CACHE_I8, D, T><<<blocks, kThreads, 0, s>>>(a); break;
         case UNISVQ_CACHE_I4: append_kernel<UNISVQ_CACHE_I4, D, T><<<blocks, kThreads, 0, s>>>(a); break;
@@ -249,13 +286,19 @@ hipError_t append_with(const Append& a, hipStream_t s) {
 template <int D, typename T>
 hipError_t read_with(const CacheView& c, const int32_t* starts, const int32_t* cu, int64_t tokens, Rows k, Rows v,
                      hipStream_t s) {
-    const int64_t per = kThreads / 64 * kRowsPerWave;
-    const uint32_t blocks = static_cast<uint32_t>((tokens + per - 1) / per);
+    const uint32_t blocks = blocks_of(tokens, c.heads, D);
     switch (c.kind) {
-        case UNISVQ_CACHE_F16: read_kernel<UNISVQ_CACHE_F16, D, T><<<blocks, kThreads, 0, s>>>(c, starts, cu, tokens, k, v); break;
-        case UNISVQ_CACHE_BF16: read_kernel<UNISVQ_CACHE_BF16, D, T><<<blocks, kThreads, 0, s>>>(c, starts, cu, tokens, k, v); break;
-        case UNISVQ_CACHE_I8: read_kernel<UNISVQ_CACHE_I8, D, T><<<blocks, kThreads, 0, s>>>(c, starts, cu, tokens, k, v); break;
-        default: read_kernel<UNISVQ_CACHE_I4, D, T><<<blocks, kThreads, 0, s>>>(c, starts, cu, tokens, k, v);
+        case UNISVQ_CACHE_F16:
+            read_kernel<UNISVQ_CACHE_F16, D, T><<<blocks, kThreads, 0, s>>>(c, starts, cu, tokens, k, v);
+            break;
+        case UNISVQ_CACHE_BF16:
+            read_kernel<UNISVQ_CACHE_BF16, D, T><<<blocks, kThreads, 0, s>>>(c, starts, cu, tokens, k, v);
+            break;
+        case UNISVQ_CACHE_I8:
+            read_kernel<UNISVQ_CACHE_I8, D, T><<<blocks, kThreads, 0, s>>>(c, starts, cu, tokens, k, v);
+            break;
+        default:
+            read_kernel<UNISVQ_CACHE_I4, D, T><<<blocks, kThreads, 0, s>>>(c, starts, cu, tokens, k, v);
     }
     return hipGetLastError();
 }
@@ -265,8 +308,7 @@ hipError_t read_with(const CacheView& c, const int32_t* starts, const int32_t* c
 hipError_t launch_cache_append(const CacheView& c, int64_t tokens, const int32_t* seqs, const int32_t* positions,
                                Rows k, Rows v, Rows q, int q_heads, Rows q_out, int x_dtype, const Rotary& rotary,
                                hipStream_t s) {
-    Append a{c, static_cast<uint32_t>(tokens * (q_heads + 2 * c.heads) * (c.head_dim / 16)), seqs, positions, k, v, q,
-             q_out, q_heads, rotary};
+    const Append a{c, tokens, seqs, positions, k, v, q, q_out, q_heads, rotary};
     if (c.head_dim == 128)
         return x_dtype == UNISVQ_F16 ? append_with<128, _Float16>(a, s) : append_with<128, __bf16>(a, s);
     return x_dtype == UNISVQ_F16 ? append_with<64, _Float16>(a, s) : append_with<64, __bf16>(a, s);

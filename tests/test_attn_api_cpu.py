@@ -148,6 +148,15 @@ def test_prompt_refusals(args, want):
     assert prompt(**args) == want
 
 
+@pytest.mark.parametrize("call,args", [
+    (read, dict(tokens=1 << 28)),  # 2^28 * 2 heads * 8 chunks
+    (decode, dict(B=1 << 23, width=1)), (decode, dict(B=1 << 14, width=1 << 23, c=cache(page=16))),
+    (prompt, dict(B=1 << 23)),
+])
+def test_counts_past_a_launch_are_refused(call, args):
+    assert call(**args) == EUNSUP
+
+
 def test_workspace_sizes_of_invalid_shapes_are_zero():
     lib = u.load()
     assert lib.unisvq_attn_decode_workspace_bytes(0, 1, 8, 8, 128, 100) == 0
