@@ -2,10 +2,13 @@
 //
 //   s = scale (q . k),  p = exp(s - m),  out = sum p v / sum p
 //
-// Bound: the matrix cores (4 D operations a visible pair).  A workgroup of
-// four waves has 128 queries of one head, 32 a wave; keys and values come in
-// tiles of 64 through LDS, two tiles deep, loaded there directly.  The products
-// are 32x32x16 ones, arranged so that the scores never leave their lanes:
+// Bound: the matrix cores (4 D operations a visible pair), and under long
+// prompts the power that they draw.  A workgroup of four waves has 128 rows, 32
+// a wave; a row is a query of one of the heads that share a key head, so heads
+// that share keys share the tiles.  Keys and values come in tiles of 64 through
+// LDS, two tiles deep, loaded there directly; two workgroups fit a CU, and the
+// one's vector work runs under the other's products.  The products are 32x32x16
+// ones, arranged so that the scores never leave their lanes:
 //   S^T = K Q^T   (32 keys x 32 queries): lane (i, h) = (lane % 32, lane / 32)
 //                 ends with keys 8x + 4h .. + 3 of query i.
 //   O^T = V^T P^T (32 dims x 32 queries, 16 keys inner): P^T's operand wants
@@ -14,7 +17,25 @@
 //                 transposing read, four keys of one dim a lane.
 // So a query's maximum and sum need one exchange between the halves of a wave,
 // the maximum's only when a score exceeds it by 2^8 (the weights stay below
-// 2^8, so nothing overflows, and most tiles need no rescaling).
+// 2^8, so nothing overflows, and most tiles need no rescaling).  The weights
+// are rounded to the type of v, which is what the matrix cores multiply; their
+// sum is of the unrounded ones, in fp32.
+//
+// A tile's weights are followed by one run of 32 products, its values' and the
+// next tile's scores', with one barrier a tile; a wave in its products goes
+// before one in its vector work (16384 tokens of 32 heads 1.90 ms for 2.00; the
+// other way round 2.01).
+//
+// 16384 tokens of 32 heads of 128, causal: 1.90 ms, 1155 TFLOP/s, matrix cores
+// busy 71% of the cycles at a clock of 1.6 GHz (8192^3 library products under
+// the same power: 1280-1560 TFLOP/s at 86-90%).  2048 tokens: 54 us, of which
+// 4 us pass before the first products (512 workgroups ask for all of q at
+// once), 3-4 us with the first two tiles, and the rest with tiles of 1.1 us for a
+// workgroup alone on its CU, 0.93 us for each of two.  64 on 8 heads, 8 prompts
+// of 1 to 1500 tokens: 69 us.  Slower were: one wave a SIMD with three tiles
+// under way (8192 tokens 1270 us for 980: a lone wave issues at most one
+// instruction in four to five cycles), eight waves that take turns at products
+// and vector work, and sums of weights by dot products (2.09 ms for 2.00).
 #include <algorithm>
 #include <cfloat>
 
@@ -26,7 +47,7 @@ namespace {
 constexpr int kThreads = 256, kWaves = 4, kKeys = 64, kTileQ = 128;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kSlack = 8.0f;
-constexpr int64_t kResident = 512;  // workgroups that the GPU holds at once, two a CU
+constexpr int kCUs = 256, kResident = 2 * kCUs;  // workgroups that the GPU holds at once: two a CU
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -277,6 +298,14 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(Prompt g) {
     // keys first (of 64 at a time), and of a sequence the late tiles, which
     // see most.
     int tile = blockIdx.x / parts;
+    // Workgroups i and i + kCUs share a CU.  Where all are resident, those with
+    // most work have a CU to themselves or share it with those with least
+    // (2048 tokens of 32 heads 53.7 us for 55, 1536 tokens 36 for 37).
+    const int at_once = kCUs / parts, order = gridDim.x / parts;
+    if (gridDim.x > kCUs && gridDim.x <= kResident && kCUs % parts == 0) {
+        const int alone = 2 * at_once - order;
+        tile = tile >= at_once ? order - 1 - (tile - at_once) : tile + alone < at_once ? tile + alone : tile + alone - at_once;
+    }
     // the sequence of the tile: its tiles are its queries times the group's heads, 128 a tile
     int first = 0, q_first = 0, nq = 0, k_first = 0, nk = 0;
     for (int base = 0;; base += 64) {
@@ -418,9 +447,11 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(Prompt g) {
             issue(next_k(slot), off_k);
             issue(next_v(slot ^ 1), off_v);
             check_values(t, sv[slot]);
+            __builtin_amdgcn_s_setprio(1);
             w.values(sv[slot]);
             w.scores(sk[slot ^ 1], s);  // (after the last tile: zeros or what was there, and not used)
             schedule_products<D>();
+            __builtin_amdgcn_s_setprio(0);
         }
         wait_loads<0>();  // none may come to LDS after this
     }
