@@ -40,8 +40,8 @@
 // 2048 units a share is what 512 workgroups (two a CU) make of them, up to
 // 4096 four units, above that what 1024 workgroups make of them: a workgroup
 // costs about what two units do, and two rounds of them even out what CUs
-// differ by (16 x 8192 tokens of 8-bit cache, 8 heads: 1024 workgroups 62 us,
-// 2048 72 us; 16 ragged sequences up to 8192 tokens: 25 us, 43 us where each
+// differ by (16 x 8192 tokens of 8-bit cache, 8 heads: 1024 workgroups 60 us,
+// 2048 72 us; 16 ragged sequences up to 8192 tokens: 24 us, 43 us where each
 // sequence was cut into as many parts).  A share may begin and end within items: an item
 // within one share is finished there, others are joined by a second launch.
 // A workgroup's four waves take every fourth 32-token tile of its part of an
@@ -451,31 +451,36 @@ __device__ __forceinline__ void attend_item(const Decode& a, int b, int hr, int 
     const int i = lane & 15, g = lane >> 4;
     end = min(len, end * kUnit);
 
-    // the first tiles are on their way while the queries are made ready
-    const int32_t* row_pages = a.c.table + static_cast<int64_t>(b) * a.c.width;
-    TileRegs<KIND, D> r0, r1;
-    int pos = begin * kUnit + wave * kTile;
-    Pages pages = look_up(a, row_pages, pos, end);
-    if (pos < end) load_tile<KIND, D>(a, pages, h, pos, i, g, r0);
-    pages = look_up(a, row_pages, pos + kUnit, end);
-
     // the lane's query row: token j, head hq of the group
     const int rows = a.q_len * a.group;
     const int row = row0 + i;
     const bool live = row < rows;
     const int j = live ? row / a.group : 0, hq = h * a.group + (live ? row % a.group : 0);
     const int64_t token = static_cast<int64_t>(b) * a.q_len + j;
+    // the queries, then the first tile: loads return in their order, so the
+    // queries are made ready while the tile is on its way
+    const int32_t* row_pages = a.c.table + static_cast<int64_t>(b) * a.c.width;
+    int pos = begin * kUnit + wave * kTile;
+    Pages pages = look_up(a, row_pages, pos, end);
+    typename Vec8<XT>::type raw[D / 32];
+    {
+        const XT* x = static_cast<const XT*>(a.q.p) + token * a.q.ts + hq * a.q.hs;
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n)
+            raw[n] = *reinterpret_cast<const typename Vec8<XT>::type*>(x + query_dim<KIND, D>(n, g));
+    }
+    TileRegs<KIND, D> r0, r1;
+    if (pos < end) load_tile<KIND, D>(a, pages, h, pos, i, g, r0);
+    pages = look_up(a, row_pages, pos + kUnit, end);
+
     Running<KIND, D, CT> w;
     w.limit = live ? len - a.q_len + 1 + j : 0;
     w.qscale = a.scale;
 #pragma unroll
     for (int x = 0; x < HV; ++x) w.start[x] = 0.0f;
     {
-        const XT* x = static_cast<const XT*>(a.q.p) + token * a.q.ts + hq * a.q.hs;
-        typename Vec8<XT>::type raw[D / 32];
 #pragma unroll
         for (int n = 0; n < D / 32; ++n) {
-            raw[n] = *reinterpret_cast<const typename Vec8<XT>::type*>(x + query_dim<KIND, D>(n, g));
             if (!live)
 #pragma unroll
                 for (int y = 0; y < 8; ++y) raw[n][y] = static_cast<XT>(0.0f);
