@@ -36,19 +36,24 @@
 // Work.  An item is a sequence's rows on one key head (sixteen of them), in
 // units of 128 tokens.  The units of all items are dealt out evenly, so that a
 // ragged batch loads the GPU as evenly as one of equal lengths; the lengths are
-// on the device, so every workgroup finds its share by a scan over them.  Up to
-// 2048 units a share is what 512 workgroups (two a CU) make of them, up to
-// 4096 four units, above that what 1024 workgroups make of them: a workgroup
-// costs about what two units do, and two rounds of them even out what CUs
-// differ by (16 x 8192 tokens of 8-bit cache, 8 heads: 1024 workgroups 60 us,
-// 2048 72 us; 16 ragged sequences up to 8192 tokens: 24 us, 43 us where each
-// sequence was cut into as many parts).  A share may begin and end within items: an item
-// within one share is finished there, others are joined by a second launch.
+// on the device, so every workgroup finds its share by a scan over them.  There
+// are as many workgroups as the GPU holds at once, two a CU, since one costs
+// about what three units do before it has its first tile (16 x 8192 tokens of
+// 8-bit cache, 8 heads: 512 workgroups 54 us, 768 62 us, 1024 59 us; 16 ragged
+// sequences up to 8192 tokens: 24 us, 43 us where each was cut into as many
+// parts).  A share may begin and end within items: an item within one share is
+// finished there, others are joined by a second launch.
 // A workgroup's four waves take every fourth 32-token tile of its part of an
 // item, the next tile's loads under way while one is computed, each with its
-// own running maximum m, sum and outputs, joined through LDS.  m is raised only when a score exceeds
-// it by 2^8 (the weights then stay below 2^8, well inside f16), so most tiles
-// need no exchange between lanes and no rescaling.
+// own running maximum m, sum and outputs, joined through LDS.  m is raised only
+// when a score exceeds it by 2^8 (the weights then stay below 2^8, well inside
+// f16), so most tiles need no exchange between lanes and no rescaling.
+//
+// Measured, with the launch that joins: 4 x 32768 tokens of 4-bit cache, 32
+// heads, 122 us (4.7 TB/s); 4 x 16384 of 8-bit 94 us (5.9 TB/s); 4 x 8192 of
+// f16 87 us (6.2 TB/s); one sequence of 1001 tokens of f16 16 us, of which the
+// first launch takes 7 and the second 5: 1 us to find the share, 2.6 until the
+// queries and the first tile are there, 1.4 for a tile, 0.8 to join the waves.
 #include <algorithm>
 #include <cfloat>
 
@@ -59,8 +64,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = 4, kTile = 32, kRows = 16;
 constexpr int kUnit = kWaves * kTile;  // tokens
-constexpr int kResident = 512;         // workgroups that the GPU holds at once: two a CU
-constexpr int kGrid = 2 * kResident;   // workgroups at most
+constexpr int kGrid = 512;             // workgroups at most: what the GPU holds at once, two a CU
 constexpr int kSlots = 66;             // parts of a row at most, of which two are not whole shares
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kSlack = 8.0f;  // log2 of how far scores may exceed the running maximum
@@ -613,10 +617,8 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(Decode a) {
             most = max(most, __builtin_amdgcn_readlane(scan64_max(units), 63));
         }
         const int n = all * items;
-        const auto dealt = [n](int workgroups) { return (n + workgroups - 1) / workgroups; };
-        share = max(dealt(kGrid), min(4, dealt(kResident)));
-        // what the launch has workgroups and rows have slots for, whatever the lengths
-        share = max(max(share, dealt(gridDim.x)), (most + a.slots - 3) / (a.slots - 2));
+        // even shares, and rows have slots for their parts
+        share = max((n + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x), (most + a.slots - 3) / (a.slots - 2));
         if (blockIdx.x == 0 && wave == 0 && lane == 0) a.before[sequences] = all, a.before[sequences + 1] = share;
         if (static_cast<int64_t>(blockIdx.x) * share >= n) return;
         unit = blockIdx.x * share;
@@ -693,7 +695,7 @@ hipError_t run(const Decode& a, int64_t max_len, hipStream_t s) {
 int decode_slots(int64_t sequences, int q_len, int q_heads, int kv_heads, int64_t max_len) {
     if (max_len <= kUnit) return 1;
     const int items = kv_heads * row_tiles_of(q_len, q_heads, kv_heads);
-    return std::min(kSlots, decode_grid(sequences, items, max_len) / items + 2);
+    return std::min(kSlots, std::max(1, decode_grid(sequences, items, max_len) / items) + 2);
 }
 
 size_t decode_workspace_bytes(int64_t sequences, int q_len, int q_heads, int head_dim, int slots) {

@@ -141,6 +141,13 @@ def test_pages_that_are_missing(u, kind):
     assert not out.any() and torch.isneginf(lse).all()
 
 
+def test_more_heads_than_workgroups(u):
+    lens = [300, 1, 0, 129]
+    cache, pt, held = filled(u, "i8", lens, 16, 520, 64, 41)
+    q = torch.from_numpy(np.random.default_rng(42).standard_normal((4, 1, 520, 64))).half()
+    run_and_check(u, cache, pt, held, lens, q, "i8", "f16")
+
+
 def test_lengths_beyond_the_page_table_and_below_zero(u):
     cache, pt, held = filled(u, "i8", [64, 64], 16, 1, 128, seed=8)
     q = torch.randn((2, 1, 4, 128)).half()
