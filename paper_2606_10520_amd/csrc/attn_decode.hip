@@ -675,6 +675,7 @@ hipError_t run(const Decode& a, int64_t max_len, hipStream_t s) {
     j.part_ml = a.part_ml;
     j.rows = a.c.sequences * a.q_len * a.q_heads;
     j.slots = a.slots;
+    j.expected = static_cast<int>(blocks / (a.c.sequences * items));
     j.q_heads = a.q_heads;
     j.out = a.out;
     j.lse = a.lse;

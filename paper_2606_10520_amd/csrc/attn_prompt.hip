@@ -547,6 +547,7 @@ hipError_t run(const PromptArgs& a, void* workspace, hipStream_t s) {
     j.part_ml = g.part_ml;
     j.rows = rows;
     j.slots = g.splits;
+    j.expected = g.splits;
     j.q_heads = a.q_heads;
     j.out = a.out;
     j.lse = a.lse;
