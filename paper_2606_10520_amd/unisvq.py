@@ -895,10 +895,20 @@ def _words(t, count: int, what: str, dtype):
     return t.data_ptr()
 
 
-def _out_rows(out, like, tokens: int, heads: int, head_dim: int, what: str = "out"):
+def _new(shape, dtype, device, stream):
+    """A new tensor, the memory of the stream that is to write it: what that memory held before was used in the stream's
+    order."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _out_rows(out, like, tokens: int, heads: int, head_dim: int, stream, what: str = "out"):
     """The caller's out (checked) or a new tensor, and its rows."""
     if out is None:
-        out = like.new_empty((tokens, heads, head_dim))
+        out = _new((tokens, heads, head_dim), like.dtype, like.device, stream)
     return out, _rows(out, what, heads, head_dim, tokens, like.dtype)
 
 
@@ -908,14 +918,11 @@ def _workspace_size(name: str, *shape) -> int:
 
 
 def _scratch(workspace, need: int, like, stream):
-    """(tensor, pointer, bytes) of the caller's workspace or of a new one, which stays the stream's until its work there
-    is done."""
+    """(tensor, pointer, bytes) of the caller's workspace or of a new one of the stream's own memory."""
     if workspace is None:
         if not need:
             return None, None, 0
-        workspace = like.new_empty(need, dtype=_torch().uint8)
-        if stream is not None:
-            workspace.record_stream(stream)
+        workspace = _new(need, _torch().uint8, like.device, stream)
     else:
         workspace, need = _workspace(workspace, need, like)
     return workspace, workspace.data_ptr(), need
@@ -926,7 +933,7 @@ def rope_table(positions: int, rot: int, theta: float = 10000.0, factor: float =
     """Cosines and sines [positions][2][rot / 2] (fp32) of rotary positions; factor, low, high, original and magnitude
     stretch them over long contexts as unisvq_rope_table says."""
     torch = _torch()
-    table = torch.empty((positions, 2, rot // 2), dtype=torch.float32, device=device)
+    table = _new((positions, 2, rot // 2), torch.float32, device, stream)
     _check("unisvq_rope_table", load().unisvq_rope_table(positions, rot, theta, factor, low, high, original, magnitude,
                                                          _ptr(table), _stream(stream)))
     return table
@@ -946,7 +953,7 @@ def rope(x, positions, table, interleaved: bool = False, inverse: bool = False, 
     out may be x (in place) or a view with its own strides."""
     xr = _rows(x, "x")
     tokens, heads, head_dim = x.shape
-    out, yr = _out_rows(out, x, tokens, heads, head_dim)
+    out, yr = _out_rows(out, x, tokens, heads, head_dim, stream)
     tp, n, rot = _rope_rows(table)
     st = load().unisvq_rope(tokens, heads, head_dim, rot, interleaved, inverse, *xr,
                             _words(positions, tokens, "positions", _torch().int32), tp, n, *yr, _halves()[x.dtype],
@@ -1026,7 +1033,7 @@ def cache_append(cache, page_table, seqs, positions, k, v, q=None, rope_table=No
     if q is not None:
         qr = _rows(q, "q", None, head_dim, tokens, dt)
         q_heads = q.shape[1]
-        q_out, qor = _out_rows(q_out, q, tokens, q_heads, head_dim, "q_out")
+        q_out, qor = _out_rows(q_out, q, tokens, q_heads, head_dim, stream, "q_out")
     st = load().unisvq_cache_append(
         c, *_page_table(page_table), tokens, _words(seqs, tokens, "seqs", int32),
         _words(positions, tokens, "positions", int32), *kr, *vr, qr[0], q_heads, qr[1], qr[2], *qor, _halves()[dt],
@@ -1045,7 +1052,7 @@ def cache_read(cache, page_table, starts, cu, tokens: int, out=None, out_dtype=N
     pt = _page_table(page_table)
     if out is None:
         dt = out_dtype or (cache[0].dtype if cache[0].dtype.is_floating_point else torch.float16)
-        out = tuple(cache[0].new_empty((tokens, c.kv_heads, c.head_dim), dtype=dt) for _ in range(2))
+        out = tuple(_new((tokens, c.kv_heads, c.head_dim), dt, cache[0].device, stream) for _ in range(2))
     k, v = out
     kr = _rows(k, "out k", c.kv_heads, c.head_dim, tokens)
     vr = _rows(v, "out v", c.kv_heads, c.head_dim, tokens, k.dtype)
@@ -1078,7 +1085,7 @@ def attn_decode(q, cache, page_table, lens, scale: float | None = None, max_len:
     sequences, q_len, q_heads = shape[0], shape[1] if len(shape) == 4 else 1, shape[-2]
     tokens = sequences * q_len
     if out is None:
-        out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        out = _new(shape, q.dtype, q.device, stream)
     elif out.shape != shape:
         raise ValueError(f"out is {tuple(out.shape)}, q {tuple(shape)}")
     q3, out3 = (q, out) if len(shape) == 3 else (q.view(tokens, q_heads, shape[3]), out.view(tokens, q_heads, shape[3]))
@@ -1114,7 +1121,7 @@ def attn_prompt(q, k, v, cu_q, cu_k, causal: bool = True, scale: float | None = 
     kr = _rows(k, "k", None, head_dim, None, q.dtype)
     k_tokens, kv_heads = k.shape[0], k.shape[1]
     vr = _rows(v, "v", kv_heads, head_dim, k_tokens, q.dtype)
-    out, orr = _out_rows(out, q, tokens, q_heads, head_dim)
+    out, orr = _out_rows(out, q, tokens, q_heads, head_dim, stream)
     sequences = cu_q.numel() - 1
     need = _workspace_size("unisvq_attn_prompt_workspace_bytes", sequences, tokens, k_tokens, q_heads, kv_heads, head_dim)
     ws, wp, size = _scratch(workspace, need, q, stream)

@@ -39,3 +39,23 @@ def test_prompt_in_chunks_is_the_prompt_at_once(example):
         outs.append(torch.cat([block.prefill(p, [p.shape[0]]) for p in x.split(parts)]))
     err = (outs[0].float() - outs[1].float()).norm() / outs[0].float().norm()
     assert err <= 4e-3  # other kernels for other token counts: a few fp16 roundings apart
+
+
+def test_new_memory_is_the_streams_own():
+    """What a call makes for another stream must not be memory that the current stream may still be using."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2606_10520_amd.unisvq as u
+    x = torch.randn((1000, 8, 64), device="cuda").half()
+    pos = torch.arange(1000, dtype=torch.int32, device="cuda")
+    cu = torch.tensor([0, 1000], dtype=torch.int32, device="cuda")
+    s, table = torch.cuda.Stream(), u.rope_table(1000, 64)
+    torch.cuda.synchronize()
+    for call in (lambda: u.rope(x, pos, table, stream=s), lambda: u.attn_prompt(x, x, x, cu, cu, stream=s)):
+        freed = torch.empty_like(x)
+        at = freed.data_ptr()
+        del freed
+        assert torch.empty_like(x).data_ptr() == at  # the current stream would get it again
+        out = call()
+        assert out.data_ptr() != at
+        s.synchronize()
