@@ -703,7 +703,8 @@ int unisvq_cache_read(const unisvq_cache* cache, const int32_t* page_table, int6
  * Scores, softmax and sums are fp32; the products run on the matrix cores in
  * 16 bits (8- and 4-bit codes exactly, the weights of the values rounded to
  * f16, or to bf16 for a BF16 cache).  Long sequences are split over
- * workgroups and joined in a fixed order by a second launch. */
+ * workgroups and joined in a fixed order by a second launch; the workspace
+ * size is what any kind of cache needs for it. */
 size_t unisvq_attn_decode_workspace_bytes(int64_t sequences, int64_t q_len, int64_t q_heads, int64_t kv_heads,
                                           int64_t head_dim, int64_t max_len);
 int unisvq_attn_decode(const unisvq_cache* cache, const int32_t* page_table, int64_t sequences, int64_t table_width,

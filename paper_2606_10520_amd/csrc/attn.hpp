@@ -49,7 +49,7 @@ hipError_t launch_cache_read(const CacheView& c, const int32_t* starts, const in
                              Rows v, int dtype, hipStream_t s);
 
 // Attention over the cache.  slots: parts that a row's work can be split into.
-int decode_slots(int64_t sequences, int q_len, int q_heads, int kv_heads, int64_t max_len);
+int decode_slots(int64_t sequences, int q_len, int q_heads, int kv_heads, int64_t max_len, int token_bytes);
 size_t decode_workspace_bytes(int64_t sequences, int q_len, int q_heads, int head_dim, int slots);
 hipError_t launch_attn_decode(const CacheView& c, const int32_t* lens, int64_t max_len, int slots, int q_len, int q_heads,
                               Rows q, int x_dtype, float scale, Rows out, float* lse, void* workspace, hipStream_t s);

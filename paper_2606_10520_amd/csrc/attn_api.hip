@@ -159,8 +159,9 @@ bool decode_shape_ok(int64_t sequences, int64_t q_len, int64_t q_heads, int64_t 
 size_t unisvq_attn_decode_workspace_bytes(int64_t sequences, int64_t q_len, int64_t q_heads, int64_t kv_heads,
                                           int64_t head_dim, int64_t max_len) {
     if (!decode_shape_ok(sequences, q_len, q_heads, kv_heads, head_dim, max_len) || sequences == 0) return 0;
+    // for the 16-bit kinds, which are split first
     const int slots = unisvq::decode_slots(sequences, static_cast<int>(q_len), static_cast<int>(q_heads),
-                                             static_cast<int>(kv_heads), max_len);
+                                           static_cast<int>(kv_heads), max_len, static_cast<int>(4 * head_dim));
     return unisvq::decode_workspace_bytes(sequences, static_cast<int>(q_len), static_cast<int>(q_heads),
                                           static_cast<int>(head_dim), slots);
 }
@@ -185,7 +186,7 @@ int unisvq_attn_decode(const unisvq_cache* cache, const int32_t* page_table, int
         !aligned(lens, 4) || !aligned(lse, 4))
         return UNISVQ_EALIGN;
     const int slots = unisvq::decode_slots(sequences, static_cast<int>(q_len), static_cast<int>(q_heads), c.heads,
-                                             max_len);
+                                           max_len, c.head_dim * unisvq::entry_bits(c.kind) / 4);
     // workgroups and units of work are counted in 32 bits
     const int64_t row_tiles = (q_len * (q_heads / c.heads) + 15) / 16;
     if (sequences > kMostGroups / (c.heads * row_tiles) || c.heads * row_tiles > kMost / 2 / (room / 128 + 1) ||

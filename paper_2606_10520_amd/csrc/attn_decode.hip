@@ -42,7 +42,8 @@
 // 8-bit cache, 8 heads: 512 workgroups 54 us, 768 62 us, 1024 59 us; 16 ragged
 // sequences up to 8192 tokens: 24 us, 43 us where each was cut into as many
 // parts).  A share may begin and end within items: an item within one share is
-// finished there, others are joined by a second launch.
+// finished there, others are joined by a second launch.  Short sequences are
+// not split (form_of).
 // A workgroup's four waves take every fourth 32-token tile of its part of an
 // item, the next tile's loads under way while one is computed, each with its
 // own running maximum m, sum and outputs, joined through LDS.  m is raised only
@@ -51,9 +52,10 @@
 //
 // Measured, with the launch that joins: 4 x 32768 tokens of 4-bit cache, 32
 // heads, 122 us (4.7 TB/s); 4 x 16384 of 8-bit 94 us (5.9 TB/s); 4 x 8192 of
-// f16 87 us (6.2 TB/s); one sequence of 1001 tokens of f16 16 us, of which the
-// first launch takes 7 and the second 5: 1 us to find the share, 2.6 until the
-// queries and the first tile are there, 1.4 for a tile, 0.8 to join the waves.
+// f16 87 us (6.2 TB/s); one sequence of 1001 tokens of f16 10.5 us, of which
+// the first launch takes 7 and the second 4: 1 us to find the share, 2.6 until
+// the queries and the first tile are there, 1.4 for a tile, 0.8 to join the
+// waves; 512 tokens 8.8 us, one launch with whole items.
 #include <algorithm>
 #include <cfloat>
 
@@ -62,7 +64,7 @@
 namespace unisvq {
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4, kTile = 32, kRows = 16;
+constexpr int kWaves = 4, kTile = 32, kRows = 16;
 constexpr int kUnit = kWaves * kTile;  // tokens
 constexpr int kGrid = 512;             // workgroups at most: what the GPU holds at once, two a CU
 constexpr int kSlots = 66;             // parts of a row at most, of which two are not whole shares
@@ -446,11 +448,11 @@ __device__ inline int length_of(const Decode& a, int64_t b) {
 
 // Units begin .. end - 1 of item (b, hr), for sequences of length len.  `slot`:
 // of the part, or -1 where the item is all here.
-template <int KIND, int D, typename XT>
+template <int KIND, int D, typename XT, int WAVES>
 __device__ __forceinline__ void attend_item(const Decode& a, int b, int hr, int len, int begin, int end, int slot, int wave, int lane) {
     typedef Geometry<KIND, D> G;
     typedef std::conditional_t<G::scaled, _Float16, XT> CT;
-    constexpr int E = G::E, HV = G::halves, kPad = 4;
+    constexpr int E = G::E, HV = G::halves, kPad = 4, kStep = WAVES * kTile;
     const int h = hr / a.row_tiles, row0 = hr % a.row_tiles * kRows;
     const int i = lane & 15, g = lane >> 4;
     end = min(len, end * kUnit);
@@ -475,7 +477,7 @@ __device__ __forceinline__ void attend_item(const Decode& a, int b, int hr, int 
     }
     TileRegs<KIND, D> r0, r1;
     if (pos < end) load_tile<KIND, D>(a, pages, h, pos, i, g, r0);
-    pages = look_up(a, row_pages, pos + kUnit, end);
+    pages = look_up(a, row_pages, pos + kStep, end);
 
     Running<KIND, D, CT> w;
     w.limit = live ? len - a.q_len + 1 + j : 0;
@@ -534,22 +536,22 @@ __device__ __forceinline__ void attend_item(const Decode& a, int b, int hr, int 
     }
 
     while (pos < end) {
-        if (pos + kUnit < end) load_tile<KIND, D>(a, pages, h, pos + kUnit, i, g, r1);
-        pages = look_up(a, row_pages, pos + 2 * kUnit, end);
+        if (pos + kStep < end) load_tile<KIND, D>(a, pages, h, pos + kStep, i, g, r1);
+        pages = look_up(a, row_pages, pos + 2 * kStep, end);
         attend<KIND, D, CT>(a, r0, pos, len, g, w);
-        pos += kUnit;
+        pos += kStep;
         if (pos >= end) break;
-        if (pos + kUnit < end) load_tile<KIND, D>(a, pages, h, pos + kUnit, i, g, r0);
-        pages = look_up(a, row_pages, pos + 2 * kUnit, end);
+        if (pos + kStep < end) load_tile<KIND, D>(a, pages, h, pos + kStep, i, g, r0);
+        pages = look_up(a, row_pages, pos + 2 * kStep, end);
         attend<KIND, D, CT>(a, r1, pos, len, g, w);
-        pos += kUnit;
+        pos += kStep;
     }
 
     // join the waves: dim E (4g + n) + e of query i
     w.l += __shfl_xor(w.l, 16);
     w.l += __shfl_xor(w.l, 32);
-    __shared__ float so[kWaves][kRows][D + kPad];
-    __shared__ float sm[kWaves][kRows], sl[kWaves][kRows];
+    __shared__ float so[WAVES][kRows][D + kPad];
+    __shared__ float sm[WAVES][kRows], sl[WAVES][kRows];
     if (live) {
         const float unit = G::scaled ? exp2_(-w.unit_log) : 1.0f;  // of the weights
 #pragma unroll
@@ -570,11 +572,11 @@ __device__ __forceinline__ void attend_item(const Decode& a, int b, int hr, int 
     if (y >= kRows || row0 + y >= rows) return;
     float mt = sm[0][y], lt = 0.0f, f[8];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) mt = fmaxf(mt, sm[w][y]);
+    for (int w = 1; w < WAVES; ++w) mt = fmaxf(mt, sm[w][y]);
 #pragma unroll
     for (int n = 0; n < 8; ++n) f[n] = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         const float c = exp2_(sm[w][y] - mt);
         lt += c * sl[w][y];
 #pragma unroll
@@ -596,13 +598,14 @@ __device__ __forceinline__ void attend_item(const Decode& a, int b, int hr, int 
     }
 }
 
-template <int KIND, int D, typename XT>
-__global__ __launch_bounds__(kThreads, 2) void decode_kernel(Decode a) {
+// With eight waves, one a CU: whole items only.
+template <int KIND, int D, typename XT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void decode_kernel(Decode a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int items = a.c.heads * a.row_tiles, sequences = static_cast<int>(a.c.sequences);
     int first = 0, unit, last;  // units of the sequences before b, and those of this workgroup
     int b = 0, share;
-    if (a.slots == 1) {  // an item, whatever its length
+    if (WAVES > kWaves || a.slots == 1) {  // an item, whatever its length
         b = blockIdx.x / items;
         share = units_of(length_of(a, b));
         unit = blockIdx.x % items * share;
@@ -642,7 +645,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(Decode a) {
         const int hr = (unit - first * items) / n, item = first * items + hr * n;
         const int begin = unit - item, end = min(n, last - item);
         const Shares s = shares_of(item, n, share);
-        attend_item<KIND, D, XT>(a, b, hr, len, begin, end, s.count == 1 ? -1 : static_cast<int>(blockIdx.x) - s.first, wave, lane);
+        attend_item<KIND, D, XT, WAVES>(a, b, hr, len, begin, end, s.count == 1 ? -1 : static_cast<int>(blockIdx.x) - s.first, wave, lane);
         unit += end - begin;
         if (hr == items - 1 && end == n) first += n, ++b;
         __syncthreads();  // (LDS is used again)
@@ -657,17 +660,44 @@ int decode_grid(int64_t sequences, int items, int64_t max_len) {
 
 int row_tiles_of(int q_len, int q_heads, int kv_heads) { return (q_len * (q_heads / kv_heads) + kRows - 1) / kRows; }
 
+// How items are worked on.  A workgroup has a whole one, whatever its length,
+// where that takes less than joining parts costs (4 us on the GPU, and a
+// launch): where none has more than a unit; and where all workgroups are
+// resident and none has more than eight units, with eight waves each where
+// there is a CU for each.  Of these, few that have much to read take longer,
+// a CU reading 40 GB/s: items above 256 KB on half the CUs or fewer are split.
+// Calls, with the launches: 32 heads of f16, 512 tokens 10 us whole and 16
+// split, 1001 tokens 18 and 16; 8 heads of 8 bits, 1001 tokens 11 and 16, 2000
+// tokens 18 and 16; 32 heads of 8 bits, 8 sequences of 1001 tokens 15 and 20,
+// 16 of them 25 and 28, 16 ragged ones 15 and 22.
+enum Form { kSplit, kWhole, kWholeWide };
+Form form_of(int64_t sequences, int items, int64_t max_len, int token_bytes) {
+    const int64_t count = sequences * items;
+    if (max_len <= kUnit) return kWhole;
+    if (max_len > 8 * kUnit || count > kGrid) return kSplit;
+    if (count > kGrid / 2) return kWhole;
+    return count > kGrid / 4 || max_len * token_bytes <= 1 << 18 ? kWholeWide : kSplit;
+}
+
+template <int D, typename XT, int WAVES>
+void launch(const Decode& a, uint32_t blocks, hipStream_t s) {
+    constexpr int raw = std::is_same_v<XT, _Float16> ? UNISVQ_CACHE_F16 : UNISVQ_CACHE_BF16;
+    if (a.c.kind == UNISVQ_CACHE_I8)
+        decode_kernel<UNISVQ_CACHE_I8, D, XT, WAVES><<<blocks, 64 * WAVES, 0, s>>>(a);
+    else if (a.c.kind == UNISVQ_CACHE_I4)
+        decode_kernel<UNISVQ_CACHE_I4, D, XT, WAVES><<<blocks, 64 * WAVES, 0, s>>>(a);
+    else
+        decode_kernel<raw, D, XT, WAVES><<<blocks, 64 * WAVES, 0, s>>>(a);
+}
+
 template <int D, typename XT>
 hipError_t run(const Decode& a, int64_t max_len, hipStream_t s) {
     const int items = a.c.heads * a.row_tiles;
     const uint32_t blocks = a.slots == 1 ? static_cast<uint32_t>(a.c.sequences * items) : decode_grid(a.c.sequences, items, max_len);
-    constexpr int raw = std::is_same_v<XT, _Float16> ? UNISVQ_CACHE_F16 : UNISVQ_CACHE_BF16;
-    if (a.c.kind == UNISVQ_CACHE_I8)
-        decode_kernel<UNISVQ_CACHE_I8, D, XT><<<blocks, kThreads, 0, s>>>(a);
-    else if (a.c.kind == UNISVQ_CACHE_I4)
-        decode_kernel<UNISVQ_CACHE_I4, D, XT><<<blocks, kThreads, 0, s>>>(a);
+    if (form_of(a.c.sequences, items, max_len, D * entry_bits(a.c.kind) / 4) == kWholeWide)
+        launch<D, XT, 2 * kWaves>(a, blocks, s);
     else
-        decode_kernel<raw, D, XT><<<blocks, kThreads, 0, s>>>(a);
+        launch<D, XT, kWaves>(a, blocks, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.slots == 1) return e;
     Join j{};
@@ -691,11 +721,11 @@ hipError_t run(const Decode& a, int64_t max_len, hipStream_t s) {
 
 }  // namespace
 
-// Parts a row can have (a share is made large enough for it): one where no
-// sequence is to have more than a unit; then workgroups have whole items.
-int decode_slots(int64_t sequences, int q_len, int q_heads, int kv_heads, int64_t max_len) {
-    if (max_len <= kUnit) return 1;
+// Parts a row can have (a share is made large enough for it); one: workgroups
+// have whole items.
+int decode_slots(int64_t sequences, int q_len, int q_heads, int kv_heads, int64_t max_len, int token_bytes) {
     const int items = kv_heads * row_tiles_of(q_len, q_heads, kv_heads);
+    if (form_of(sequences, items, max_len, token_bytes) != kSplit) return 1;
     return std::min(kSlots, std::max(1, decode_grid(sequences, items, max_len) / items) + 2);
 }
 

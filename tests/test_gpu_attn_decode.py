@@ -148,6 +148,17 @@ def test_more_heads_than_workgroups(u):
     run_and_check(u, cache, pt, held, lens, q, "i8", "f16")
 
 
+@pytest.mark.parametrize("kind,D,H", [("i4", 64, 25), ("f16", 64, 25), ("f16", 128, 25), ("i8", 128, 50), ("f16", 64, 50),
+                                      ("i4", 64, 100), ("f16", 64, 100), ("i8", 64, 150), ("f16", 64, 150)])
+@pytest.mark.parametrize("longest,max_len", [(1024, 0), (1025, 0), (1000, 300), (129, 0)])
+def test_from_few_items_to_many(u, kind, D, H, longest, max_len):
+    """Whole items with four or eight wavefronts, and shares of them: both sides of what chooses between them."""
+    lens = [longest, 300 % longest, 0, 1]
+    cache, pt, held = filled(u, kind, lens, 32, H, D, 51)
+    q = torch.from_numpy(np.random.default_rng(52).standard_normal((4, 1, H, D))).half()
+    run_and_check(u, cache, pt, held, lens, q, kind, "f16", max_len=max_len)
+
+
 def test_lengths_beyond_the_page_table_and_below_zero(u):
     cache, pt, held = filled(u, "i8", [64, 64], 16, 1, 128, seed=8)
     q = torch.randn((2, 1, 4, 128)).half()
