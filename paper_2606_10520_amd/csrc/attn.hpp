@@ -96,12 +96,6 @@ __device__ inline void store8(T* p, const float (&f)[8]) {
     *reinterpret_cast<typename Vec8<T>::type*>(p) = v;
 }
 
-__device__ inline void load8(const float* p, float (&f)[8]) {
-    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = a[i], f[4 + i] = b[i];
-}
-
 // Eight pairs rotated; products and sums are rounded one by one (a contracted
 // product would differ from the plain formula in the last bit, and where the
 // result is quantised, in a code).
@@ -116,24 +110,34 @@ __device__ inline void rotate8(float (&a)[8], float (&b)[8], const float (&c)[8]
     }
 }
 
-// Sixteen dims of a head as one thread holds them: dims d0 + i and d1 + i, or
-// where the layout is interleaved (and for dims that are not rotated) the
-// sixteen from d0 on, split into even and odd ones by `turn`.
+// Sixteen dims of a head as one thread holds them: eight from d0 and eight from
+// d1 on, so that neighbouring threads have whole lines of either half of what is
+// rotated and of what is not.  Pairs are (d0 + i, d1 + i), or where the layout
+// is interleaved neighbours of either run, which `turn` takes apart.
 struct Chunk {
-    int d0, d1;   // first dims of the two runs of eight
+    int d0, d1;
     bool turned;  // whether they are rotated
 };
 
-__device__ inline Chunk chunk_of(int c, int rot, int interleaved) {
+__device__ inline Chunk chunk_of(int c, int rot, int head_dim) {
     Chunk k;
     k.turned = 16 * c < rot;
-    k.d0 = k.turned && !interleaved ? 8 * c : 16 * c;
-    k.d1 = k.turned && !interleaved ? rot / 2 + 8 * c : 16 * c + 8;
+    k.d0 = k.turned ? 8 * c : rot + 8 * (c - rot / 16);
+    k.d1 = k.d0 + (k.turned ? rot : head_dim - rot) / 2;
     return k;
 }
 
-// Rotates a chunk's dims (u from d0, w from d1) with cosines c and sines s of
-// pairs 8 * chunk .. 8 * chunk + 7.
+// Cosines and sines of the chunk's pairs from a table row.
+__device__ inline void load_angles(const float* row, int rot, int c, int interleaved, float (&cs)[8], float (&sn)[8]) {
+    const float* lo = row + (interleaved ? 4 * c : 8 * c);
+    const float* hi = row + (interleaved ? rot / 4 + 4 * c : 8 * c + 4);
+    const f32x4 v[4] = {*reinterpret_cast<const f32x4*>(lo), *reinterpret_cast<const f32x4*>(hi),
+                        *reinterpret_cast<const f32x4*>(lo + rot / 2), *reinterpret_cast<const f32x4*>(hi + rot / 2)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) cs[i] = v[0][i], cs[4 + i] = v[1][i], sn[i] = v[2][i], sn[4 + i] = v[3][i];
+}
+
+// Rotates a chunk's dims (u from d0, w from d1) with its cosines c and sines s.
 __device__ inline void turn(float (&u)[8], float (&w)[8], const float (&c)[8], const float (&s)[8], int interleaved) {
     if (!interleaved) {
         rotate8(u, w, c, s);

@@ -132,7 +132,7 @@ __device__ inline void store_entry(uint8_t* pool, uint32_t* scales, int64_t e, b
 // pieces to different dies' caches.
 //
 // 2048 tokens of 64 + 2 * 8 heads into 8-bit pages: 18.5 us, 4.3 TB/s; 2000
-// tokens of 3 * 32 heads into 4-bit pages: 23 us, 3.3 TB/s.  A thread waits for
+// tokens of 3 * 32 heads into 4-bit pages: 23 us, 3.2 TB/s.  A thread waits for
 // its position and then for its table row and page, so what is left is waves
 // that start and wait; two heads a thread take as long, four 1-2 us longer
 // (fewer waves fit).
@@ -148,9 +148,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Append a) {
     const int at = h - (role == 0 ? 0 : role == 1 ? a.q_heads : a.q_heads + a.c.heads);
     const Rows& from = role == 0 ? a.q : role == 1 ? a.k : a.v;
     const int64_t pos = a.positions[t];
-    // dims that are not rotated are taken in halves too: whole lines a load
-    const Chunk k = role != 2 && a.rotary.table ? chunk_of(c, a.rotary.rot, a.rotary.interleaved)
-                                                : Chunk{8 * c, D / 2 + 8 * c, false};
+    const Chunk k = chunk_of(c, role != 2 && a.rotary.table ? a.rotary.rot : 0, D);
     const T* row = static_cast<const T*>(from.p) + t * from.ts + at * from.hs;
     float u[8], w[8];
     load8(row + k.d0, u);
@@ -158,9 +156,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Append a) {
     if (k.turned) {
         float cs[8], sn[8];
         if (pos >= 0 && pos < a.rotary.positions) {
-            const float* angles = a.rotary.table + pos * a.rotary.rot + 8 * c;
-            load8(angles, cs);
-            load8(angles + a.rotary.rot / 2, sn);
+            load_angles(a.rotary.table + pos * a.rotary.rot, a.rotary.rot, c, a.rotary.interleaved, cs, sn);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) cs[j] = sn[j] = __builtin_nanf("");

@@ -49,14 +49,12 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(uint32_t count, int head
     const uint32_t groups = (heads + kHeads - 1) / kHeads;
     const uint32_t c = i % chunks, th = i / chunks, t = th / groups;
     const int h0 = static_cast<int>(th % groups) * kHeads;
-    const Chunk k = chunk_of(c, rotary.rot, rotary.interleaved);
+    const Chunk k = chunk_of(c, rotary.rot, 16 * chunks);
     float cs[8], sn[8];
     if (k.turned) {
         const int64_t p = positions[t];
         if (p >= 0 && p < rotary.positions) {
-            const float* row = rotary.table + p * rotary.rot + 8 * c;
-            load8(row, cs);
-            load8(row + rotary.rot / 2, sn);
+            load_angles(rotary.table + p * rotary.rot, rotary.rot, c, rotary.interleaved, cs, sn);
             if (rotary.inverse)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) sn[j] = -sn[j];
