@@ -32,7 +32,9 @@
 // 4 us pass before the first products (512 workgroups ask for all of q at
 // once), 3-4 us with the first two tiles, and the rest with tiles of 1.1 us for a
 // workgroup alone on its CU, 0.93 us for each of two.  64 on 8 heads, 8 prompts
-// of 1 to 1500 tokens: 69 us.  Slower were: one wave a SIMD with three tiles
+// of 1 to 1500 tokens: 70-73 us, three workgroups in turn on each place, and
+// for each 5 us before its first product and 4 from its last to the next one's
+// start.  Slower were: one wave a SIMD with three tiles
 // under way (8192 tokens 1270 us for 980: a lone wave issues at most one
 // instruction in four to five cycles), eight waves that take turns at products
 // and vector work, a tile's weights between the next tile's products (2.10 ms
@@ -268,11 +270,34 @@ struct Wave {
     }
 };
 
+// Division of n < 2^31 by d as a product and a shift: (mulhi(n, magic) + n) >>
+// shift with 2^shift >= d and magic = floor(2^32 (2^shift - d) / d) + 1.
+struct Divisor {
+    uint32_t magic, shift;
+};
+
+Divisor divisor(uint32_t d) {
+    uint32_t shift = 0;
+    while ((uint64_t{1} << shift) < d) ++shift;
+    return {static_cast<uint32_t>((((uint64_t{1} << shift) - d) << 32) / d + 1), shift};
+}
+
+__device__ inline int quotient(int n, Divisor d) {
+    return static_cast<int>((__umulhi(static_cast<uint32_t>(n), d.magic) + static_cast<uint32_t>(n)) >> d.shift);
+}
+
+// (Divisions are made ready on the host: they were 350 of 900 instructions
+// before the first product, 0.3 to 0.5 us of a workgroup's 5.)
 struct Prompt {
     PromptArgs a;
     float scale_log2;
     int group;        // query heads of a key head
     int splits;       // parts that a tile's keys are split into, a workgroup each
+    int parts;        // workgroups of a tile: key heads times splits
+    int spread;       // key heads of an XCD; 0: they do not go evenly
+    int at_once;      // tiles of the first kCUs workgroups ...
+    int order;        // ... and of all, where those that share a CU are paired, else 0
+    Divisor by_parts, by_group, by_heads;
     float* part;      // [query][head][splits][D] sums of the parts, where there are several
     float2* part_ml;  // and their maximum (log2) and sum
 };
@@ -291,22 +316,22 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(Prompt g) {
     const int i = lane & 31, hf = lane >> 5;
 
     // workgroups of a key head go to one XCD (they go round the eight)
-    const int parts = a.kv_heads * g.splits;
-    int kv = blockIdx.x % parts;
-    const int part = kv / a.kv_heads;
-    kv %= a.kv_heads;
-    if (a.kv_heads % 8 == 0) kv = kv % 8 * (a.kv_heads / 8) + kv / 8;
+    int tile = quotient(blockIdx.x, g.by_parts);
+    int kv = blockIdx.x - tile * g.parts, part = 0;
+    if (g.splits > 1) {
+        part = quotient(kv, g.by_heads);
+        kv -= part * a.kv_heads;
+    }
+    if (g.spread) kv = kv % 8 * g.spread + kv / 8;
     // Tiles go in the order of their work, most first: sequences with most
     // keys first (of 64 at a time), and of a sequence the late tiles, which
-    // see most.
-    int tile = blockIdx.x / parts;
-    // Workgroups i and i + kCUs share a CU.  Where all are resident, those with
-    // most work have a CU to themselves or share it with those with least
-    // (2048 tokens of 32 heads 53.7 us for 55, 1536 tokens 36 for 37).
-    const int at_once = kCUs / parts, order = gridDim.x / parts;
-    if (gridDim.x > kCUs && gridDim.x <= kResident && kCUs % parts == 0) {
-        const int alone = 2 * at_once - order;
-        tile = tile >= at_once ? order - 1 - (tile - at_once) : tile + alone < at_once ? tile + alone : tile + alone - at_once;
+    // see most.  Workgroups i and i + kCUs share a CU: where all are resident,
+    // those with most work have a CU to themselves or share it with those with
+    // least (2048 tokens of 32 heads 53.7 us for 55, 1536 tokens 36 for 37).
+    if (g.order) {
+        const int alone = 2 * g.at_once - g.order;
+        tile = tile >= g.at_once ? g.order - 1 - (tile - g.at_once)
+                                 : tile + alone < g.at_once ? tile + alone : tile + alone - g.at_once;
     }
     // the sequence of the tile: its tiles are its queries times the group's heads, 128 a tile
     int first = 0, q_first = 0, nq = 0, k_first = 0, nk = 0;
@@ -348,14 +373,14 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(Prompt g) {
     const int rows = nq * g.group, row0 = tile * kTileQ, wave_row = row0 + wave * kQ;
     const int row = min(wave_row + i, rows - 1);
     const bool live = wave_row + i < rows;
-    const int qi = row / g.group, head = kv * g.group + row - qi * g.group;
+    const int qi = quotient(max(row, 0), g.by_group), head = kv * g.group + row - qi * g.group;
 
     // the lane's row: keys below `limit` are seen
     const int more = nk - nq + 1;
     const int limit = !live ? 0 : a.causal ? qi + more : nk;
-    const int wave_low = a.causal ? wave_row / g.group + more : nk;  // seen by all its rows
-    const int block_low = a.causal ? row0 / g.group + more : nk;  // seen by all rows of the tile
-    const int keys = a.causal ? min(nk, (min(row0 + kTileQ, rows) - 1) / g.group + more) : nk;  // seen by any
+    const int wave_low = a.causal ? quotient(wave_row, g.by_group) + more : nk;  // seen by all its rows
+    const int block_low = a.causal ? quotient(row0, g.by_group) + more : nk;  // seen by all rows of the tile
+    const int keys = a.causal ? min(nk, quotient(min(row0 + kTileQ, rows) - 1, g.by_group) + more) : nk;  // seen by any
     Wave<D, T> w;
     w.hf = hf;
     w.at_k = i * D + (hf ^ turn_k<D>(i)) * 8;
@@ -378,8 +403,11 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(Prompt g) {
     // The part's tiles of keys: those before `plain` are seen whole by all the
     // workgroup's rows, before `whole` by the wave's.
     const int all_tiles = keys > 0 ? (keys + kKeys - 1) / kKeys : 0;
-    const int from = static_cast<int>(static_cast<int64_t>(all_tiles) * part / g.splits);
-    const int tiles = static_cast<int>(static_cast<int64_t>(all_tiles) * (part + 1) / g.splits) - from;
+    int from = 0, tiles = all_tiles;
+    if (g.splits > 1) {  // (at most 32, of at most 2^24 tiles)
+        from = all_tiles * part / g.splits;
+        tiles = all_tiles * (part + 1) / g.splits - from;
+    }
     const int plain = max(0, block_low) / kKeys - from;
     const int whole = max(0, wave_low) / kKeys - from;
     const int key0 = from * kKeys;
@@ -533,14 +561,26 @@ int prompt_splits(int64_t sequences, int64_t q_tokens, int64_t k_tokens, int q_h
 
 template <int D, typename T>
 hipError_t run(const PromptArgs& a, void* workspace, hipStream_t s) {
-    Prompt g{a, a.scale * kLog2e, a.q_heads / a.kv_heads, prompt_splits(a.sequences, a.q_tokens, a.k_tokens, a.q_heads, a.kv_heads, D),
-             nullptr, nullptr};
+    Prompt g{};
+    g.a = a;
+    g.scale_log2 = a.scale * kLog2e;
+    g.group = a.q_heads / a.kv_heads;
+    g.splits = prompt_splits(a.sequences, a.q_tokens, a.k_tokens, a.q_heads, a.kv_heads, D);
+    g.parts = a.kv_heads * g.splits;
+    g.spread = a.kv_heads % 8 == 0 ? a.kv_heads / 8 : 0;
+    g.by_parts = divisor(g.parts);
+    g.by_group = divisor(g.group);
+    g.by_heads = divisor(a.kv_heads);
+    const uint32_t blocks = static_cast<uint32_t>(prompt_blocks(a.sequences, a.q_tokens, a.q_heads, a.kv_heads) * g.splits);
+    if (blocks > kCUs && blocks <= kResident && kCUs % g.parts == 0) {
+        g.at_once = kCUs / g.parts;
+        g.order = static_cast<int>(blocks) / g.parts;
+    }
     const int64_t rows = a.q_tokens * a.q_heads;
     if (g.splits > 1) {
         g.part = static_cast<float*>(workspace);
         g.part_ml = reinterpret_cast<float2*>(g.part + rows * g.splits * D);
     }
-    const uint32_t blocks = static_cast<uint32_t>(prompt_blocks(a.sequences, a.q_tokens, a.q_heads, a.kv_heads) * g.splits);
     prompt_kernel<D, T><<<blocks, kThreads, 0, s>>>(g);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || g.splits == 1) return e;
