@@ -39,11 +39,14 @@
 // on the device, so every workgroup finds its share by a scan over them.  There
 // are as many workgroups as the GPU holds at once, two a CU, since one costs
 // about what three units do before it has its first tile (16 x 8192 tokens of
-// 8-bit cache, 8 heads: 512 workgroups 54 us, 768 62 us, 1024 59 us; 16 ragged
+// 8-bit cache, 8 heads: 512 workgroups 53 us, 768 62 us, 1024 59 us; 16 ragged
 // sequences up to 8192 tokens: 24 us, 43 us where each was cut into as many
-// parts).  A share may begin and end within items: an item within one share is
-// finished there, others are joined by a second launch.  Short sequences are
-// not split (form_of).
+// parts).  Where a share of up to two units more allows it, items are rounded up
+// to whole shares, so that no workgroup has parts of two, which costs it a start
+// more (the 16 ragged sequences 22 us for 24, 32 up to 4096 tokens 25 for 33;
+// batches of equal lengths lose 0.4 us to the search).  Else a share may begin
+// and end within items.  An item within one share is finished there, others are
+// joined by a second launch.  Short sequences are not split (form_of).
 // A workgroup's four waves take every fourth 32-token tile of its part of an
 // item, the next tile's loads under way while one is computed, each with its
 // own running maximum m, sum and outputs, joined through LDS.  m is raised only
@@ -78,7 +81,7 @@ struct Decode {
     float* lse;
     float* part;      // [rows][slots][D] sums, where slots > 1
     float2* part_ml;  // [rows][slots] maximum (log2) and sum
-    int32_t* before;  // [sequences + 1] units of an item of the sequences before, and the share after them
+    int32_t* before;  // [sequences + 1] (rounded) units of an item of the sequences before, and the share after them
     int slots;        // parts a row can have; 1: a workgroup has an item
     int q_len, q_heads, group, row_tiles;
     float scale;      // of the scores, times log2 e
@@ -441,6 +444,8 @@ __device__ __forceinline__ void attend(const Decode& a, TileRegs<KIND, D>& r, in
 // are to become zeros).
 __device__ inline int units_of(int len) { return max(1, (len + kUnit - 1) / kUnit); }
 
+__device__ inline int padded(int units, int pad) { return pad == 1 ? units : (units + pad - 1) / pad * pad; }
+
 __device__ inline int length_of(const Decode& a, int64_t b) {
     const int64_t room = a.c.width << a.c.page_shift;
     return static_cast<int>(min(static_cast<int64_t>(max(0, a.lens[b])), room));
@@ -604,30 +609,55 @@ __global__ __launch_bounds__(64 * WAVES, 2) void decode_kernel(Decode a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int items = a.c.heads * a.row_tiles, sequences = static_cast<int>(a.c.sequences);
     int first = 0, unit, last;  // units of the sequences before b, and those of this workgroup
-    int b = 0, share;
+    int b = 0, share, pad = 1;  // (units of items are rounded up to multiples of pad)
     if (WAVES > kWaves || a.slots == 1) {  // an item, whatever its length
         b = blockIdx.x / items;
         share = units_of(length_of(a, b));
         unit = blockIdx.x % items * share;
         last = unit + share;
     } else {
+        const int mine = lane < sequences ? units_of(length_of(a, lane)) : 0;
+        const auto units_at = [&](int base) {
+            return base == 0 ? mine : base + lane < sequences ? units_of(length_of(a, base + lane)) : 0;
+        };
         int all = 0, most = 0;
         for (int base = 0; base < sequences; base += 64) {
-            const int units = base + lane < sequences ? units_of(length_of(a, base + lane)) : 0;
-            const int sum = scan64(units);
-            if (blockIdx.x == 0 && wave == 0 && base + lane < sequences) a.before[base + lane] = all + sum - units;
-            all += __builtin_amdgcn_readlane(sum, 63);
+            const int units = units_at(base);
+            all += __builtin_amdgcn_readlane(scan64(units), 63);
             most = max(most, __builtin_amdgcn_readlane(scan64_max(units), 63));
         }
-        const int n = all * items;
         // even shares, and rows have slots for their parts
-        share = max((n + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x), (most + a.slots - 3) / (a.slots - 2));
-        if (blockIdx.x == 0 && wave == 0 && lane == 0) a.before[sequences] = all, a.before[sequences + 1] = share;
+        const int grid = gridDim.x;
+        share = max((all * items + grid - 1) / grid, (most + a.slots - 3) / (a.slots - 2));
+        if (sequences * items <= grid) {
+            bool found = false;
+            for (int s = share; s < share + 3 && !found; ++s) {
+                int parts = 0;
+                for (int base = 0; base < sequences; base += 64)
+                    parts += __builtin_amdgcn_readlane(scan64((units_at(base) + s - 1) / s), 63);
+                found = parts * items <= grid;
+                if (found) share = pad = s;
+            }
+        }
+        if (pad > 1) {
+            all = 0;
+            for (int base = 0; base < sequences; base += 64) all += __builtin_amdgcn_readlane(scan64(padded(units_at(base), pad)), 63);
+        }
+        if (blockIdx.x == 0 && wave == 0) {
+            int sum = 0;
+            for (int base = 0; base < sequences; base += 64) {
+                const int units = padded(units_at(base), pad), here = scan64(units);
+                if (base + lane < sequences) a.before[base + lane] = sum + here - units;
+                sum += __builtin_amdgcn_readlane(here, 63);
+            }
+            if (lane == 0) a.before[sequences] = all, a.before[sequences + 1] = share;
+        }
+        const int n = all * items;
         if (static_cast<int64_t>(blockIdx.x) * share >= n) return;
         unit = blockIdx.x * share;
         last = min(unit + share, n);
         for (int base = 0;; base += 64) {
-            const int units = base + lane < sequences ? units_of(length_of(a, base + lane)) : 0;
+            const int units = padded(units_at(base), pad);
             const int sum = scan64(units);
             const uint64_t in = __ballot(unit < (first + sum) * items);
             if (in) {
@@ -641,7 +671,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void decode_kernel(Decode a) {
     }
     while (unit < last) {
         const int64_t room = a.c.width << a.c.page_shift;
-        const int len = static_cast<int>(min(static_cast<int64_t>(max(0, load_uniform(a.lens + b))), room)), n = units_of(len);
+        const int len = static_cast<int>(min(static_cast<int64_t>(max(0, load_uniform(a.lens + b))), room));
+        const int n = padded(units_of(len), pad);
         const int hr = (unit - first * items) / n, item = first * items + hr * n;
         const int begin = unit - item, end = min(n, last - item);
         const Shares s = shares_of(item, n, share);

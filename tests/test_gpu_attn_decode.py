@@ -159,6 +159,17 @@ def test_from_few_items_to_many(u, kind, D, H, longest, max_len):
     run_and_check(u, cache, pt, held, lens, q, kind, "f16", max_len=max_len)
 
 
+@pytest.mark.parametrize("H,lens", [
+    (8, [7000, 2300, 1, 4097]),  # rounded up to whole shares
+    (8, [31 * i % 2000 for i in range(60)]),  # too many items for that
+    (3, [130] * 70 + [9000, 0]),  # more sequences than a wavefront has lanes, some as long as many
+])
+def test_ragged_batches(u, H, lens):
+    cache, pt, held = filled(u, "i8", lens, 64, H, 64, 61)
+    q = torch.from_numpy(np.random.default_rng(62).standard_normal((len(lens), 1, 2 * H, 64))).half()
+    run_and_check(u, cache, pt, held, lens, q, "i8", "f16")
+
+
 def test_lengths_beyond_the_page_table_and_below_zero(u):
     cache, pt, held = filled(u, "i8", [64, 64], 16, 1, 128, seed=8)
     q = torch.randn((2, 1, 4, 128)).half()
