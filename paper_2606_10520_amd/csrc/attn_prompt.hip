@@ -90,10 +90,28 @@ struct TileLoad {
           to(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(
               reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)(lds + wave * 64 * 8))))) {}
 
-    // Its n-th load.  (The compiler would wait for a load that it knows of
-    // before any read of LDS that might be of its place.)
-    __device__ __forceinline__ void issue(int n, uint32_t off) const {
-        asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + n * kThreads * 16), "v"(off), "s"(r));
+    // (In asm, as the compiler would wait for a load that it knows of before any
+    // read of LDS that might be of its place.)  What the compiler does elsewhere
+    // has to be done here: a load that goes to LDS by M0 comes a wait state after
+    // the write of M0, and one that reads scalar registers five after vector
+    // instructions that wrote them.
+    template <int LOADS>
+    __device__ __forceinline__ void issue(const uint32_t (&off)[LOADS]) const {
+        static_assert(LOADS == 2 || LOADS == 4, "");
+        if constexpr (LOADS == 4)
+            asm volatile(
+                "s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
+                "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %5, 0 offen lds\n\t"
+                "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %5, 0 offen lds\n\t"
+                "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %5, 0 offen lds" ::"s"(to),
+                "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(r), "n"(kThreads * 16)
+                : "scc");
+        else
+            asm volatile(
+                "s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %3, 0 offen lds\n\t"
+                "s_add_u32 m0, m0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds" ::"s"(to),
+                "v"(off[0]), "v"(off[1]), "s"(r), "n"(kThreads * 16)
+                : "scc");
     }
 };
 
@@ -450,16 +468,12 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(Prompt g) {
             local_phase();
         }
     };
-    const auto issue = [&](const TileLoad<D, T>& l, const uint32_t (&off)[kLoads]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int n = 0; n < kLoads; ++n) l.issue(n, off[n]);
-    };
     // Tile t's weights; then its values and the next tile's scores in one run
     // of products, with the loads of the tiles after them: one barrier a tile.
     if (tiles > 0) {
-        issue(next_k(0), off_k);
-        issue(next_v(0), off_v);
-        issue(next_k(1), off_k);
+        next_k(0).issue(off_k);
+        next_v(0).issue(off_v);
+        next_k(1).issue(off_k);
         wait_loads<0>();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         // (the queries too: the compiler would go on waiting for them in the loop)
@@ -474,8 +488,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(Prompt g) {
             w.weights(s);
             wait_loads<0>();
             phase();  // keys t + 1 and values t are there; keys t and values t - 1 are done with
-            issue(next_k(slot), off_k);
-            issue(next_v(slot ^ 1), off_v);
+            next_k(slot).issue(off_k);
+            next_v(slot ^ 1).issue(off_v);
             check_values(t, sv[slot]);
             __builtin_amdgcn_s_setprio(1);
             w.values(sv[slot]);
