@@ -701,8 +701,14 @@ int unisvq_cache_read(const unisvq_cache* cache, const int32_t* page_table, int6
  *              16-byte aligned (UNISVQ_EWORKSPACE / UNISVQ_EALIGN); may be
  *              NULL when that size is 0.  Overwritten.
  * Scores, softmax and sums are fp32; the products run on the matrix cores in
- * 16 bits (8- and 4-bit codes exactly, the weights of the values rounded to
- * f16, or to bf16 for a BF16 cache).  Long sequences are split over
+ * 16 bits: 8- and 4-bit codes exactly, the weights of the values rounded to
+ * f16, or to bf16 for a BF16 cache.  Over codes it is a weight times the
+ * token's scale that is rounded to f16, in a unit set by the largest such
+ * product among the tokens that the row sees (for I4, of that half of the
+ * head): products of 2^-18 of the largest and more are rounded to 11 bits, those
+ * below 2^-29 vanish (in the half of an I4 head whose products are the smaller
+ * ones 2^-12 and 2^-23).  Scales are not negative; where they differ by more
+ * than 2^90 between tokens the smaller ones' bits may be lost.  Long sequences are split over
  * workgroups and joined in a fixed order by a second launch; the workspace
  * size is what any kind of cache needs for it. */
 size_t unisvq_attn_decode_workspace_bytes(int64_t sequences, int64_t q_len, int64_t q_heads, int64_t kv_heads,

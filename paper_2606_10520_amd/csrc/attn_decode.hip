@@ -73,6 +73,11 @@ constexpr int kGrid = 512;             // workgroups at most: what the GPU holds
 constexpr int kSlots = 66;             // parts of a row at most, of which two are not whole shares
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kSlack = 8.0f;  // log2 of how far scores may exceed the running maximum
+// For codes (see Running): a bound of the sum of a tile's 32 operands, so that
+// none passes f16's range and one of at least 2^10 is there where it is passed;
+// and (log2) where the largest one starts, how far apart halves may share a unit,
+// bounds of units.
+constexpr float kMostSum = 0x1p15f, kAim = 4.0f, kApart = 6.0f, kMostUnit = 95.0f, kLeastShift = -60.0f;
 
 struct Decode {
     CacheView c;
@@ -294,36 +299,128 @@ __device__ inline float scale_of(uint32_t word, int h) {
     return __uint_as_float(word);
 }
 
-// The larger of two scale words (of both halves of them), and the largest of a
-// word as bits of fp32.  Scales are not negative, so they are ordered as their
-// bits are, with NaN above all.
-typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-template <int KIND>
-__device__ inline uint32_t larger(uint32_t a, uint32_t b) {
-    if constexpr (KIND == UNISVQ_CACHE_I4)
-        return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
-    return max(a, b);
-}
-template <int KIND>
-__device__ inline uint32_t largest_bits(uint32_t word) {
-    if constexpr (KIND == UNISVQ_CACHE_I4) return max(word << 16, word & 0xffff0000u);
-    return word;
+// A scale word times a factor each; what is finite stays finite.
+template <int KIND, int HV>
+__device__ inline uint32_t scaled_word(uint32_t word, const float (&factor)[2]) {
+    uint32_t half[HV];
+#pragma unroll
+    for (int x = 0; x < HV; ++x) {
+        const float was = scale_of<KIND>(word, x), is = was * factor[x];
+        half[x] = is == INFINITY && was < INFINITY ? 0x7f7f0000u : __float_as_uint(is);
+    }
+    if constexpr (KIND == UNISVQ_CACHE_I4) return half[0] >> 16 | (half[HV - 1] & 0xffff0000u);
+    return half[0];
 }
 
-// One wave's running result: weights are 2^(s - m + unit_log), sums l of them
-// and o of their products with the values' codes.
+// One wave's running result.  Weights are 2^(s - m + shift), l their sum.  o: the
+// sums of the values' codes times operands; for codes these are the weights
+// times the values' scales in f16, in a unit 2^u that is the half of the head's
+// own.  u follows from the row's own products weight * scale, whatever scales
+// there are and whatever the row does not see: the largest one starts at 2^kAim
+// and may grow to 2^10 and more.  A f16 has all its bits down to 2^-14 and some
+// down to 2^-25.  u is lowered where a tile's operands sum up to 2^15 (which the
+// product for the bias shows), and raised with m and as much, so that o stays.
+// The weights' shift is the lower u, which costs nothing; the other half has it
+// too while they are 2^kApart or less apart, else its scales are multiplied (as
+// all are below kLeastShift, where l would lose weights; kMostUnit keeps l in
+// range).  Beside units set by the largest scale met, which lost what a row
+// sees to a token of large scale and no weight, 8-bit caches take as long and
+// 4-bit ones 1 to 2.5% longer (16 x 8192 tokens 40.2 us for 39.1).
 template <int KIND, int D, typename CT>
 struct Running {
+    typedef Geometry<KIND, D> G;
     typedef typename Vec8<CT>::type C8;
-    static constexpr int E = D / 16, HV = Geometry<KIND, D>::halves;
+    static constexpr int E = D / 16, HV = G::halves;
     C8 q[D / 32];
     float start[HV];       // of the scores
     float qscale;          // of the scores to log2 units
     float m, l;
-    float unit_log;        // log2 of the unit that the values' scales are taken in
-    uint32_t most_bits;    // the largest scale that this unit takes (fp32 bits)
-    f32x4 o[HV][E], b[HV];  // b: sums of the weights times the bias
-    int limit;             // tokens below it are seen by the lane's row
+    float u[HV];           // units (log2, whole numbers) that the halves ask for
+    bool apart;            // whether scales of a lane are multiplied (the same in all lanes)
+    f32x4 o[HV][E];
+    float b[HV];           // sums of the operands times the bias
+    int seen;              // tokens below it are seen by the lane's row
+
+    __device__ __forceinline__ float least() const { return HV == 1 ? u[0] : fminf(u[0], u[HV - 1]); }
+    __device__ __forceinline__ float shift() const { return G::scaled ? fmaxf(least(), kLeastShift) : 0.0f; }
+    // The unit that half x of o has.
+    __device__ __forceinline__ float used(int x) const { return HV > 1 && u[x] - least() > kApart ? u[x] : least(); }
+
+    __device__ __forceinline__ void begin() {
+        m = -FLT_MAX;
+        l = 0.0f;
+        apart = false;
+#pragma unroll
+        for (int x = 0; x < HV; ++x) {
+            u[x] = kMostUnit;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[x][e] = f32x4{0, 0, 0, 0};
+            b[x] = 0.0f;
+        }
+    }
+
+    // Changes the units, where m has risen by `up`.
+    __device__ __forceinline__ void set_units(const float (&to)[HV], float up) {
+        float was[HV];
+        const float shift_was = shift();
+#pragma unroll
+        for (int x = 0; x < HV; ++x) was[x] = used(x);
+#pragma unroll
+        for (int x = 0; x < HV; ++x) u[x] = to[x];
+        l *= exp2_(shift() - shift_was - up);
+        bool far = false;
+#pragma unroll
+        for (int x = 0; x < HV; ++x) {
+            const float c = exp2_(used(x) - was[x] - up);
+            far = far || used(x) != shift();
+            b[x] *= c;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[x][e] *= c;
+        }
+        apart = __any(far);
+    }
+
+    // Raises the maximum (`top`: the lane's largest score of the tile) and finds
+    // new units, where an operand would be 2^10 or more and where the row has none.
+    __device__ __forceinline__ void renew(const float (&s)[2][4], float top, TileRegs<KIND, D>& r) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m2 = fmaxf(m, top), up = m2 - m;
+        if constexpr (G::scaled) {
+            float to[HV];
+#pragma unroll
+            for (int x = 0; x < HV; ++x) {
+                float largest = 0.0f;  // product, of those that are finite, times 2^-16
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) {
+                        const float p = exp2_(__builtin_fmaf(s[t][n], qscale, -m2)) * (scale_of<KIND>(r.vs[t][n], x) * 0x1p-16f);
+                        largest = fmaxf(largest, p < INFINITY ? p : 0.0f);
+                    }
+                largest = fmaxf(largest, __shfl_xor(largest, 16));
+                largest = fmaxf(largest, __shfl_xor(largest, 32));
+                const float log = static_cast<float>(static_cast<int>(__float_as_uint(largest) >> 23) - 127 + 16);
+                to[x] = fminf(u[x] + floorf(up), kMostUnit);
+                if (m == -FLT_MAX || log + to[x] >= 10.0f) to[x] = fminf(kAim - log, kMostUnit);
+            }
+            m = m2;
+            set_units(to, up);
+            if (apart) {
+                const float factor[2] = {exp2_(used(0) - shift()), exp2_(used(HV - 1) - shift())};
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) r.vs[t][n] = scaled_word<KIND, HV>(r.vs[t][n], factor);
+            }
+        } else {
+            const float c = exp2_(-up);
+            m = m2;
+            l *= c;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[0][e] *= c;
+        }
+    }
 };
 
 template <int KIND, int D, typename CT>
@@ -354,89 +451,61 @@ __device__ __forceinline__ void attend(const Decode& a, TileRegs<KIND, D>& r, in
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
                 const int p = pos + 16 * t + 4 * g + n;
-                if (!(p < w.limit && r.there[t])) s[t][n] = -INFINITY;
-                // what no row sees may hold anything
-                if (!(p < len && r.there[t])) {
-                    if constexpr (G::scaled) r.vs[t][n] = 0;
-                    else r.v[t][n] = {};
+                if (!(p < w.seen && r.there[t])) {
+                    s[t][n] = -INFINITY;
+                    if constexpr (G::scaled) r.vs[t][n] = 0;  // (the lane's copy, which serves its row alone)
                 }
+                // what no row sees may hold anything
+                if constexpr (!G::scaled)
+                    if (!(p < len && r.there[t])) r.v[t][n] = {};
             }
     }
     float top = s[0][0];
-    uint32_t vtop = 0;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            top = fmaxf(top, s[t][n]);
-            if constexpr (G::scaled) vtop = larger<KIND>(vtop, r.vs[t][n]);
-        }
+        for (int n = 0; n < 4; ++n) top = fmaxf(top, s[t][n]);
     top *= w.qscale;
-    if constexpr (G::scaled) vtop = largest_bits<KIND>(vtop);
-    const uint32_t vmost = vtop;  // the lane's
-    if (__any(top > w.m + kSlack || (G::scaled && vtop > w.most_bits))) {
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float m2 = fmaxf(w.m, top);
-        float c = exp2_(w.m - m2);
-        w.m = m2;
-        if constexpr (G::scaled) {
-            vtop = max(vtop, static_cast<uint32_t>(__shfl_xor(static_cast<int>(vtop), 16)));
-            vtop = max(vtop, static_cast<uint32_t>(__shfl_xor(static_cast<int>(vtop), 32)));
-            if (vtop > w.most_bits && vtop < 0x7f800000u) {
-                // the unit: the power of two below the largest scale; scales of up to 2^7 of it are taken
-                const int exponent = max(1, static_cast<int>(vtop >> 23));
-                const float unit = static_cast<float>(127 - exponent);
-                c *= exp2_(unit - w.unit_log);
-                w.unit_log = unit;
-                w.most_bits = static_cast<uint32_t>(min(exponent + 7, 254)) << 23;
+    C8 p[HV], values[E];
+    float sum;
+    f32x4 bias[HV];  // the operands' sum times the codes' bias, in all four
+#pragma nounroll
+    for (bool again = false;; again = true) {
+        const bool renew = again || (G::scaled && w.apart) || __any(top > w.m + kSlack);
+        if (renew) w.renew(s, top, r);
+        const float m = w.m - w.shift();
+        sum = 0.0f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const float v = exp2_(__builtin_fmaf(s[t][n], w.qscale, -m));
+                sum += v;
+#pragma unroll
+                for (int x = 0; x < HV; ++x)
+                    p[x][4 * t + n] = static_cast<CT>(G::scaled ? v * scale_of<KIND>(r.vs[t][n], x) : v);
             }
-        }
-        w.l *= c;
+        if constexpr (!G::scaled) break;
+        constexpr uint32_t word = G::bias | G::bias << 16;
+        bool over = false;
 #pragma unroll
         for (int x = 0; x < HV; ++x) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) w.o[x][e] *= c;
-            if constexpr (G::scaled) w.b[x] *= c;
+            bias[x] = mfma(__builtin_bit_cast(C8, u32x4{word, word, word, word}), p[x], f32x4{0, 0, 0, 0});
+            over = over || bias[x][0] > static_cast<float>(G::bias) * 0x1p-24f * kMostSum;
         }
+        value_operands<KIND, D>(r, values);
+        if (renew || !__any(over)) break;
     }
-    C8 p[HV];
-    const float m = w.m - w.unit_log;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            const float v = exp2_(__builtin_fmaf(s[t][n], w.qscale, -m));
-            w.l += v;
-#pragma unroll
-            for (int x = 0; x < HV; ++x)
-                p[x][4 * t + n] = static_cast<CT>(G::scaled ? v * scale_of<KIND>(r.vs[t][n], x) : v);
-        }
-    if constexpr (G::scaled) {
-        // rows that do not see a token have no part of a scale that is not finite
-        if (!full && __any(vmost >= 0x7f800000u))
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int n = 0; n < 4; ++n)
-                    if (s[t][n] == -INFINITY)
-#pragma unroll
-                        for (int x = 0; x < HV; ++x) p[x][4 * t + n] = static_cast<CT>(0.0f);
-    }
+    w.l += sum;
     if constexpr (!G::scaled) {  // codes are finite, and a scale that is not is the weight's matter
-        if (!full && a.q_len > 1) only_where_seen<KIND, D, CT>(r, pos, w.limit, g, w.o[0]);
+        if (!full && a.q_len > 1) only_where_seen<KIND, D, CT>(r, pos, w.seen, g, w.o[0]);
     }
-    C8 v[E];
-    value_operands<KIND, D>(r, v);
+    if constexpr (!G::scaled) value_operands<KIND, D>(r, values);
 #pragma unroll
-    for (int e = 0; e < E; ++e)
+    for (int x = 0; x < HV; ++x) {
+        if constexpr (G::scaled) w.b[x] += bias[x][0];
 #pragma unroll
-        for (int x = 0; x < HV; ++x) w.o[x][e] = mfma(v[e], p[x], w.o[x][e]);
-    if constexpr (G::scaled) {
-        constexpr uint32_t bias = G::bias | G::bias << 16;
-        const C8 ones = __builtin_bit_cast(C8, u32x4{bias, bias, bias, bias});
-#pragma unroll
-        for (int x = 0; x < HV; ++x) w.b[x] = mfma(ones, p[x], w.b[x]);
+        for (int e = 0; e < E; ++e) w.o[x][e] = mfma(values[e], p[x], w.o[x][e]);
     }
 }
 
@@ -485,7 +554,7 @@ __device__ __forceinline__ void attend_item(const Decode& a, int b, int hr, int 
     pages = look_up(a, row_pages, pos + kStep, end);
 
     Running<KIND, D, CT> w;
-    w.limit = live ? len - a.q_len + 1 + j : 0;
+    w.seen = live ? len - a.q_len + 1 + j : 0;
     w.qscale = a.scale;
 #pragma unroll
     for (int x = 0; x < HV; ++x) w.start[x] = 0.0f;
@@ -529,16 +598,7 @@ __device__ __forceinline__ void attend_item(const Decode& a, int b, int hr, int 
             w.qscale = ldexpf(w.qscale, -up) * G::unit;
         }
     }
-    w.m = -FLT_MAX;
-    w.l = 0.0f;
-    w.unit_log = 0.0f;
-    w.most_bits = 0;
-#pragma unroll
-    for (int x = 0; x < HV; ++x) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) w.o[x][e] = f32x4{0, 0, 0, 0};
-        w.b[x] = f32x4{0, 0, 0, 0};
-    }
+    w.begin();
 
     while (pos < end) {
         if (pos + kStep < end) load_tile<KIND, D>(a, pages, h, pos + kStep, i, g, r1);
@@ -558,19 +618,19 @@ __device__ __forceinline__ void attend_item(const Decode& a, int b, int hr, int 
     __shared__ float so[WAVES][kRows][D + kPad];
     __shared__ float sm[WAVES][kRows], sl[WAVES][kRows];
     if (live) {
-        const float unit = G::scaled ? exp2_(-w.unit_log) : 1.0f;  // of the weights
 #pragma unroll
         for (int n = 0; n < 4; ++n)
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 float v = HV == 2 && g >= 2 ? w.o[HV - 1][e][n] : w.o[0][e][n];
                 if constexpr (G::scaled) {
-                    const float bias = HV == 2 && g >= 2 ? w.b[HV - 1][n] : w.b[0][n];
-                    v = (v - bias) * G::unit * unit;
+                    const float bias = HV == 2 && g >= 2 ? w.b[HV - 1] : w.b[0];
+                    const float u = w.used(HV == 2 && g >= 2 ? HV - 1 : 0);
+                    v = (v - bias) * G::unit * exp2_(-u);
                 }
                 so[wave][i][E * (4 * g + n) + e] = v;
             }
-        if (g == 0) sm[wave][i] = w.m, sl[wave][i] = w.l * unit;
+        if (g == 0) sm[wave][i] = w.m, sl[wave][i] = w.l * exp2_(-w.shift());
     }
     __syncthreads();
     const int y = threadIdx.x / (D / 8), d = threadIdx.x % (D / 8) * 8;
