@@ -77,6 +77,7 @@ constexpr float kSlack = 8.0f;  // log2 of how far scores may exceed the running
 // none passes f16's range and one of at least 2^10 is there where it is passed;
 // and (log2) where the largest one starts, how far apart halves may share a unit,
 // bounds of units.
+constexpr int kLarge = 24;  // log2 of what scores of very large queries on codes are times besides
 constexpr float kMostSum = 0x1p15f, kAim = 4.0f, kApart = 6.0f, kMostUnit = 95.0f, kLeastShift = -60.0f;
 
 struct Decode {
@@ -337,6 +338,7 @@ struct Running {
     float m, l;
     float u[HV];           // units (log2, whole numbers) that the halves ask for
     bool apart;            // whether scales of a lane are multiplied (the same in all lanes)
+    bool large = false;    // whether scores are times 2^kLarge besides (the same in all lanes)
     f32x4 o[HV][E];
     float b[HV];           // sums of the operands times the bias
     int seen;              // tokens below it are seen by the lane's row
@@ -349,7 +351,7 @@ struct Running {
     __device__ __forceinline__ void begin() {
         m = -FLT_MAX;
         l = 0.0f;
-        apart = false;
+        apart = large;
 #pragma unroll
         for (int x = 0; x < HV; ++x) {
             u[x] = kMostUnit;
@@ -377,7 +379,7 @@ struct Running {
 #pragma unroll
             for (int e = 0; e < E; ++e) o[x][e] *= c;
         }
-        apart = __any(far);
+        apart = large || __any(far);
     }
 
     // Raises the maximum (`top`: the lane's largest score of the tile) and finds
@@ -472,7 +474,16 @@ __device__ __forceinline__ void attend(const Decode& a, TileRegs<KIND, D>& r, in
 #pragma nounroll
     for (bool again = false;; again = true) {
         const bool renew = again || (G::scaled && w.apart) || __any(top > w.m + kSlack);
-        if (renew) w.renew(s, top, r);
+        if (renew) {
+            if (G::scaled && w.large) {  // (then every tile comes here, and once)
+                top *= ldexpf(1.0f, kLarge);
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) s[t][n] *= ldexpf(1.0f, kLarge);
+            }
+            w.renew(s, top, r);
+        }
         const float m = w.m - w.shift();
         sum = 0.0f;
 #pragma unroll
@@ -579,7 +590,16 @@ __device__ __forceinline__ void attend_item(const Decode& a, int b, int hr, int 
             most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 16)));
             most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 32)));
             const int exponent = static_cast<int>(most >> 23) - 127;
-            const int up = most == 0 || exponent == 128 ? 0 : 14 - exponent;
+            int up = most == 0 || exponent == 128 ? 0 : 14 - exponent;
+            // The scores' factor is scale * unit * 2^-up.  Where it is past fp32's
+            // range for a row, scores take kLarge of it apart (see attend); where it
+            // would be subnormal, the queries are smaller instead (which costs
+            // nothing: what f16 loses of them is far below the scores' last bit).
+            constexpr int unit = KIND == UNISVQ_CACHE_I4 ? 18 : 24;
+            const int factor = (static_cast<int>(__float_as_uint(a.scale) >> 23) - 127) + unit;
+            w.large = __any(factor - up > 126);
+            const int apart = w.large ? kLarge : 0;
+            up = min(up, factor - apart + 126);
             constexpr bool nibble = KIND == UNISVQ_CACHE_I4;
 #pragma unroll
             for (int n = 0; n < D / 32; ++n)
@@ -595,7 +615,7 @@ __device__ __forceinline__ void attend_item(const Decode& a, int b, int hr, int 
                 w.start[n] += __shfl_xor(w.start[n], 32);
                 w.start[n] *= -static_cast<float>(G::bias) * 0x1p-24f;
             }
-            w.qscale = ldexpf(w.qscale, -up) * G::unit;
+            w.qscale = fminf(ldexpf(a.scale, unit - up - apart), FLT_MAX);
         }
     }
     w.begin();

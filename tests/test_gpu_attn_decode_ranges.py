@@ -57,12 +57,13 @@ def attend_and_check(u, kind, q, k, v, scale, rows=None, spoil=()):
         seen = n - q_len + 1 + j
         qj, kj, vj = q[j:j + 1].double().numpy(), hk[:seen], hv[:seen]
         r = ref.attention(qj, kj, vj, [seen - 1], scale)
-        halves = np.abs(vj).reshape(seen, H, 2 if kind == "i4" else 1, -1).max(-1)  # [token][head][half]
+        parts = 2 if kind == "i4" else 1
+        halves = np.abs(vj).reshape(seen, H, parts, D // parts).max(-1)  # [token][head][half]
         most = np.zeros((1, HQ, D))
         for h in range(HQ):
             s = scale * (kj[:, h * H // HQ] @ qj[0, h])
             p = np.exp(s - r[1][0, h])
-            most[0, h] = np.repeat((p[:, None] * halves[:, h * H // HQ]).max(0), D // halves.shape[2])
+            most[0, h] = np.repeat((p[:, None] * halves[:, h * H // HQ]).max(0, initial=0), D // parts)
         ref.check(out[j:j + 1].double().cpu().numpy(), lse[0, j:j + 1].double().cpu().numpy(), r, seen, "f16", "bf16", most)
     return out
 
@@ -158,3 +159,20 @@ def test_values_of_all_magnitudes(u, kind, up):
     k, v = rng.standard_normal((2, 400, 1, 128))
     q = torch.from_numpy(rng.standard_normal((1, 2, 128))).bfloat16()
     attend_and_check(u, kind, q, k, v * 2.0 ** up, 0.1)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n", [1, 45, 300])
+@pytest.mark.parametrize("query,key,scale", [
+    (-130, 0, 1e-3),  # subnormal queries: all tokens count alike
+    (-130, 0, 1e-30), (0, 0, 1e-40),
+    (122, None, None), (126, None, 1.0),  # keys of zero
+    (122, -98, None), (125, -95, 2.0 ** -30), (120, -98, 1.0),
+])
+def test_queries_at_the_ends_of_their_type(u, kind, n, query, key, scale):
+    """bf16 queries of 2^query, keys of 2^key (None: zeros): the scores are finite numbers, and so are the results."""
+    rng = np.random.default_rng(5)
+    k, v = rng.standard_normal((2, n, 1, 128))
+    q = torch.from_numpy(np.clip(rng.standard_normal((2, 2, 128)), -3, 3) * 2.0 ** query).bfloat16()
+    q[0, 1] = 0  # (a row of another magnitude beside it)
+    attend_and_check(u, kind, q, k * 2.0 ** key if key is not None else 0 * k, v, 128 ** -0.5 if scale is None else scale)
