@@ -699,7 +699,9 @@ int unisvq_cache_read(const unisvq_cache* cache, const int32_t* page_table, int6
  *              the sum of exp(scale * q k), to join this with other parts
  *   workspace  device, >= unisvq_attn_decode_workspace_bytes(...) bytes,
  *              16-byte aligned (UNISVQ_EWORKSPACE / UNISVQ_EALIGN); may be
- *              NULL when that size is 0.  Overwritten.
+ *              NULL when that size is 0.  Overwritten.  The size for a max_len
+ *              serves every call with that max_len or less, whatever the page
+ *              table's width; for max_len 0 it serves every call
  * Scores, softmax and sums are fp32; the products run on the matrix cores in
  * 16 bits: 8- and 4-bit codes exactly, the weights of the values rounded to
  * f16, or to bf16 for a BF16 cache.  Over codes it is a weight times the

@@ -159,6 +159,7 @@ bool decode_shape_ok(int64_t sequences, int64_t q_len, int64_t q_heads, int64_t 
 size_t unisvq_attn_decode_workspace_bytes(int64_t sequences, int64_t q_len, int64_t q_heads, int64_t kv_heads,
                                           int64_t head_dim, int64_t max_len) {
     if (!decode_shape_ok(sequences, q_len, q_heads, kv_heads, head_dim, max_len) || sequences == 0) return 0;
+    if (max_len == 0) max_len = kMaxContext;  // any page table's width: more is never needed for less
     // for the 16-bit kinds, which are split first
     const int slots = unisvq::decode_slots(sequences, static_cast<int>(q_len), static_cast<int>(q_heads),
                                            static_cast<int>(kv_heads), max_len, static_cast<int>(4 * head_dim));

@@ -1066,6 +1066,7 @@ def cache_read(cache, page_table, starts, cu, tokens: int, out=None, out_dtype=N
 
 def attn_decode_workspace_bytes(sequences: int, q_len: int, q_heads: int, kv_heads: int, head_dim: int,
                                 max_len: int) -> int:
+    """Bytes that attn_decode with this max_len needs (0: with any, over any page table)."""
     return load().unisvq_attn_decode_workspace_bytes(sequences, q_len, q_heads, kv_heads, head_dim, max_len)
 
 
@@ -1093,7 +1094,7 @@ def attn_decode(q, cache, page_table, lens, scale: float | None = None, max_len:
     orr = _rows(out3, "out", None, None, None, q.dtype)
     room = pt[2] * c.page_tokens
     need = _workspace_size("unisvq_attn_decode_workspace_bytes", sequences, q_len, q_heads, c.kv_heads, head_dim,
-                           min(max_len, room) if max_len else room)
+                           max(1, min(max_len, room) if max_len else room))  # (0 would be any width)
     ws, wp, size = _scratch(workspace, need, q, stream)
     st = load().unisvq_attn_decode(
         c, *pt, _words(lens, sequences, "lens", torch.int32), max_len, q_len, q_heads, *qr, _halves()[q.dtype],
