@@ -765,8 +765,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void decode_kernel(Decode a) {
 
 // Workgroups: as many as there are units if all sequences have max_len tokens.
 int decode_grid(int64_t sequences, int items, int64_t max_len) {
-    const int64_t units = std::max<int64_t>(1, (max_len + kUnit - 1) / kUnit) * sequences * items;
-    return static_cast<int>(std::min<int64_t>(units, kGrid));
+    const int64_t count = std::min<int64_t>(sequences * items, kGrid);  // (their product with the units may pass 64 bits)
+    return static_cast<int>(std::min<int64_t>(count * std::max<int64_t>(1, (max_len + kUnit - 1) / kUnit), kGrid));
 }
 
 int row_tiles_of(int q_len, int q_heads, int kv_heads) { return (q_len * (q_heads / kv_heads) + kRows - 1) / kRows; }

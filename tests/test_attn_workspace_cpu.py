@@ -45,3 +45,10 @@ def test_calls_ask_for_the_size_of_the_width():
         need = size(1, 1, 8, 8, 128, 16 * width)
         assert need > 0 and asks_for_workspace(1, 1, 8, 8, 128, 0, width)
         assert need <= size(1, 1, 8, 8, 128, 0)
+
+
+@pytest.mark.parametrize("q_len,heads,slots", [(16, (65535, 65535), 3), (16, (65535, 1), 3), (1, (8, 8), 66), (1, (1024, 1024), 3)])
+def test_the_largest_counts_do_not_overflow(q_len, heads, slots):
+    """fp32 sums, a maximum and a sum for each part of each row, and the words that say where sequences begin."""
+    n = 2 ** 31 - 1
+    assert size(n, q_len, *heads, 128, 1 << 30) == n * q_len * heads[0] * slots * 130 * 4 + (n + 2) * 4
