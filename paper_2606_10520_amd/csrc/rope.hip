@@ -4,6 +4,7 @@
 //
 // The table is made once, in fp64: an angle p f_i reaches 10^5 and more, where
 // an fp32 product would be off by a hundredth of a turn.
+#include <algorithm>
 #include <cmath>
 
 #include "attn.hpp"
@@ -16,21 +17,22 @@ constexpr int kThreads = 256;
 __global__ __launch_bounds__(kThreads) void rope_table_kernel(int64_t count, int half, double log_theta, double factor,
                                                               double low, double high, double original,
                                                               double magnitude, float* table) {
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    if (i >= count) return;
-    const int64_t p = i / half;
-    const int j = static_cast<int>(i - p * half);
-    double f = exp(-log_theta * j / half);
-    double g = 0.0;
-    if (original > 0) {
-        const double turns = original * f * 0.15915494309189533577;  // 1 / (2 pi)
-        g = fmin(fmax((turns - low) / (high - low), 0.0), 1.0);
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < count;
+         i += static_cast<int64_t>(gridDim.x) * kThreads) {
+        const int64_t p = i / half;
+        const int j = static_cast<int>(i - p * half);
+        double f = exp(-log_theta * j / half);
+        double g = 0.0;
+        if (original > 0) {
+            const double turns = original * f * 0.15915494309189533577;  // 1 / (2 pi)
+            g = fmin(fmax((turns - low) / (high - low), 0.0), 1.0);
+        }
+        f = (1.0 - g) * f / factor + g * f;
+        double s, c;
+        sincos(static_cast<double>(p) * f, &s, &c);
+        table[2 * p * half + j] = static_cast<float>(magnitude * c);
+        table[(2 * p + 1) * half + j] = static_cast<float>(magnitude * s);
     }
-    f = (1.0 - g) * f / factor + g * f;
-    double s, c;
-    sincos(static_cast<double>(p) * f, &s, &c);
-    table[2 * p * half + j] = static_cast<float>(magnitude * c);
-    table[(2 * p + 1) * half + j] = static_cast<float>(magnitude * s);
 }
 
 // Bound by memory: x is read and y written once.  A thread rotates sixteen dims
@@ -83,7 +85,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(uint32_t count, int head
 hipError_t launch_rope_table(int64_t positions, int rot, double theta, double factor, double low, double high,
                              double original, double magnitude, float* table, hipStream_t s) {
     const int64_t count = positions * (rot / 2);
-    const uint32_t blocks = static_cast<uint32_t>((count + kThreads - 1) / kThreads);
+    // (a launch has fewer than 2^32 threads, the largest table twice as many entries)
+    const uint32_t blocks = static_cast<uint32_t>(std::min<int64_t>((count + kThreads - 1) / kThreads, 1 << 20));
     rope_table_kernel<<<blocks, kThreads, 0, s>>>(count, rot / 2, std::log(theta), factor, low, high, original,
                                                   magnitude, table);
     return hipGetLastError();

@@ -126,3 +126,13 @@ def test_another_stream(u):
     u.rope(x, pos, table, out=out, stream=s)
     s.synchronize()
     assert torch.equal(out, want)
+
+
+def test_table_of_more_entries_than_a_launch_has_threads(u):
+    """2^24 positions of 256 pairs: rows at both ends and around the 2^32nd entry."""
+    table = u.rope_table(1 << 24, 512, theta=1e6)
+    for p in (0, 1, (1 << 23) - 1, 1 << 23, (1 << 24) - 2, (1 << 24) - 1):
+        angle = p * 1e6 ** (-2.0 * np.arange(256) / 512)
+        want = np.stack([np.cos(angle), np.sin(angle)])
+        # one rounding to fp32, and the angle's: p * (a few 2^-53)
+        assert np.max(np.abs(table[p].double().cpu().numpy() - want)) <= 2.0 ** -24 + p * 2.0 ** -49
