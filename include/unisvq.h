@@ -693,6 +693,7 @@ int unisvq_cache_read(const unisvq_cache* cache, const int32_t* page_table, int6
  *              * kv_heads * ceil(q_len * q_heads / kv_heads / 16): items below
  *              2^24 and items * (table_width * page_tokens / 128 + 1) to 2^30
  *              (UNISVQ_EUNSUP otherwise)
+ *   scale      above 0, scale * log2(e) finite (UNISVQ_EINVAL otherwise)
  *   q, out     device [sequences * q_len][q_heads][head_dim], x_dtype; a
  *              16-bit kind has to be x_dtype's (UNISVQ_EUNSUP)
  *   lse        device fp32 [sequences * q_len][q_heads] or NULL: the log of
@@ -735,6 +736,7 @@ int unisvq_attn_decode(const unisvq_cache* cache, const int32_t* page_table, int
  *               and v from head_dim to 2^22; q_tokens * q_heads below 2^31
  *               and q_tokens * q_heads / 128 + sequences * kv_heads below 2^24
  *               (UNISVQ_EUNSUP otherwise)
+ *   scale       as above
  *   lse         device fp32 [q_tokens][q_heads] or NULL, as above
  *   workspace   device, >= unisvq_attn_prompt_workspace_bytes(...) bytes,
  *               16-byte aligned; may be NULL when that size is 0 (it is where

@@ -55,6 +55,9 @@ bool kind_serves(int kind, int dtype) {
     return kind == UNISVQ_CACHE_F16 ? dtype == UNISVQ_F16 : kind == UNISVQ_CACHE_BF16 ? dtype == UNISVQ_BF16 : true;
 }
 
+// Scores are multiplied by scale * log2(e) in fp32.
+bool scale_ok(float scale) { return scale > 0 && std::isfinite(scale * 1.44269504088896340736f); }
+
 bool heads_ok(int64_t q_heads, int64_t kv_heads) {
     return kv_heads >= 1 && q_heads >= kv_heads && q_heads <= 65535 && q_heads % kv_heads == 0;
 }
@@ -177,7 +180,7 @@ int unisvq_attn_decode(const unisvq_cache* cache, const int32_t* page_table, int
     if (st != UNISVQ_OK) return st;
     const int64_t room = table_width * cache->page_tokens;
     if (max_len == 0 || max_len > room) max_len = room;
-    if (!dtype_ok(x_dtype) || !(scale > 0) || !std::isfinite(scale) ||
+    if (!dtype_ok(x_dtype) || !scale_ok(scale) ||
         !decode_shape_ok(sequences, q_len, q_heads, c.heads, c.head_dim, max_len))
         return UNISVQ_EINVAL;
     if (!kind_serves(c.kind, x_dtype)) return UNISVQ_EUNSUP;
@@ -221,7 +224,7 @@ int unisvq_attn_prompt(int64_t sequences, int64_t q_tokens, int64_t k_tokens, co
                        int causal, float scale, void* out, int64_t out_token_stride, int64_t out_head_stride,
                        float* lse, void* workspace, size_t workspace_bytes, void* stream) {
     if (sequences < 0 || sequences > kMost || q_tokens < 0 || q_tokens > kMaxContext || k_tokens < 0 ||
-        k_tokens > kMaxContext || !dtype_ok(dtype) || !(scale > 0) || !std::isfinite(scale) || !heads_ok(q_heads, kv_heads))
+        k_tokens > kMaxContext || !dtype_ok(dtype) || !scale_ok(scale) || !heads_ok(q_heads, kv_heads))
         return UNISVQ_EINVAL;
     if (head_dim != 64 && head_dim != 128) return UNISVQ_EUNSUP;
     if (sequences == 0 || q_tokens == 0) return UNISVQ_OK;
