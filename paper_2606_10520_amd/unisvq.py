@@ -854,30 +854,50 @@ def _halves():
     return _HALVES
 
 
-_current_stream = None  # of a device's index, as a handle
+_current = None  # the current device, and the current stream of a device, as a handle
 
 
-def _raw_stream(stream, t) -> int:
-    """The stream's handle; None: the current one of t's device."""
-    global _current_stream
-    if stream is not None:
-        return stream.cuda_stream
-    if _current_stream is None:
-        torch = _torch()
+def _launch(name: str, device: int, stream, *args):
+    """Calls an entry point with `device` current, on `stream` (None: the device's current one), and checks its status."""
+    global _current
+    torch = _torch()
+    if _current is None:
         # (torch's own way to the handle without a Stream object around it, where it has one)
-        _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
-                                  lambda device: torch.cuda.current_stream(device).cuda_stream)
-    return _current_stream(t.get_device())
+        _current = (torch.cuda.current_device, getattr(torch._C, "_cuda_getCurrentRawStream",
+                                                       lambda device: torch.cuda.current_stream(device).cuda_stream))
+    if stream is None:
+        handle = _current[1](device)
+    else:
+        if stream.device.index != device:
+            raise ValueError(f"the stream is device {stream.device.index}'s, the tensors are on device {device}")
+        handle = stream.cuda_stream
+    call = getattr(load(), name)
+    if _current[0]() == device:
+        st = call(*args, handle)
+    else:
+        with torch.cuda.device(device):
+            st = call(*args, handle)
+    if st:
+        raise UniSVQError(name, st)
 
 
-def _rows(t, what: str, heads=None, head_dim=None, tokens=None, dtype=None):
+def _device(t, what: str, device=None) -> int:
+    """The index of the device that t is on, which has to be `device` if that is given."""
+    at = t.get_device()
+    if at < 0:
+        raise ValueError("libunisvq takes device tensors only")
+    if device is not None and at != device:
+        raise ValueError(f"{what} is on device {at}, other tensors of the call are on device {device}")
+    return at
+
+
+def _rows(t, what: str, device: int, heads=None, head_dim=None, tokens=None, dtype=None):
     """A [tokens][heads][head_dim] fp16/bf16 device tensor, its last axis contiguous, any strides of the other two (the
     C entry refuses those that are not multiples of 8): checked, and as (pointer, token stride, head stride)."""
     shape, strides = t.shape, t.stride()
     if len(shape) != 3 or strides[2] != 1:
         raise ValueError(f"{what} must be [tokens][heads][head_dim] with contiguous dims, got {tuple(shape)}, strides {strides}")
-    if not t.is_cuda:
-        raise ValueError("libunisvq takes device tensors only")
+    _device(t, what, device)
     if t.dtype is not dtype and (dtype is not None or t.dtype not in _halves()):
         raise TypeError(f"{what} is {t.dtype}, expected {'fp16 or bf16' if dtype is None else dtype}")
     if (tokens is not None and shape[0] != tokens) or (heads is not None and shape[1] != heads) or \
@@ -886,12 +906,13 @@ def _rows(t, what: str, heads=None, head_dim=None, tokens=None, dtype=None):
     return t.data_ptr(), strides[0], strides[1]
 
 
-def _words(t, count: int, what: str, dtype):
+def _words(t, count: int, what: str, dtype, device: int):
     """A contiguous device tensor of `count` elements of dtype, as a pointer (None: None)."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.numel() != count or not t.is_contiguous() or not t.is_cuda:
+    if t.dtype is not dtype or t.numel() != count or not t.is_contiguous():
         raise ValueError(f"{what} must hold {count} contiguous {dtype} on the device, got {t.dtype} {tuple(t.shape)}")
+    _device(t, what, device)
     return t.data_ptr()
 
 
@@ -905,11 +926,11 @@ def _new(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _out_rows(out, like, tokens: int, heads: int, head_dim: int, stream, what: str = "out"):
+def _out_rows(out, like, tokens: int, heads: int, head_dim: int, device: int, stream, what: str = "out"):
     """The caller's out (checked) or a new tensor, and its rows."""
     if out is None:
         out = _new((tokens, heads, head_dim), like.dtype, like.device, stream)
-    return out, _rows(out, what, heads, head_dim, tokens, like.dtype)
+    return out, _rows(out, what, device, heads, head_dim, tokens, like.dtype)
 
 
 @functools.lru_cache(maxsize=4096)
@@ -925,6 +946,7 @@ def _scratch(workspace, need: int, like, stream):
         workspace = _new(need, _torch().uint8, like.device, stream)
     else:
         workspace, need = _workspace(workspace, need, like)
+        _device(workspace, "workspace", like.get_device())
     return workspace, workspace.data_ptr(), need
 
 
@@ -932,18 +954,18 @@ def rope_table(positions: int, rot: int, theta: float = 10000.0, factor: float =
                high: float = 4.0, original: float = 0.0, magnitude: float = 1.0, device="cuda", stream=None):
     """Cosines and sines [positions][2][rot / 2] (fp32) of rotary positions; factor, low, high, original and magnitude
     stretch them over long contexts as unisvq_rope_table says."""
-    torch = _torch()
-    table = _new((positions, 2, rot // 2), torch.float32, device, stream)
-    _check("unisvq_rope_table", load().unisvq_rope_table(positions, rot, theta, factor, low, high, original, magnitude,
-                                                         _ptr(table), _stream(stream)))
+    table = _new((positions, 2, rot // 2), _torch().float32, device, stream)
+    _launch("unisvq_rope_table", _device(table, "table"), stream, positions, rot, theta, factor, low, high, original,
+            magnitude, _ptr(table))
     return table
 
 
-def _rope_rows(table):
+def _rope_rows(table, device: int):
     """(pointer, positions, rot) of a table of rope_table's."""
     shape = table.shape
-    if table.dtype is not _torch().float32 or len(shape) != 3 or shape[1] != 2 or not table.is_contiguous() or not table.is_cuda:
+    if table.dtype is not _torch().float32 or len(shape) != 3 or shape[1] != 2 or not table.is_contiguous():
         raise ValueError("the rope table must be contiguous fp32 [positions][2][rot / 2] on the device")
+    _device(table, "the rope table", device)
     return table.data_ptr(), shape[0], 2 * shape[2]
 
 
@@ -951,15 +973,13 @@ def rope(x, positions, table, interleaved: bool = False, inverse: bool = False, 
     """x [tokens][heads][head_dim] rotated to int32 positions [tokens]: the first rot = 2 * table.shape[2] dims of
     every head, in pairs (i, i + rot / 2) or, interleaved, (2i, 2i + 1); inverse: the transpose (the gradient).
     out may be x (in place) or a view with its own strides."""
-    xr = _rows(x, "x")
+    device = x.get_device()
+    xr = _rows(x, "x", device)
     tokens, heads, head_dim = x.shape
-    out, yr = _out_rows(out, x, tokens, heads, head_dim, stream)
-    tp, n, rot = _rope_rows(table)
-    st = load().unisvq_rope(tokens, heads, head_dim, rot, interleaved, inverse, *xr,
-                            _words(positions, tokens, "positions", _torch().int32), tp, n, *yr, _halves()[x.dtype],
-                            _raw_stream(stream, x))
-    if st:
-        raise UniSVQError("unisvq_rope", st)
+    out, yr = _out_rows(out, x, tokens, heads, head_dim, device, stream)
+    tp, n, rot = _rope_rows(table, device)
+    _launch("unisvq_rope", device, stream, tokens, heads, head_dim, rot, interleaved, inverse, *xr,
+            _words(positions, tokens, "positions", _torch().int32, device), tp, n, *yr, _halves()[x.dtype])
     return out
 
 
@@ -984,7 +1004,7 @@ def new_cache(pages: int, kv_heads: int, page_tokens: int, head_dim: int, kind: 
 _KINDS = {}  # dtype of the pools -> (kind, dims an element holds, dtype of the scales)
 
 
-def _cache(cache):
+def _cache(cache, device: int):
     """The C description of a cache tuple (k, v, k_scales, v_scales), checked; the kind is the pools' dtype's."""
     if not _KINDS:
         torch = _torch()
@@ -997,22 +1017,23 @@ def _cache(cache):
     kind, dims, scale_type = _KINDS[dt]
     if len(shape) != 4 or v.shape != shape or v.dtype is not dt or not (k.is_contiguous() and v.is_contiguous()):
         raise ValueError("k and v pools must be contiguous [pages][kv_heads][page_tokens][..] of one dtype")
-    if not (k.is_cuda and v.is_cuda):
-        raise ValueError("libunisvq takes device tensors only")
+    _device(k, "the k pool", device)
+    _device(v, "the v pool", device)
     pages, kv_heads, page_tokens, last = shape
     ksp = vsp = None
     if scale_type is not None:
         if ks is None or vs is None:
             raise ValueError("codes come with scales")
         count = pages * kv_heads * page_tokens * dims
-        ksp, vsp = _words(ks, count, "k_scales", scale_type), _words(vs, count, "v_scales", scale_type)
+        ksp, vsp = _words(ks, count, "k_scales", scale_type, device), _words(vs, count, "v_scales", scale_type, device)
     return Cache(pages, page_tokens, kv_heads, last * dims, kind, k.data_ptr(), v.data_ptr(), ksp, vsp)
 
 
-def _page_table(table):
+def _page_table(table, device: int):
     shape = table.shape
-    if table.dtype is not _torch().int32 or len(shape) != 2 or not table.is_contiguous() or not table.is_cuda:
+    if table.dtype is not _torch().int32 or len(shape) != 2 or not table.is_contiguous():
         raise ValueError("the page table must be contiguous int32 [sequences][pages of a sequence] on the device")
+    _device(table, "the page table", device)
     return table.data_ptr(), shape[0], shape[1]
 
 
@@ -1024,22 +1045,21 @@ def cache_append(cache, page_table, seqs, positions, k, v, q=None, rope_table=No
     """Write k and v [tokens][kv_heads][head_dim] to the cache, keys rotated by rope_table (None: as they are), at
     int32 positions [tokens] of sequences seqs [tokens] (None: token t is sequence t's).  q [tokens][q_heads][head_dim]
     is rotated in the same launch and returned (q_out, which may be q, or a new tensor; None where q is None)."""
-    c = _cache(cache)
+    device = k.get_device()
+    c = _cache(cache, device)
     int32, kv_heads, head_dim, dt = _torch().int32, c.kv_heads, c.head_dim, k.dtype
-    kr = _rows(k, "k", kv_heads, head_dim)
+    kr = _rows(k, "k", device, kv_heads, head_dim)
     tokens = k.shape[0]
-    vr = _rows(v, "v", kv_heads, head_dim, tokens, dt)
+    vr = _rows(v, "v", device, kv_heads, head_dim, tokens, dt)
     q_heads, qr, qor = 0, _NO_ROWS, _NO_ROWS
     if q is not None:
-        qr = _rows(q, "q", None, head_dim, tokens, dt)
+        qr = _rows(q, "q", device, None, head_dim, tokens, dt)
         q_heads = q.shape[1]
-        q_out, qor = _out_rows(q_out, q, tokens, q_heads, head_dim, stream, "q_out")
-    st = load().unisvq_cache_append(
-        c, *_page_table(page_table), tokens, _words(seqs, tokens, "seqs", int32),
-        _words(positions, tokens, "positions", int32), *kr, *vr, qr[0], q_heads, qr[1], qr[2], *qor, _halves()[dt],
-        *(_NO_ROWS if rope_table is None else _rope_rows(rope_table)), interleaved, _raw_stream(stream, k))
-    if st:
-        raise UniSVQError("unisvq_cache_append", st)
+        q_out, qor = _out_rows(q_out, q, tokens, q_heads, head_dim, device, stream, "q_out")
+    _launch("unisvq_cache_append", device, stream, c, *_page_table(page_table, device), tokens,
+            _words(seqs, tokens, "seqs", int32, device), _words(positions, tokens, "positions", int32, device), *kr, *vr,
+            qr[0], q_heads, qr[1], qr[2], *qor, _halves()[dt],
+            *(_NO_ROWS if rope_table is None else _rope_rows(rope_table, device)), interleaved)
     return q_out if q is not None else None
 
 
@@ -1048,19 +1068,17 @@ def cache_read(cache, page_table, starts, cu, tokens: int, out=None, out_dtype=N
     cu[b] .. cu[b + 1] - 1 are sequence b's (cu int32 [sequences + 1]; starts int32 [sequences] or None: 0).  out: a
     pair (k, v) of tensors to write, or None."""
     torch = _torch()
-    c = _cache(cache)
-    pt = _page_table(page_table)
+    device = cache[0].get_device()
+    c = _cache(cache, device)
+    pt = _page_table(page_table, device)
     if out is None:
         dt = out_dtype or (cache[0].dtype if cache[0].dtype.is_floating_point else torch.float16)
         out = tuple(_new((tokens, c.kv_heads, c.head_dim), dt, cache[0].device, stream) for _ in range(2))
     k, v = out
-    kr = _rows(k, "out k", c.kv_heads, c.head_dim, tokens)
-    vr = _rows(v, "out v", c.kv_heads, c.head_dim, tokens, k.dtype)
-    st = load().unisvq_cache_read(c, *pt, _words(starts, pt[1], "starts", torch.int32),
-                                  _words(cu, pt[1] + 1, "cu", torch.int32), tokens, *kr, *vr, _halves()[k.dtype],
-                                  _raw_stream(stream, k))
-    if st:
-        raise UniSVQError("unisvq_cache_read", st)
+    kr = _rows(k, "out k", device, c.kv_heads, c.head_dim, tokens)
+    vr = _rows(v, "out v", device, c.kv_heads, c.head_dim, tokens, k.dtype)
+    _launch("unisvq_cache_read", device, stream, c, *pt, _words(starts, pt[1], "starts", torch.int32, device),
+            _words(cu, pt[1] + 1, "cu", torch.int32, device), tokens, *kr, *vr, _halves()[k.dtype])
     return k, v
 
 
@@ -1077,8 +1095,9 @@ def attn_decode(q, cache, page_table, lens, scale: float | None = None, max_len:
     scores (None: head_dim ** -0.5).  max_len: what the lengths are at most (0: the page table's width).  lse: fp32
     tensor for the log of the sum of exponentials, or None.  workspace: as gemm's."""
     torch = _torch()
-    c = _cache(cache)
-    pt = _page_table(page_table)
+    device = q.get_device()
+    c = _cache(cache, device)
+    pt = _page_table(page_table, device)
     shape, head_dim = q.shape, c.head_dim
     if len(shape) not in (3, 4) or shape[0] != pt[1]:
         raise ValueError(f"q must be [sequences][q_heads][head_dim] or [sequences][q_len][q_heads][head_dim] of the page "
@@ -1090,18 +1109,15 @@ def attn_decode(q, cache, page_table, lens, scale: float | None = None, max_len:
     elif out.shape != shape:
         raise ValueError(f"out is {tuple(out.shape)}, q {tuple(shape)}")
     q3, out3 = (q, out) if len(shape) == 3 else (q.view(tokens, q_heads, shape[3]), out.view(tokens, q_heads, shape[3]))
-    qr = _rows(q3, "q", None, head_dim)
-    orr = _rows(out3, "out", None, None, None, q.dtype)
+    qr = _rows(q3, "q", device, None, head_dim)
+    orr = _rows(out3, "out", device, None, None, None, q.dtype)
     room = pt[2] * c.page_tokens
     need = _workspace_size("unisvq_attn_decode_workspace_bytes", sequences, q_len, q_heads, c.kv_heads, head_dim,
                            max(1, min(max_len, room) if max_len else room))  # (0 would be any width)
     ws, wp, size = _scratch(workspace, need, q, stream)
-    st = load().unisvq_attn_decode(
-        c, *pt, _words(lens, sequences, "lens", torch.int32), max_len, q_len, q_heads, *qr, _halves()[q.dtype],
-        head_dim ** -0.5 if scale is None else scale, *orr, _words(lse, tokens * q_heads, "lse", torch.float32), wp,
-        size, _raw_stream(stream, q))
-    if st:
-        raise UniSVQError("unisvq_attn_decode", st)
+    _launch("unisvq_attn_decode", device, stream, c, *pt, _words(lens, sequences, "lens", torch.int32, device), max_len,
+            q_len, q_heads, *qr, _halves()[q.dtype], head_dim ** -0.5 if scale is None else scale, *orr,
+            _words(lse, tokens * q_heads, "lse", torch.float32, device), wp, size)
     return out
 
 
@@ -1117,20 +1133,19 @@ def attn_prompt(q, k, v, cu_q, cu_k, causal: bool = True, scale: float | None = 
     [sequences + 1]).  Causal: the last query of a sequence sees all its keys, each one before it one key less.  scale,
     lse, workspace: as attn_decode's."""
     torch = _torch()
-    qr = _rows(q, "q")
+    device = q.get_device()
+    qr = _rows(q, "q", device)
     tokens, q_heads, head_dim = q.shape
-    kr = _rows(k, "k", None, head_dim, None, q.dtype)
+    kr = _rows(k, "k", device, None, head_dim, None, q.dtype)
     k_tokens, kv_heads = k.shape[0], k.shape[1]
-    vr = _rows(v, "v", kv_heads, head_dim, k_tokens, q.dtype)
-    out, orr = _out_rows(out, q, tokens, q_heads, head_dim, stream)
+    vr = _rows(v, "v", device, kv_heads, head_dim, k_tokens, q.dtype)
+    out, orr = _out_rows(out, q, tokens, q_heads, head_dim, device, stream)
     sequences = cu_q.numel() - 1
     need = _workspace_size("unisvq_attn_prompt_workspace_bytes", sequences, tokens, k_tokens, q_heads, kv_heads, head_dim)
     ws, wp, size = _scratch(workspace, need, q, stream)
-    st = load().unisvq_attn_prompt(
-        sequences, tokens, k_tokens, _words(cu_q, sequences + 1, "cu_q", torch.int32),
-        _words(cu_k, sequences + 1, "cu_k", torch.int32), q_heads, kv_heads, head_dim, *qr, *kr, *vr,
-        _halves()[q.dtype], causal, head_dim ** -0.5 if scale is None else scale, *orr,
-        _words(lse, tokens * q_heads, "lse", torch.float32), wp, size, _raw_stream(stream, q))
-    if st:
-        raise UniSVQError("unisvq_attn_prompt", st)
+    _launch("unisvq_attn_prompt", device, stream, sequences, tokens, k_tokens,
+            _words(cu_q, sequences + 1, "cu_q", torch.int32, device),
+            _words(cu_k, sequences + 1, "cu_k", torch.int32, device), q_heads, kv_heads, head_dim, *qr, *kr, *vr,
+            _halves()[q.dtype], causal, head_dim ** -0.5 if scale is None else scale, *orr,
+            _words(lse, tokens * q_heads, "lse", torch.float32, device), wp, size)
     return out
