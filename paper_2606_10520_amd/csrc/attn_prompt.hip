@@ -134,8 +134,9 @@ __device__ inline void mark_not_finite(const T* vs, int k0, int limit, int lane,
             left &= left - 1;
             const int place = at - lane + from, row = place / chunks;
             const int dim = ((place % chunks) ^ turn_v<D>(row)) * 8;
-            uint64_t lo = __builtin_amdgcn_readlane(w[0], from) | static_cast<uint64_t>(__builtin_amdgcn_readlane(w[1], from)) << 32;
-            uint64_t hi = __builtin_amdgcn_readlane(w[2], from) | static_cast<uint64_t>(__builtin_amdgcn_readlane(w[3], from)) << 32;
+            const auto word = [&](int x) { return static_cast<uint32_t>(__builtin_amdgcn_readlane(w[x], from)); };
+            uint64_t lo = word(0) | static_cast<uint64_t>(word(1)) << 32;
+            uint64_t hi = word(2) | static_cast<uint64_t>(word(3)) << 32;
 #pragma nounroll
             for (int e = 0; e < 8; ++e) {
                 const uint32_t bits = static_cast<uint32_t>(lo & 0xffffu);
