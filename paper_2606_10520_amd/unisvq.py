@@ -860,35 +860,33 @@ _current = None  # the current device, and the current stream of a device, as a 
 def _launch(name: str, device: int, stream, *args):
     """Calls an entry point with `device` current, on `stream` (None: the device's current one), and checks its status."""
     global _current
-    torch = _torch()
     if _current is None:
-        # (torch's own way to the handle without a Stream object around it, where it has one)
-        _current = (torch.cuda.current_device, getattr(torch._C, "_cuda_getCurrentRawStream",
-                                                       lambda device: torch.cuda.current_stream(device).cuda_stream))
+        torch = _torch()
+        # (torch's own ways without its lazy initialisation, done by then, and a Stream object, where it has them)
+        _current = (getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device),
+                    getattr(torch._C, "_cuda_getCurrentRawStream",
+                            lambda device: torch.cuda.current_stream(device).cuda_stream))
     if stream is None:
         handle = _current[1](device)
-    else:
-        if stream.device.index != device:
-            raise ValueError(f"the stream is device {stream.device.index}'s, the tensors are on device {device}")
+    elif stream.device.index == device:
         handle = stream.cuda_stream
+    else:
+        raise ValueError(f"the stream is device {stream.device.index}'s, the tensors are on device {device}")
     call = getattr(load(), name)
     if _current[0]() == device:
         st = call(*args, handle)
     else:
-        with torch.cuda.device(device):
+        with _torch().cuda.device(device):
             st = call(*args, handle)
     if st:
         raise UniSVQError(name, st)
 
 
-def _device(t, what: str, device=None) -> int:
-    """The index of the device that t is on, which has to be `device` if that is given."""
-    at = t.get_device()
-    if at < 0:
+def _elsewhere(t, what: str, device: int):
+    """Refuses t, which is not on `device`, the first tensor's (below 0: the host)."""
+    if t.get_device() < 0 or device < 0:
         raise ValueError("libunisvq takes device tensors only")
-    if device is not None and at != device:
-        raise ValueError(f"{what} is on device {at}, other tensors of the call are on device {device}")
-    return at
+    raise ValueError(f"{what} is on device {t.get_device()}, other tensors of the call are on device {device}")
 
 
 def _rows(t, what: str, device: int, heads=None, head_dim=None, tokens=None, dtype=None):
@@ -897,7 +895,8 @@ def _rows(t, what: str, device: int, heads=None, head_dim=None, tokens=None, dty
     shape, strides = t.shape, t.stride()
     if len(shape) != 3 or strides[2] != 1:
         raise ValueError(f"{what} must be [tokens][heads][head_dim] with contiguous dims, got {tuple(shape)}, strides {strides}")
-    _device(t, what, device)
+    if t.get_device() != device or device < 0:
+        _elsewhere(t, what, device)
     if t.dtype is not dtype and (dtype is not None or t.dtype not in _halves()):
         raise TypeError(f"{what} is {t.dtype}, expected {'fp16 or bf16' if dtype is None else dtype}")
     if (tokens is not None and shape[0] != tokens) or (heads is not None and shape[1] != heads) or \
@@ -912,7 +911,8 @@ def _words(t, count: int, what: str, dtype, device: int):
         return None
     if t.dtype is not dtype or t.numel() != count or not t.is_contiguous():
         raise ValueError(f"{what} must hold {count} contiguous {dtype} on the device, got {t.dtype} {tuple(t.shape)}")
-    _device(t, what, device)
+    if t.get_device() != device or device < 0:
+        _elsewhere(t, what, device)
     return t.data_ptr()
 
 
@@ -946,7 +946,8 @@ def _scratch(workspace, need: int, like, stream):
         workspace = _new(need, _torch().uint8, like.device, stream)
     else:
         workspace, need = _workspace(workspace, need, like)
-        _device(workspace, "workspace", like.get_device())
+        if workspace.get_device() != like.get_device():
+            _elsewhere(workspace, "workspace", like.get_device())
     return workspace, workspace.data_ptr(), need
 
 
@@ -955,7 +956,8 @@ def rope_table(positions: int, rot: int, theta: float = 10000.0, factor: float =
     """Cosines and sines [positions][2][rot / 2] (fp32) of rotary positions; factor, low, high, original and magnitude
     stretch them over long contexts as unisvq_rope_table says."""
     table = _new((positions, 2, rot // 2), _torch().float32, device, stream)
-    _launch("unisvq_rope_table", _device(table, "table"), stream, positions, rot, theta, factor, low, high, original,
+    _need_cuda(table)
+    _launch("unisvq_rope_table", table.get_device(), stream, positions, rot, theta, factor, low, high, original,
             magnitude, _ptr(table))
     return table
 
@@ -965,7 +967,8 @@ def _rope_rows(table, device: int):
     shape = table.shape
     if table.dtype is not _torch().float32 or len(shape) != 3 or shape[1] != 2 or not table.is_contiguous():
         raise ValueError("the rope table must be contiguous fp32 [positions][2][rot / 2] on the device")
-    _device(table, "the rope table", device)
+    if table.get_device() != device or device < 0:
+        _elsewhere(table, "the rope table", device)
     return table.data_ptr(), shape[0], 2 * shape[2]
 
 
@@ -1017,8 +1020,10 @@ def _cache(cache, device: int):
     kind, dims, scale_type = _KINDS[dt]
     if len(shape) != 4 or v.shape != shape or v.dtype is not dt or not (k.is_contiguous() and v.is_contiguous()):
         raise ValueError("k and v pools must be contiguous [pages][kv_heads][page_tokens][..] of one dtype")
-    _device(k, "the k pool", device)
-    _device(v, "the v pool", device)
+    if k.get_device() != device or device < 0:
+        _elsewhere(k, "the k pool", device)
+    if v.get_device() != device or device < 0:
+        _elsewhere(v, "the v pool", device)
     pages, kv_heads, page_tokens, last = shape
     ksp = vsp = None
     if scale_type is not None:
@@ -1033,7 +1038,8 @@ def _page_table(table, device: int):
     shape = table.shape
     if table.dtype is not _torch().int32 or len(shape) != 2 or not table.is_contiguous():
         raise ValueError("the page table must be contiguous int32 [sequences][pages of a sequence] on the device")
-    _device(table, "the page table", device)
+    if table.get_device() != device or device < 0:
+        _elsewhere(table, "the page table", device)
     return table.data_ptr(), shape[0], shape[1]
 
 
