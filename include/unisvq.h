@@ -705,7 +705,8 @@ int unisvq_cache_read(const unisvq_cache* cache, const int32_t* page_table, int6
  *              table's width; for max_len 0 it serves every call
  * Scores, softmax and sums are fp32; the products run on the matrix cores in
  * 16 bits: 8- and 4-bit codes exactly, the weights of the values rounded to
- * f16, or to bf16 for a BF16 cache.  Over codes it is a weight times the
+ * f16 (those below 2^-32 of the largest vanish), or to bf16 for a BF16 cache.
+ * Over codes it is a weight times the
  * token's scale that is rounded to f16, in a unit set by the largest such
  * product among the tokens that the row sees (for I4, of that half of the
  * head): products of 2^-18 of the largest and more are rounded to 11 bits, those
@@ -743,7 +744,7 @@ int unisvq_attn_decode(const unisvq_cache* cache, const int32_t* page_table, int
  *               the queries fill the GPU; few queries before many keys are
  *               split along the keys).  Overwritten.
  * fp32 scores, softmax and sums; the softmax weights are rounded to dtype
- * for their product with v. */
+ * for their product with v (f16: those below 2^-32 of the largest vanish). */
 size_t unisvq_attn_prompt_workspace_bytes(int64_t sequences, int64_t q_tokens, int64_t k_tokens, int64_t q_heads,
                                           int64_t kv_heads, int64_t head_dim);
 int unisvq_attn_prompt(int64_t sequences, int64_t q_tokens, int64_t k_tokens, const int32_t* cu_q,

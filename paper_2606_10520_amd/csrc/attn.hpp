@@ -167,6 +167,13 @@ __device__ inline bool not_finite(uint32_t w) {
     return (w & e) == e || (w >> 16 & e) == e;
 }
 
+// Weights of 16-bit values are 2^(s - m) with m so far (log2) below the maximum
+// as f16's range allows beside what scores may exceed it by (2^8): a weight keeps
+// all its bits down to 2^-21 of the largest and vanishes below 2^-32.  bf16 has
+// fp32's range and needs none.
+template <typename T>
+__device__ constexpr float weight_lift() { return std::is_same_v<T, _Float16> ? 7.0f : 0.0f; }
+
 // w with zeros in place of what is not finite.
 template <typename T>
 __device__ inline uint32_t finite_only(uint32_t w) {

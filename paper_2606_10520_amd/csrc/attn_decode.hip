@@ -50,8 +50,8 @@
 // A workgroup's four waves take every fourth 32-token tile of its part of an
 // item, the next tile's loads under way while one is computed, each with its
 // own running maximum m, sum and outputs, joined through LDS.  m is raised only
-// when a score exceeds it by 2^8 (the weights then stay below 2^8, well inside
-// f16), so most tiles need no exchange between lanes and no rescaling.
+// when a score exceeds it by 2^8 (the weights then stay inside f16), so most tiles
+// need no exchange between lanes and no rescaling.
 //
 // Measured, with the launch that joins: 4 x 32768 tokens of 4-bit cache, 32
 // heads, 122 us (4.7 TB/s); 4 x 16384 of 8-bit 94 us (5.9 TB/s); 4 x 8192 of
@@ -332,6 +332,7 @@ struct Running {
     typedef Geometry<KIND, D> G;
     typedef typename Vec8<CT>::type C8;
     static constexpr int E = D / 16, HV = G::halves;
+    static constexpr float lift = G::scaled ? 0.0f : weight_lift<CT>();
     C8 q[D / 32];
     float start[HV];       // of the scores
     float qscale;          // of the scores to log2 units
@@ -387,7 +388,7 @@ struct Running {
     __device__ __forceinline__ void renew(const float (&s)[2][4], float top, TileRegs<KIND, D>& r) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float m2 = fmaxf(m, top), up = m2 - m;
+        const float m2 = fmaxf(m, top - lift), up = m2 - m;
         if constexpr (G::scaled) {
             float to[HV];
 #pragma unroll
@@ -473,7 +474,7 @@ __device__ __forceinline__ void attend(const Decode& a, TileRegs<KIND, D>& r, in
     f32x4 bias[HV];  // the operands' sum times the codes' bias, in all four
 #pragma nounroll
     for (bool again = false;; again = true) {
-        const bool renew = again || (G::scaled && w.apart) || __any(top > w.m + kSlack);
+        const bool renew = again || (G::scaled && w.apart) || __any(top > w.m + (kSlack + w.lift));
         if (renew) {
             if (G::scaled && w.large) {  // (then every tile comes here, and once)
                 top *= ldexpf(1.0f, kLarge);

@@ -17,9 +17,9 @@
 //                 transposing read, four keys of one dim a lane.
 // So a query's maximum and sum need one exchange between the halves of a wave,
 // the maximum's only when a score exceeds it by 2^8 (the weights stay below
-// 2^8, so nothing overflows, and most tiles need no rescaling).  The weights
-// are rounded to the type of v, which is what the matrix cores multiply; their
-// sum is of the unrounded ones, in fp32.
+// 2^8, or 2^15 in f16's range, so nothing overflows, and most tiles need no
+// rescaling).  The weights are rounded to the type of v, which is what the matrix
+// cores multiply; their sum is of the unrounded ones, in fp32.
 //
 // A tile's weights are followed by one run of 32 products, its values' and the
 // next tile's scores', with one barrier a tile; a wave in its products goes
@@ -265,9 +265,9 @@ struct Wave {
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, s[x][r]);
         top *= scale;
-        if (!__any(top > m + kSlack)) return;
+        if (!__any(top > m + (kSlack + weight_lift<T>()))) return;
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float m2 = fmaxf(m, top), c = exp2_(m - m2);
+        const float m2 = fmaxf(m, top - weight_lift<T>()), c = exp2_(m - m2);
         m = m2;
         l *= c;
 #pragma unroll
