@@ -737,7 +737,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void decode_kernel(Decode a) {
         if (static_cast<int64_t>(blockIdx.x) * share >= n) return;
         unit = blockIdx.x * share;
         last = min(unit + share, n);
+        // (this search and the loop below end, and stay inside, also where another
+        // stream writes the lengths meanwhile)
         for (int base = 0;; base += 64) {
+            if (base >= sequences) return;
             const int units = padded(units_at(base), pad);
             const int sum = scan64(units);
             const uint64_t in = __ballot(unit < (first + sum) * items);
@@ -750,11 +753,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void decode_kernel(Decode a) {
             first += __builtin_amdgcn_readlane(sum, 63);
         }
     }
-    while (unit < last) {
+    while (unit < last && b < sequences) {
         const int64_t room = a.c.width << a.c.page_shift;
         const int len = static_cast<int>(min(static_cast<int64_t>(max(0, load_uniform(a.lens + b))), room));
         const int n = padded(units_of(len), pad);
         const int hr = (unit - first * items) / n, item = first * items + hr * n;
+        if (hr >= items) return;
         const int begin = unit - item, end = min(n, last - item);
         const Shares s = shares_of(item, n, share);
         attend_item<KIND, D, XT, WAVES>(a, b, hr, len, begin, end, s.count == 1 ? -1 : static_cast<int>(blockIdx.x) - s.first, wave, lane);

@@ -115,3 +115,11 @@ def test_a_stream_of_another_device_is_refused(calls, op):
 def test_a_new_table_is_made_on_its_device(calls):
     assert u.rope_table(9, 64, device="cuda:1").get_device() == 1
     assert [c[1:] for c in calls] == [(1, 1001)]
+
+
+def test_a_table_in_host_memory_is_refused(calls):
+    with pytest.MonkeyPatch.context() as m:
+        m.setattr(u, "_new", lambda shape, dtype, device, stream: torch.empty(shape, dtype=dtype))
+        with pytest.raises(ValueError):
+            u.rope_table(9, 64, device="cpu")
+    assert calls == []
