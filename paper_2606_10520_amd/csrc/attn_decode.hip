@@ -2,8 +2,10 @@
 //
 //   s_t = scale (q . k_t),  p_t = exp(s_t - m),  out = sum_t p_t v_t / sum_t p_t
 //
-// Bound: HBM (every key and value is read once, for two products of at most
-// sixteen rows).  So nothing is staged: a wave reads 32 tokens at a time
+// Bound: HBM (keys and values are read for two products of at most sixteen rows:
+// once where the new tokens times the heads that share a key head are sixteen or
+// fewer, else once for every sixteen of them).  So nothing is staged: a wave
+// reads 32 tokens at a time
 // straight into the registers that the matrix cores take their operands from,
 // and the products are arranged so that this works without moving data
 // between lanes:
@@ -53,12 +55,15 @@
 // when a score exceeds it by 2^8 (the weights then stay inside f16), so most tiles
 // need no exchange between lanes and no rescaling.
 //
-// Measured, with the launch that joins: 4 x 32768 tokens of 4-bit cache, 32
-// heads, 122 us (4.7 TB/s); 4 x 16384 of 8-bit 94 us (5.9 TB/s); 4 x 8192 of
-// f16 87 us (6.2 TB/s); one sequence of 1001 tokens of f16 10.5 us, of which
-// the first launch takes 7 and the second 4: 1 us to find the share, 2.6 until
-// the queries and the first tile are there, 1.4 for a tile, 0.8 to join the
-// waves; 512 tokens 8.8 us, one launch with whole items.
+// Measured a call among others, with the launch that joins: 4 x 32768 tokens of
+// 4-bit cache, 32 heads, 117 us (4.9 TB/s); 4 x 16384 of 8-bit 94 us (5.9 TB/s);
+// 4 x 8192 of f16 87 us (6.1 TB/s), where a plain read has 7.1 TB/s: the order is
+// that of the bytes that a wave has under way, a tile of 4.5, 8 or 16 KB.  Rows
+// beyond sixteen: 16 x 8192 tokens of 8-bit cache, 64 heads on 8, 53 us for one
+// new token and 97 us for four, whose 32 rows read everything twice.  One sequence
+// of 1001 tokens of f16, 32 heads: launches of 8.5 and 3.9 us, in the first 1 us to
+// find the share, 2.6 until the queries and the first tile are there, 1.4 for a
+// tile, 0.8 to join the waves; 512 tokens 9.0 us, one launch with whole items.
 #include <algorithm>
 #include <cfloat>
 

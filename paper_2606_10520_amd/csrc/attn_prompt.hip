@@ -26,20 +26,20 @@
 // before one in its vector work (16384 tokens of 32 heads 1.90 ms for 2.00; the
 // other way round 2.01).
 //
-// 16384 tokens of 32 heads of 128, causal: 1.90 ms, 1155 TFLOP/s, matrix cores
-// busy 71% of the cycles at a clock of 1.6 GHz (8192^3 library products under
-// the same power: 1280-1560 TFLOP/s at 86-90%).  2048 tokens: 54 us, of which
-// 4 us pass before the first products (512 workgroups ask for all of q at
-// once), 3-4 us with the first two tiles, and the rest with tiles of 1.1 us for a
-// workgroup alone on its CU, 0.93 us for each of two.  64 on 8 heads, 8 prompts
-// of 1 to 1500 tokens: 70-73 us, three workgroups in turn on each place, and
-// for each 5 us before its first product and 4 from its last to the next one's
-// start.  Slower were: one wave a SIMD with three tiles
-// under way (8192 tokens 1270 us for 980: a lone wave issues at most one
-// instruction in four to five cycles), eight waves that take turns at products
-// and vector work, a tile's weights between the next tile's products (2.10 ms
-// for 1.95, 2048 tokens 62 us for 54), and sums of weights by dot products (2.09
-// ms for 2.00).
+// 16384 tokens of 32 heads of 128, causal: 1.90 ms (1.96 on another card), 1155
+// TFLOP/s, matrix cores busy 67-71% of the cycles at up to 1.6 GHz (8192^3
+// library products under the same power: 1280-1560 TFLOP/s at 86-90%).  2048
+// tokens: 51 us, of which 4 us pass before the first products (512 workgroups ask
+// for all of q at once), 3-4 us with the first two tiles, and the rest with tiles
+// of 1.1 us for a workgroup alone on its CU, 0.93 us for each of two.  64 on 8
+// heads, 8 prompts of 1 to 1500 tokens: 75 us, three workgroups in turn on each
+// place, and for each 5 us before its first product and 4 from its last to the
+// next one's start.  Slower were (against the form of the time): one wave a SIMD
+// with three tiles under way (8192 tokens 1270 us for 980: a lone wave issues at
+// most one instruction in four to five cycles), eight waves that take turns at
+// products and vector work, a tile's weights between the next tile's products
+// (2.10 ms for 1.95, 2048 tokens 62 us for 54), and sums of weights by dot
+// products (2.09 ms for 2.00).
 #include <algorithm>
 #include <cfloat>
 
@@ -558,7 +558,9 @@ int64_t prompt_blocks(int64_t sequences, int64_t q_tokens, int q_heads, int kv_h
 // Few rows before many keys: the keys are split, so that there are up to two
 // workgroups a CU, if that is expected to take less time than it costs.  A tile
 // of keys takes a workgroup about 1.1 us, the launch that joins the parts 5 us
-// and what their sums (written and read) take at 3.5 TB/s.  Of a batch's
+// and what their sums (written and read) take at 3.5 TB/s.  (These are measured
+// with head_dim 128, and taken for 64 too, where a tile costs less: 2048 tokens of
+// 32 heads 36 us for 51.)  Of a batch's
 // lengths only the mean is known here: its longest sequence is taken to have
 // twice that.
 int prompt_splits(int64_t sequences, int64_t q_tokens, int64_t k_tokens, int q_heads, int kv_heads, int head_dim) {

@@ -127,15 +127,17 @@ __device__ inline void store_entry(uint8_t* pool, uint32_t* scales, int64_t e, b
 
 // A block: one head of kThreads / LANES tokens, a thread sixteen dims.
 // Neighbouring threads are neighbouring tokens of the head because that is what
-// lies together in a page: codes go out in whole lines and a block's scales are
-// one line, where a token's heads side by side would leave 64-byte and 4-byte
-// pieces to different dies' caches.
+// lies together in a page: a block's codes are whole lines (each of its two
+// stores writes halves of the rows) and its scales are one line, where a token's
+// heads side by side would leave 64-byte and 4-byte pieces to different dies'
+// caches.
 //
-// 2048 tokens of 64 + 2 * 8 heads into 8-bit pages: 18.5 us, 4.3 TB/s; 2000
-// tokens of 3 * 32 heads into 4-bit pages: 23 us, 3.2 TB/s.  A thread waits for
-// its position and then for its table row and page, so what is left is waves
-// that start and wait; two heads a thread take as long, four 1-2 us longer
-// (fewer waves fit).
+// 2048 tokens of 64 + 2 * 8 heads into 8-bit pages: 17.6 us, 4.5 TB/s; 2000
+// tokens of 3 * 32 heads into 4-bit pages: 23 us, 3.2 TB/s.  In both a thread
+// waits for its position and then for its table row and page; two heads a thread
+// take as long, four 1-2 us longer (fewer waves fit).  What holds the 4-bit form
+// below the 8-bit one is not known; its stores are of 4 bytes a lane, in 32-byte
+// halves of rows of 64.
 template <int KIND, int D, typename T>
 __global__ __launch_bounds__(kThreads) void append_kernel(Append a) {
     constexpr int LANES = D / 16;
