@@ -220,17 +220,17 @@ def _own(s):
     if op == "product":
         if len(s["weights"]) == 1:
             w = s["weights"][0]
-            return [u.w4_gemm(w["packed"], w["N"], w["K"], s["x"], out_dtype=DTYPE[case["out"]])]
-        return u.w4_gemm_batched([(w["packed"], w["N"], w["K"], s["x"], None) for w in s["weights"]],
+            return [u.fourbit_gemm(w["packed"], w["N"], w["K"], s["x"], out_dtype=DTYPE[case["out"]])]
+        return u.fourbit_gemm_batched([(w["packed"], w["N"], w["K"], s["x"], None) for w in s["weights"]],
                                  out_dtype=DTYPE[case["out"]])
     kept = torch.int8 if case["i8"] else dtype
     y, h = u.rmsnorm(s["x"], s["norm"], EPS, residual=s["residual"], out_dtype=kept)
-    outs = u.w4_gemm_batched([(w["packed"], w["N"], w["K"], y, None) for w in s["weights"]], out_dtype=dtype)
+    outs = u.fourbit_gemm_batched([(w["packed"], w["N"], w["K"], y, None) for w in s["weights"]], out_dtype=dtype)
     if op == "block":
         return {"h": h, "outs": outs}
     a = u.gated(*outs, case["act"], out_dtype=kept)
     w = s["down"]
-    return {"h": h, "y": u.w4_gemm(w["packed"], w["N"], w["K"], a, out_dtype=dtype)}
+    return {"h": h, "y": u.fourbit_gemm(w["packed"], w["N"], w["K"], a, out_dtype=dtype)}
 
 
 def run(state):
