@@ -138,7 +138,8 @@ typedef enum {
 typedef enum {
     UNISVQ_F16 = 0,   /* IEEE binary16 */
     UNISVQ_BF16 = 1,  /* bfloat16 */
-    UNISVQ_F32 = 2    /* IEEE binary32 (outputs only) */
+    UNISVQ_F32 = 2,   /* IEEE binary32 (outputs only) */
+    UNISVQ_I8 = 3     /* signed bytes with a scale a row (only where an entry point names it) */
 } unisvq_dtype;
 
 /* Library and format version (UNISVQ_FORMAT_VERSION). */
@@ -753,6 +754,121 @@ int unisvq_attn_prompt(int64_t sequences, int64_t q_tokens, int64_t k_tokens, co
                        int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride, int dtype,
                        int causal, float scale, void* out, int64_t out_token_stride, int64_t out_head_stride,
                        float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- A decoder layer's rows: norm and gated activations ----
+ * Rows of activations are given as (pointer, row stride in elements): element
+ * i of row t is at t * stride + i.  Such pointers are 16-byte aligned and their
+ * strides multiples of 8 elements, row lengths n multiples of 8 (UNISVQ_EALIGN,
+ * UNISVQ_EUNSUP otherwise).
+ * An output of type UNISVQ_I8 is bytes with one fp32 scale a row (scales[t], row
+ * t): value = code * scale, scale = a / 127 with a the row's largest magnitude
+ * in fp32, code = round-to-even(v * (1 / scale)).  a < 1e-30: scale 0 and codes
+ * 0.  Inf or NaN in the row: scale NaN and codes 0.  (The rule of an I8 cache.)
+ * n is at most 65536 where an output is bytes. */
+
+/* Root-mean-square norm with the residual's addition:
+ *   h = x + r                                 (h = x without a residual stream)
+ *   y = h / sqrt(mean(h^2) + eps) * (w + weight_offset)
+ * in fp32; h is rounded to the stream's type before it is normalised, so a later
+ * layer that reads it sees what this one saw.  y is rounded once.
+ *   tokens        >= 0; n 8..65536, a multiple of 8
+ *   x             device [tokens][n], F16 or BF16
+ *   weight        device [n], contiguous, x_dtype or F32, 16-byte aligned
+ *   weight_offset 0, or 1 for weights that are kept as differences from one
+ *   eps           above 0
+ *   residual      the stream, device [tokens][n], x_dtype or F32, or NULL;
+ *   residual_out  the stream after the addition, same type: NULL exactly where
+ *                 residual is.  May be residual, or x where the types are the
+ *                 same, each with the same stride, and may not overlap an input
+ *                 otherwise
+ *   y             device [tokens][n], x_dtype, F32 or I8; may be x or residual
+ *                 on the same terms, and not residual_out
+ *   y_scales      device fp32 [tokens] for I8, ignored otherwise
+ * A row whose squares' sum passes fp32's range (magnitudes of 10^18) gives zeros. */
+int unisvq_rmsnorm(int64_t tokens, int64_t n, const void* x, int64_t x_stride, int x_dtype, const void* weight,
+                   int weight_dtype, float weight_offset, float eps, const void* residual, int64_t residual_stride,
+                   void* residual_out, int64_t residual_out_stride, int residual_dtype, void* y, int64_t y_stride,
+                   int y_dtype, float* y_scales, void* stream);
+
+typedef enum {
+    UNISVQ_SILU = 0, /* g / (1 + exp(-g)) */
+    UNISVQ_GELU = 1  /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 */
+} unisvq_activation;
+
+/* Gated activation y = act(gate) * up, in fp32, rounded once.
+ *   tokens    >= 0; tokens * n below 2^34 (UNISVQ_EUNSUP otherwise)
+ *   gate, up  device [tokens][n], F16 or BF16 (the two outputs of a gate and up
+ *             product, or the halves of one fused row)
+ *   y         device [tokens][n], x_dtype, F32 or I8; may be gate or up with the
+ *             same type and stride, and may not overlap them otherwise
+ *   y_scales  device fp32 [tokens] for I8, ignored otherwise */
+int unisvq_gated(int64_t tokens, int64_t n, const void* gate, int64_t gate_stride, const void* up, int64_t up_stride,
+                 int x_dtype, int activation, void* y, int64_t y_stride, int y_dtype, float* y_scales, void* stream);
+
+/* ---- Products with 4-bit weights ----
+ * One fp16 scale for each row and group of 128 columns, codes c in 0..15:
+ *   w_hat[n][k] = S[n][k / 128] * (c[n][k] - 8)
+ * Packed: tiles of 16 rows x 128 columns, [row block][group], 1 KB each: slot s
+ * = 0..63 (16 bytes) is row s % 16 and chunk s / 16; its 32-bit word j = 0..3
+ * holds columns 64 (j / 2) + 16 (s / 16) + 8 (j % 2) + 0..7, byte b having column
+ * b in its low and column 4 + b in its high half.  Behind all tiles the scales:
+ * for every row block and four groups 128 bytes, 8 a row (its groups' fp16
+ * scales, zeros behind the last group).  A slot is one lane's operands of either
+ * width of activations, so every load is a coalesced 16-byte-per-lane read.
+ * Shapes: N % 16 == 0, K % 128 == 0; K to 2^20 (UNISVQ_EUNSUP above). */
+
+/* Bytes of the packed buffer, N*K/2 + N*8*ceil(K/512); 0 for an invalid shape.
+ * Host-only. */
+size_t unisvq_fourbit_bytes(int64_t N, int64_t K);
+
+/* Pack codes uint8 [N][K] and scales fp16 bits [N][K/128] (device) into packed
+ * (device, unisvq_fourbit_bytes(N, K) bytes, 16-byte aligned).  bad_codes: as
+ * unisvq_pack (codes above 15 counted, stored modulo 16).  Bit exact. */
+int unisvq_fourbit_pack(int64_t N, int64_t K, const uint8_t* codes, const uint16_t* scales, void* packed,
+                   int32_t* bad_codes, void* stream);
+
+/* Exact inverse of unisvq_fourbit_pack.  All device. */
+int unisvq_fourbit_unpack(int64_t N, int64_t K, const void* packed, uint8_t* codes, uint16_t* scales, void* stream);
+
+/* Round weights to 4 bits and pack them: for each row's group S = fp16(a / 7), a
+ * its largest magnitude (S at most 65504), and c - 8 = round-to-even(w / S)
+ * within -8..7.  S = 0: codes 8.  Inf or NaN in a group: S NaN, codes 8.
+ *   W  device [N][K] contiguous, F16, BF16 or F32, 16-byte aligned */
+int unisvq_fourbit_quantize(int64_t N, int64_t K, const void* W, int w_dtype, void* packed, void* stream);
+
+/* y = x W_hat^T for any M >= 1, from single tokens to prompts.
+ *   x         device [M][K] contiguous, 16-byte aligned: F16, BF16, or I8 with
+ *             x_scales device fp32 [M] (a token's value = code * scale, as
+ *             unisvq_rmsnorm and unisvq_gated give them).  x_scales is NULL for
+ *             the 16-bit types (UNISVQ_EINVAL otherwise, and for I8 without them)
+ *   y         device [M][N] contiguous, F16, BF16 or F32, whatever x is
+ *   workspace device, >= unisvq_fourbit_gemm_workspace_bytes(N, K, M, x_dtype) bytes,
+ *             16-byte aligned (UNISVQ_EWORKSPACE / UNISVQ_EALIGN); may be NULL
+ *             when that size is 0.  Overwritten
+ * Codes are exact operands of the matrix cores; a group's sum is fp32 (I8: an
+ * exact integer), multiplied by its scale in fp32; y is rounded once.  Sums are
+ * added in an order that depends on shapes alone: results are reproducible bit
+ * for bit.  A token with an Inf or NaN among its activations gets NaN. */
+size_t unisvq_fourbit_gemm_workspace_bytes(int64_t N, int64_t K, int64_t M, int x_dtype);
+int unisvq_fourbit_gemm(int64_t N, int64_t K, const void* packed, int64_t M, const void* x, int x_dtype,
+                   const float* x_scales, void* y, int y_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One product of a batched call. */
+typedef struct {
+    int64_t N, K;
+    const void* packed;     /* device, packed 4-bit N x K matrix, 16-byte aligned */
+    const void* x;          /* device [M][K], 16-byte aligned */
+    const float* x_scales;  /* device fp32 [M] for I8, else NULL */
+    void* y;                /* device [M][N] */
+} unisvq_fourbit_problem;
+
+/* Several independent products of the same M and types (a layer's q, k and v, or
+ * gate and up) in one launch.  problems: HOST array of 1..UNISVQ_MAX_BATCH
+ * descriptors, read before the call returns, all validated before anything is
+ * enqueued. */
+size_t unisvq_fourbit_gemm_batched_workspace_bytes(const unisvq_fourbit_problem* problems, int count, int64_t M, int x_dtype);
+int unisvq_fourbit_gemm_batched(const unisvq_fourbit_problem* problems, int count, int64_t M, int x_dtype, int y_dtype,
+                           void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- Bandwidth reference (not part of the method) ----
  * A plain read of `count` device byte ranges in one launch, with the 16-byte

@@ -1,0 +1,147 @@
+// Root-mean-square norm with the residual's addition on gfx950.
+//   h = x + r, rounded to the stream's type (h = x without a stream)
+//   y = h / sqrt(mean(h^2) + eps) * (w + offset), as 16 bits, fp32, or 8 bits
+//   with a scale a row
+#include <algorithm>
+
+#include "layer.hpp"
+
+namespace unisvq {
+namespace {
+
+// Bound by memory: x, r, h and y pass once, so a row stays in registers from its
+// loads to its stores, V runs of eight a thread.  WIDE: a workgroup a row, else
+// 2^steps lanes of a wave.  Runs past the row's end read its last run again and
+// count as zeros, so that no load waits behind a branch.
+template <typename T, int V, bool WIDE>
+__global__ __launch_bounds__(WIDE ? 1024 : 256) void norm_kernel(NormArgs a, int steps) {
+    __shared__ float sums[16];
+    __shared__ uint32_t tops[16];
+    const int lanes = WIDE ? blockDim.x : 1 << steps;
+    const int lane = WIDE ? threadIdx.x : threadIdx.x & (lanes - 1);
+    const int64_t rows = WIDE ? 1 : 256 >> steps;
+    const int64_t t0 = WIDE ? blockIdx.x : blockIdx.x * rows + (threadIdx.x >> steps);
+    const int runs = a.n / 8;
+    for (int64_t t = t0; WIDE ? t < a.tokens : t - (threadIdx.x >> steps) < a.tokens; t += gridDim.x * rows) {
+        const bool there = WIDE || t < a.tokens;  // (lanes of rows past the end go along, and store nothing)
+        const int64_t tt = there ? t : a.tokens - 1;
+        float h[V][8];
+        int at[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            at[v] = 8 * min(lane + v * lanes, runs - 1);
+            load8(static_cast<const T*>(a.x) + tt * a.x_stride + at[v], h[v]);
+        }
+        float w[V][8];
+        if (a.w_dtype == UNISVQ_F32) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) load8(static_cast<const float*>(a.w) + at[v], w[v]);
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) load8(static_cast<const T*>(a.w) + at[v], w[v]);
+        }
+        if (a.r) {
+            float r[V][8];
+            if (a.r_dtype == UNISVQ_F32) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) load8(static_cast<const float*>(a.r) + tt * a.r_stride + at[v], r[v]);
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) h[v][i] += r[v][i];
+            } else {
+#pragma unroll
+                for (int v = 0; v < V; ++v) load8(static_cast<const T*>(a.r) + tt * a.r_stride + at[v], r[v]);
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) h[v][i] = static_cast<float>(static_cast<T>(h[v][i] + r[v][i]));
+            }
+            // (in place: every thread has read what it overwrites)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (there && lane + v * lanes < runs)
+                    store_row8<T>(a.h, t * a.h_stride + at[v], h[v], a.r_dtype == UNISVQ_F32);
+        }
+        float sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const bool in = lane + v * lanes < runs;
+            float s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s = fmaf(h[v][i], h[v][i], s);
+            sum += in ? s : 0.0f;
+        }
+        const auto add = [](float p, float q) { return p + q; };
+        if constexpr (WIDE)
+            sum = over_block(sum, sums, add);
+        else
+            sum = over_lanes(sum, steps, add);
+        const float f = __builtin_amdgcn_rsqf(sum / static_cast<float>(a.n) + a.eps);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[v][i] = h[v][i] * f * (w[v][i] + a.offset);
+        if (a.y_dtype != UNISVQ_I8) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (there && lane + v * lanes < runs)
+                    store_row8<T>(a.y, t * a.y_stride + at[v], h[v], a.y_dtype == UNISVQ_F32);
+        } else {
+            // (runs past the end are copies of the row's last: they change no maximum)
+            uint32_t most = 0;
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) most = max(most, magnitude(h[v][i]));
+            const auto larger = [](uint32_t p, uint32_t q) { return max(p, q); };
+            if constexpr (WIDE)
+                most = over_block(most, tops, larger);
+            else
+                most = over_lanes(most, steps, larger);
+            const RowScale k = row_scale(most);
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (there && lane + v * lanes < runs)
+                    *reinterpret_cast<uint2*>(static_cast<int8_t*>(a.y) + t * a.y_stride + at[v]) = codes_of(h[v], k.inv);
+            if (there && lane == 0) a.scales[t] = k.scale;
+        }
+        if constexpr (WIDE) __syncthreads();  // (the words of LDS serve the next row)
+    }
+}
+
+template <typename T>
+void launch(const NormArgs& a, hipStream_t s) {
+    constexpr int64_t kMostBlocks = 1 << 20;  // the rest of the rows in turn
+    const int runs = a.n / 8;
+    if (runs <= 64) {
+        int steps = 3;
+        while ((1 << steps) < runs) ++steps;
+        const int64_t rows = 256 >> steps;
+        const uint32_t blocks = static_cast<uint32_t>(std::min((a.tokens + rows - 1) / rows, kMostBlocks));
+        norm_kernel<T, 1, false><<<blocks, 256, 0, s>>>(a, steps);
+        return;
+    }
+    const uint32_t blocks = static_cast<uint32_t>(std::min(a.tokens, kMostBlocks));
+    const auto threads = [&](int v) { return static_cast<uint32_t>((runs + 64 * v - 1) / (64 * v) * 64); };
+    if (runs <= 1024)
+        norm_kernel<T, 1, true><<<blocks, threads(1), 0, s>>>(a, 0);
+    else if (runs <= 2048)
+        norm_kernel<T, 2, true><<<blocks, threads(2), 0, s>>>(a, 0);
+    else if (runs <= 4096)
+        norm_kernel<T, 4, true><<<blocks, threads(4), 0, s>>>(a, 0);
+    else
+        norm_kernel<T, 8, true><<<blocks, threads(8), 0, s>>>(a, 0);
+}
+
+}  // namespace
+
+hipError_t launch_rmsnorm(const NormArgs& a, hipStream_t s) {
+    if (a.x_dtype == UNISVQ_F16)
+        launch<_Float16>(a, s);
+    else
+        launch<__bf16>(a, s);
+    return hipGetLastError();
+}
+
+}  // namespace unisvq

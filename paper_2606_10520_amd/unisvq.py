@@ -15,7 +15,7 @@ import os
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libunisvq.so")
 
-F16, BF16, F32 = 0, 1, 2
+F16, BF16, F32, I8 = 0, 1, 2, 3
 GROUP, DIM, ROW_BLOCK = 128, 4, 16
 
 STATUS = {0: "UNISVQ_OK", -1: "UNISVQ_EINVAL", -2: "UNISVQ_ESHAPE", -3: "UNISVQ_EUNSUP",
@@ -34,7 +34,9 @@ EXPORTS = ("unisvq_version", "unisvq_status_string", "unisvq_packed_bytes", "uni
            "unisvq_gemm_noalloc", "unisvq_gemm_batched_workspace_bytes", "unisvq_gemm_batched",
            "unisvq_rope_table", "unisvq_rope", "unisvq_cache_append", "unisvq_cache_read",
            "unisvq_attn_decode_workspace_bytes", "unisvq_attn_decode", "unisvq_attn_prompt_workspace_bytes",
-           "unisvq_attn_prompt")
+           "unisvq_attn_prompt", "unisvq_rmsnorm", "unisvq_gated", "unisvq_fourbit_bytes", "unisvq_fourbit_pack", "unisvq_fourbit_unpack",
+           "unisvq_fourbit_quantize", "unisvq_fourbit_gemm_workspace_bytes", "unisvq_fourbit_gemm",
+           "unisvq_fourbit_gemm_batched_workspace_bytes", "unisvq_fourbit_gemm_batched")
 # format variants: (bits, d) pairs served by the unisvq_var_* entry points
 VARIANTS = ((3, 4), (2, 8), (3, 8))
 MAX_BATCH = 8
@@ -65,6 +67,12 @@ class Cache(ctypes.Structure):
     _fields_ = [("pages", ctypes.c_int64), ("page_tokens", ctypes.c_int64), ("kv_heads", ctypes.c_int64),
                 ("head_dim", ctypes.c_int64), ("kind", ctypes.c_int), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
                 ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
+
+
+class FourbitProblem(ctypes.Structure):
+    """Mirror of unisvq_fourbit_problem."""
+    _fields_ = [("N", ctypes.c_int64), ("K", ctypes.c_int64), ("packed", ctypes.c_void_p), ("x", ctypes.c_void_p),
+                ("x_scales", ctypes.c_void_p), ("y", ctypes.c_void_p)]
 
 
 class UniSVQLibraryMissing(RuntimeError):
@@ -189,6 +197,26 @@ def load():
     lib.unisvq_attn_prompt.argtypes = [i64, i64, i64, p, p, i64, i64, i64, *rows, *rows, *rows, i32, i32, f32, *rows, p,
                                        p, sz, p]
     lib.unisvq_attn_prompt.restype = i32
+    lib.unisvq_rmsnorm.argtypes = [i64, i64, p, i64, i32, p, i32, f32, f32, p, i64, p, i64, i32, p, i64, i32, p, p]
+    lib.unisvq_rmsnorm.restype = i32
+    lib.unisvq_gated.argtypes = [i64, i64, p, i64, p, i64, i32, i32, p, i64, i32, p, p]
+    lib.unisvq_gated.restype = i32
+    lib.unisvq_fourbit_bytes.argtypes = [i64, i64]
+    lib.unisvq_fourbit_bytes.restype = sz
+    lib.unisvq_fourbit_pack.argtypes = [i64, i64, p, p, p, p, p]
+    lib.unisvq_fourbit_pack.restype = i32
+    lib.unisvq_fourbit_unpack.argtypes = [i64, i64, p, p, p, p]
+    lib.unisvq_fourbit_unpack.restype = i32
+    lib.unisvq_fourbit_quantize.argtypes = [i64, i64, p, i32, p, p]
+    lib.unisvq_fourbit_quantize.restype = i32
+    lib.unisvq_fourbit_gemm_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    lib.unisvq_fourbit_gemm_workspace_bytes.restype = sz
+    lib.unisvq_fourbit_gemm.argtypes = [i64, i64, p, i64, p, i32, p, p, i32, p, sz, p]
+    lib.unisvq_fourbit_gemm.restype = i32
+    lib.unisvq_fourbit_gemm_batched_workspace_bytes.argtypes = [ctypes.POINTER(FourbitProblem), i32, i64, i32]
+    lib.unisvq_fourbit_gemm_batched_workspace_bytes.restype = sz
+    lib.unisvq_fourbit_gemm_batched.argtypes = [ctypes.POINTER(FourbitProblem), i32, i64, i32, i32, p, sz, p]
+    lib.unisvq_fourbit_gemm_batched.restype = i32
     _lib = lib
     return lib
 
@@ -1155,3 +1183,212 @@ def attn_prompt(q, k, v, cu_q, cu_k, causal: bool = True, scale: float | None = 
             _halves()[q.dtype], causal, head_dim ** -0.5 if scale is None else scale, *orr,
             _words(lse, tokens * q_heads, "lse", torch.float32, device), wp, size)
     return out
+
+
+# ---- a decoder layer's rows: norm and gated activations ----
+
+_TYPES = {}  # the dtypes of rows and outputs and their codes, once torch is there
+
+
+def _types():
+    if not _TYPES:
+        torch = _torch()
+        _TYPES.update({torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32, torch.int8: I8})
+    return _TYPES
+
+
+def _flat(t, what: str, device: int, shape=None, dtypes=None):
+    """A [tokens][n] device tensor of one of dtypes (None: fp16 or bf16), its last axis contiguous (the C entry refuses row
+    strides that are not multiples of 8): checked, and as (pointer, row stride)."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1) or (shape is not None and t.shape != shape):
+        raise ValueError(f"{what} must be [tokens][n]{'' if shape is None else ' ' + str(tuple(shape))} with contiguous rows, "
+                         f"got {tuple(t.shape)}, strides {t.stride()}")
+    if t.dtype not in (_halves() if dtypes is None else dtypes):
+        raise TypeError(f"{what} is {t.dtype}, expected {'fp16 or bf16' if dtypes is None else ' or '.join(map(str, dtypes))}")
+    if t.get_device() != device or device < 0:
+        _elsewhere(t, what, device)
+    return t.data_ptr(), t.stride(0)
+
+
+def _row_output(out, out_dtype, like, device: int, stream):
+    """The caller's out (a tensor, or a pair of bytes and scales) or a new one of out_dtype (None: like's): out itself,
+    (pointer, row stride), its type's code, and the pointer of its scales."""
+    torch = _torch()
+    tokens, n = like.shape
+    if out is None:
+        dt = out_dtype or like.dtype
+        out = _new((tokens, n), dt, like.device, stream)
+        if dt is torch.int8:
+            out = out, _new((tokens,), torch.float32, like.device, stream)
+    pair = type(out) in (tuple, list)
+    y, scales = out if pair else (out, None)
+    if y.dtype not in _types() or (out_dtype is not None and y.dtype is not out_dtype) or (y.dtype is torch.int8) != pair:
+        raise TypeError("out is fp16, bf16 or fp32 rows, or a pair of int8 rows and fp32 scales; and of out_dtype where that is given")
+    rows = _flat(y, "out", device, like.shape, (y.dtype,))
+    return out, rows, _TYPES[y.dtype], _words(scales, tokens, "the scales of out", torch.float32, device)
+
+
+def rmsnorm(x, weight, eps: float = 1e-5, residual=None, residual_out=None, weight_offset: float = 0.0, out=None,
+            out_dtype=None, stream=None):
+    """Root-mean-square norm of rows x [tokens][n] (fp16 or bf16) by weight [n] (x's type or fp32) + weight_offset, after
+    the addition of residual [tokens][n] (x's type or fp32) where it is given.  Returns y, or with a residual (y, h), h =
+    x + residual of residual's type (residual_out, which may be residual or x, or a new tensor).  y is of out_dtype: x's
+    (None), fp32, or int8, and then a pair (codes, scales) that fourbit_gemm takes; out: a tensor or pair to write."""
+    torch = _torch()
+    device = x.get_device()
+    xr = _flat(x, "x", device)
+    wide = (x.dtype, torch.float32)
+    if weight.dtype not in wide:
+        raise TypeError(f"weight is {weight.dtype}, expected {wide[0]} or fp32")
+    wp = _words(weight, x.shape[1], "weight", weight.dtype, device)
+    rr, hr, rt = (None, 0), (None, 0), F32
+    if residual is not None:
+        rr = _flat(residual, "residual", device, x.shape, wide)
+        if residual_out is None:
+            residual_out = _new(x.shape, residual.dtype, x.device, stream)
+        hr, rt = _flat(residual_out, "residual_out", device, x.shape, (residual.dtype,)), _types()[residual.dtype]
+    elif residual_out is not None:
+        raise ValueError("residual_out without a residual")
+    out, yr, yt, scales = _row_output(out, out_dtype, x, device, stream)
+    _launch("unisvq_rmsnorm", device, stream, *x.shape, *xr, _types()[x.dtype], wp, _TYPES[weight.dtype], weight_offset,
+            eps, *rr, *hr, rt, *yr, yt, scales)
+    return out if residual is None else (out, residual_out)
+
+
+ACTIVATIONS = {"silu": 0, "gelu": 1}
+
+
+def gated(gate, up, activation: str = "silu", out=None, out_dtype=None, stream=None):
+    """act(gate) * up of rows [tokens][n] (fp16 or bf16, any row strides, so the halves of one fused row serve); activation
+    "silu" or "gelu" (its tanh form).  out, out_dtype: as rmsnorm's; out may be gate or up."""
+    device = gate.get_device()
+    gr = _flat(gate, "gate", device)
+    ur = _flat(up, "up", device, gate.shape, (gate.dtype,))
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, got {activation!r}")
+    out, yr, yt, scales = _row_output(out, out_dtype, gate, device, stream)
+    _launch("unisvq_gated", device, stream, *gate.shape, *gr, *ur, _types()[gate.dtype], ACTIVATIONS[activation], *yr, yt,
+            scales)
+    return out
+
+
+# ---- products with 4-bit weights ----
+
+def fourbit_bytes(N: int, K: int) -> int:
+    return load().unisvq_fourbit_bytes(N, K)
+
+
+def _fourbit_new(out, N: int, K: int, like, stream):
+    need = fourbit_bytes(N, K)
+    if not need:
+        raise ValueError(f"4-bit weights are N x K with N % 16 == 0, K % 128 == 0 and K to 2^20, got {N} x {K}")
+    if out is None:
+        out = _new((need,), _torch().uint8, like.device, stream)
+    _need_buffer(out, need, "out", exact=True)
+    if out.get_device() != like.get_device():
+        _elsewhere(out, "out", like.get_device())
+    return out
+
+
+def fourbit_pack(codes, scales, out=None, bad_codes=None, stream=None):
+    """codes uint8 [N][K] (0..15), scales fp16 [N][K/128] -> packed uint8 bytes of weights scales * (codes - 8)."""
+    torch = _torch()
+    device = codes.get_device()
+    if codes.dim() != 2:
+        raise ValueError("codes must be [N][K]")
+    N, K = codes.shape
+    out = _fourbit_new(out, N, K, codes, stream)
+    _launch("unisvq_fourbit_pack", device, stream, N, K, _words(codes, N * K, "codes", torch.uint8, device),
+            _words(scales, N * (K // GROUP), "scales", torch.float16, device), out.data_ptr(),
+            _words(bad_codes, 1, "bad_codes", torch.int32, device))
+    return out
+
+
+def fourbit_unpack(packed, N: int, K: int, stream=None):
+    """Inverse of fourbit_pack: (codes uint8 [N][K], scales fp16 [N][K/128])."""
+    torch = _torch()
+    device = packed.get_device()
+    _fourbit_new(packed, N, K, packed, stream)
+    codes = _new((N, K), torch.uint8, packed.device, stream)
+    scales = _new((N, K // GROUP), torch.float16, packed.device, stream)
+    _launch("unisvq_fourbit_unpack", device, stream, N, K, packed.data_ptr(), codes.data_ptr(), scales.data_ptr())
+    return codes, scales
+
+
+def fourbit_quantize(W, out=None, stream=None):
+    """Contiguous weights W [N][K] (fp16, bf16 or fp32) rounded to 4 bits with a scale for each row and 128 columns, packed."""
+    torch = _torch()
+    device = W.get_device()
+    if W.dim() != 2 or W.dtype not in (torch.float16, torch.bfloat16, torch.float32):
+        raise ValueError(f"W must be [N][K] of fp16, bf16 or fp32, got {W.dtype} {tuple(W.shape)}")
+    N, K = W.shape
+    out = _fourbit_new(out, N, K, W, stream)
+    _launch("unisvq_fourbit_quantize", device, stream, N, K, _words(W, N * K, "W", W.dtype, device), _types()[W.dtype],
+            out.data_ptr())
+    return out
+
+
+def fourbit_gemm_workspace_bytes(N: int, K: int, M: int, x_dtype) -> int:
+    """Workspace bytes unisvq_fourbit_gemm needs for activations of the torch dtype x_dtype (int8 for pairs)."""
+    return load().unisvq_fourbit_gemm_workspace_bytes(N, K, M, _types()[x_dtype])
+
+
+@functools.lru_cache(maxsize=4096)
+def _fourbit_workspace(shapes, M: int, code: int) -> int:
+    arr = (FourbitProblem * len(shapes))(*((N, K, None, None, None, None) for N, K in shapes))
+    return load().unisvq_fourbit_gemm_batched_workspace_bytes(arr, len(shapes), M, code)
+
+
+def fourbit_gemm_batched(problems, out_dtype=None, workspace=None, stream=None):
+    """Several products y = x W^T with 4-bit weights in one launch: problems is a sequence of (packed, N, K, x, out-or-None)
+    of the same token count and types.  x is [M][K] fp16 or bf16, or a pair (codes int8 [M][K], scales fp32 [M]) as
+    rmsnorm and gated return them.  out_dtype: fp16, bf16 or fp32 (None: x's type, fp16 for a pair).  Returns the list of
+    outputs [M][N]."""
+    torch = _torch()
+    count = len(problems)
+    if not 1 <= count <= MAX_BATCH:
+        raise ValueError(f"1..{MAX_BATCH} problems per call")
+    arr = (FourbitProblem * count)()
+    outs, shapes = [], []
+    device = problems[0][0].get_device()
+    M = kind = None
+    for i, (packed, N, K, x, out) in enumerate(problems):
+        pair = type(x) in (tuple, list)
+        v, scales = x if pair else (x, None)
+        if M is None:
+            M, kind = v.numel() // max(K, 1), v.dtype
+            if (kind is not torch.int8 if pair else kind not in _halves()):
+                raise TypeError(f"activations are fp16, bf16, or a pair of int8 codes and fp32 scales, got {kind}{' in a pair' if pair else ''}")
+            if M < 1:
+                raise ValueError("x holds no tokens")
+        if v.dtype is not kind or pair is not (kind is torch.int8):
+            raise ValueError("all problems need the same activation type")
+        xp = _words(v, M * K, f"x of {M} tokens", kind, device)
+        if v.shape[-1] != K:
+            raise ValueError(f"x has {v.shape[-1]} columns, the weights K = {K}")
+        shapes.append((N, K))
+        pp = _words(packed, _fourbit_size(N, K), "packed", torch.uint8, device)
+        if out is None:
+            out = _new((M, N), out_dtype or (torch.float16 if pair else kind), v.device, stream)
+        elif out_dtype is not None and out.dtype is not out_dtype:
+            raise TypeError(f"out is {out.dtype}, out_dtype {out_dtype}")
+        outs.append(out)
+        if out.dtype is not outs[0].dtype or out.dtype is torch.int8 or out.dtype not in _types():
+            raise TypeError("outputs are fp16, bf16 or fp32, all of one type")
+        a = arr[i]
+        a.N, a.K, a.packed, a.x, a.y = N, K, pp, xp, _words(out, M * N, "out", out.dtype, device)
+        a.x_scales = _words(scales, M, "the scales of x", torch.float32, device) if pair else None
+    code = _types()[kind]
+    ws, wp, size = _scratch(workspace, _fourbit_workspace(tuple(shapes), M, code), outs[0], stream)
+    _launch("unisvq_fourbit_gemm_batched", device, stream, arr, count, M, code, _TYPES[outs[0].dtype], wp, size)
+    return outs
+
+
+@functools.lru_cache(maxsize=4096)
+def _fourbit_size(N: int, K: int) -> int:
+    return fourbit_bytes(N, K)
+
+
+def fourbit_gemm(packed, N: int, K: int, x, out=None, out_dtype=None, workspace=None, stream=None):
+    """y[M][N] = x[M][K] . W^T with packed 4-bit weights, any M; arguments as one problem of fourbit_gemm_batched."""
+    return fourbit_gemm_batched(((packed, N, K, x, out),), out_dtype, workspace, stream)[0]
