@@ -39,7 +39,7 @@ struct Kind {
     static constexpr bool kI8 = false;
     typedef typename Vec8<T>::type Operand;
     typedef f32x4 Sum;
-    static constexpr int kSteps = 4, kBytes = 2;      // products a group, bytes an element
+    static constexpr int kSteps = 4, kBytes = 2;      // products a slot of codes, bytes an element
     static constexpr float kUnit = 512.0f;            // codes are c * 2^-9
     __device__ static Operand minus8() {
         Operand v;
@@ -212,10 +212,10 @@ int launch_few(Batch b, hipStream_t s) {
 }
 
 // ---- many tokens ----
-// -8 times the sums of every token's groups, bias[token / 32][group][token % 32]
+// -8 times the sums of every token's groups, bias[token / 16][group][token % 16]
 // (fp32, or i8's integers), sixteen lanes a sum: what the tiled product's sums of
 // a group start from.
-constexpr int kSumTile = 32;
+constexpr int kSumTile = 16;
 
 struct Sums {
     const void* x;
@@ -280,40 +280,86 @@ __device__ __forceinline__ void load_lds(uint32_t to, const uint32_t (&off)[LOAD
                      : "memory");
 }
 
-// A workgroup has WM x WN waves, a wave 16 MT tokens x 16 NB rows.  A group of
-// columns at a time goes to LDS by direct loads, two groups deep: activations in
-// rows whose 16-byte chunks are turned by the row (so that sixteen rows' same
-// chunk lies in sixteen places), codes as they are, scales and sums.  A wave turns
-// its rows' codes into operands once and passes over its tokens with them.
-template <typename X, int MT, int NB, int WM, int WN>
+// A workgroup has 16 MT tokens and four waves, a wave 16 NB rows for all of them;
+// two workgroups share a CU.  A group of columns at a time goes to LDS by direct
+// loads: activations, which all waves read, in rows whose 16-byte chunks are
+// turned by the row (so that sixteen rows' same chunk lies in sixteen places),
+// and every wave's own codes and scales.  A wave turns its rows' codes into
+// operands once and passes over the tokens with them.
+//
+// SUMS: the sums that a group starts from are made here, by one product more for
+// every NB; else they come from sums_kernel.
+template <typename X, int MT, int NB, bool SUMS>
 struct Tiled {
     typedef Kind<X> Q;
-    static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
-    static constexpr int BM = 16 * MT * WM, BN = 16 * NB * WN;
-    static constexpr int kRow = kGroup * Q::kBytes;            // bytes of a token's group
-    static constexpr int kX = BM * kRow, kCodes = BN * 64, kScales = BN * 8;
-    static constexpr int kBias = (BM * 4 + 1023) / 1024 * 1024;  // (whole loads: what is behind the tokens becomes zeros)
-    static constexpr int kStage = kX + kCodes + kScales + kBias;
-    static constexpr int kLoadsX = kX / (16 * kThreads), kLoadsCodes = kCodes / (16 * kThreads);
-    static_assert(kX % (16 * kThreads) == 0 && kCodes % (16 * kThreads) == 0, "");
-    static constexpr int kWavesScales = kScales / 1024, kWavesBias = kBias / 1024;
-    static_assert(kScales % 1024 == 0 && kWavesScales + kWavesBias <= kWaves, "");
+    static constexpr int kWaves = 4, kThreads = 64 * kWaves;
+    static constexpr int BM = 16 * MT, BN = 16 * NB * kWaves;
+    static constexpr int kRow = kGroup * Q::kBytes;  // bytes of a token's group
+    // bytes of activations, of sums (whole loads: what is behind the tokens becomes
+    // zeros), and of a wave's codes and scales
+    static constexpr int kX = BM * kRow, kBias = SUMS ? 0 : 1024, kCodes = NB * 1024, kScales = 1024;
+    static constexpr int kShared = kX + kBias, kOwn = kCodes + kScales;
+    // Groups in LDS; where there is no room for two of everything, codes and
+    // scales are one deep: their next ones are asked for when they have been read.
+    static constexpr int kRoom = 80 * 1024, kGroups = kRoom / (kShared + kWaves * kOwn);
+    static constexpr int kStages = kGroups < 2 ? 2 : kGroups < 3 ? kGroups : 3, kCodeStages = kGroups < 2 ? 1 : kStages;
+    static constexpr int kLds = kStages * kShared + kWaves * kCodeStages * kOwn;
+    static_assert(kLds <= kRoom, "");
+    static constexpr int kLoadsX = kX / (16 * kThreads), kLoadsCodes = kCodes / 1024;
+    static_assert(kX % (16 * kThreads) == 0 && BM <= 256, "");
+    static constexpr int kPass = NB <= 2 && MT % 2 == 0 ? 2 : 1;  // tiles of tokens at a time: independent products to follow one another
     // a wave's outputs of one tile of tokens, staged for whole-line stores
     static constexpr int kPitch = 16 * NB * 4 + 16;
-    static_assert(kWaves * 16 * kPitch <= 2 * kStage, "");
+    static_assert(kWaves * 16 * kPitch <= kLds, "");
 };
 
-template <typename X, int MT, int NB, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void tiled_kernel(const TileBatch tb) {
-    typedef Tiled<X, MT, NB, WM, WN> C;
+// A wave's outputs, acc[m][j][i] of token 16 m + 4 (lane / 16) + i and row 16 j +
+// lane % 16, to y[token][row]: a tile of sixteen tokens at a time through the
+// wave's own LDS, and from there in pieces of 16 bytes of tokens' rows.
+template <int MT, int NB, typename Y>
+__device__ __forceinline__ void store_tiles(Y* y, int64_t pitch, const f32x4 (&acc)[MT][NB], int toks, int rows, uint8_t* mine, int lane) {
+    const int n = lane & 15, c = lane >> 4;
+    if ((reinterpret_cast<uintptr_t>(y) & 15) != 0) {  // (rows are of sixteen elements and more: one row's place says it all)
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+                    if (16 * m + 4 * c + i < toks && 16 * j < rows)
+                        y[(16 * m + 4 * c + i) * pitch + 16 * j + n] = static_cast<Y>(acc[m][j][i]);
+        return;
+    }
+    constexpr int kPieces = 16 * NB * sizeof(Y) / 16, kRow = 16 * NB + 16 / sizeof(Y);
+    Y* stage = reinterpret_cast<Y*>(mine);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) stage[(4 * c + i) * kRow + 16 * j + n] = static_cast<Y>(acc[m][j][i]);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int e = 0; e < 16 * kPieces / 64; ++e) {
+            const int piece = e * 64 + lane, t = piece / kPieces, at = piece % kPieces * (16 / static_cast<int>(sizeof(Y)));
+            const uint4 v = *reinterpret_cast<const uint4*>(stage + t * kRow + at);
+            if (16 * m + t < toks && at < rows) *reinterpret_cast<uint4*>(y + (16 * m + t) * pitch + at) = v;
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+template <typename X, int MT, int NB, bool SUMS>
+__global__ __launch_bounds__(256, 2) void tiled_kernel(const TileBatch tb) {
+    typedef Tiled<X, MT, NB, SUMS> C;
     typedef typename C::Q Q;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2][C::kStage];
+    __shared__ __attribute__((aligned(16))) uint8_t lds[C::kLds];
     TileProb p = tb.p[0];
 #pragma unroll
     for (int i = 1; i < kMaxBatch; ++i)
         if (i < tb.count && static_cast<int>(blockIdx.x) >= tb.p[i].wg_begin) p = tb.p[i];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n = lane & 15, c = lane >> 4, wm = wave % WM, wn = wave / WM;
+    const int n = lane & 15, c = lane >> 4;
     const int K = p.K, groups = K / kGroup, quads = (groups + 3) / 4;
     const int64_t blocks = p.N / kRowBlock;
 
@@ -326,17 +372,20 @@ __global__ __launch_bounds__(64 * WM * WN) void tiled_kernel(const TileBatch tb)
     // (divisions leave the scalar registers)
     const int nt_sp = __builtin_amdgcn_readfirstlane(L / tb.m_tiles), mt = L - nt_sp * tb.m_tiles;
     const int sp = __builtin_amdgcn_readfirstlane(nt_sp / n_tiles), nt = nt_sp - sp * n_tiles;
-    const int64_t tok0 = static_cast<int64_t>(mt) * C::BM, rb0 = static_cast<int64_t>(nt) * (C::BN / 16);
+    const int64_t tok0 = static_cast<int64_t>(mt) * C::BM, rb0 = nt * (C::BN / 16) + wave * NB;
     const int toks = static_cast<int>(min(static_cast<int64_t>(C::BM), tb.M - tok0));
-    const int rbs = static_cast<int>(min(static_cast<int64_t>(C::BN / 16), blocks - rb0));
+    // row blocks of the wave's that are there (a wave with none goes along)
+    const int rbs = max(min(NB, static_cast<int>(blocks - rb0)), 0);
+    const int64_t rb_at = __builtin_amdgcn_readfirstlane(static_cast<int>(min(rb0, blocks - 1)));
     const int g0 = __builtin_amdgcn_readfirstlane(groups * sp / p.splits);
     const int g1 = __builtin_amdgcn_readfirstlane(groups * (sp + 1) / p.splits);
 
     const __amdgpu_buffer_rsrc_t rx = make_rsrc(static_cast<const uint8_t*>(p.x) + tok0 * K * Q::kBytes,
                                                 static_cast<uint32_t>(toks) * K * Q::kBytes);
-    const __amdgpu_buffer_rsrc_t rw = make_rsrc(p.packed + rb0 * groups * kFourbitTile, static_cast<uint32_t>(rbs) * groups * kFourbitTile);
+    const uint32_t here = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(max(rbs, 1)));
+    const __amdgpu_buffer_rsrc_t rw = make_rsrc(p.packed + rb_at * groups * kFourbitTile, here * groups * kFourbitTile);
     const __amdgpu_buffer_rsrc_t rs =
-        make_rsrc(p.packed + p.N * (K / 2) + rb0 * quads * kFourbitQuad, static_cast<uint32_t>(rbs) * quads * kFourbitQuad);
+        make_rsrc(p.packed + p.N * (K / 2) + rb_at * quads * kFourbitQuad, here * quads * kFourbitQuad);
     const __amdgpu_buffer_rsrc_t rb = make_rsrc(static_cast<const uint8_t*>(p.bias) + tok0 * groups * 4,
                                                 static_cast<uint32_t>((toks + kSumTile - 1) / kSumTile * groups * kSumTile * 4));
 
@@ -349,112 +398,129 @@ __global__ __launch_bounds__(64 * WM * WN) void tiled_kernel(const TileBatch tb)
         off_x[i] = static_cast<uint32_t>(min(row, toks - 1)) * K * Q::kBytes + 16 * chunk;
     }
     const uint32_t at16[1] = {16u * lane};
-    uint32_t off_s[1], off_b[1];
-    const bool has_scales = wave < C::kWavesScales, has_bias = wave >= C::kWaves - C::kWavesBias;
-    {
-        const int at = wave * 1024 + 16 * lane, r = at >> 7;
-        off_s[0] = static_cast<uint32_t>(min(r, rbs - 1)) * quads * kFourbitQuad + (at & 127);
-        const int t = (wave - (C::kWaves - C::kWavesBias)) * 256 + 4 * lane;
-        off_b[0] = t < C::BM ? static_cast<uint32_t>(t / kSumTile * groups * kSumTile + t % kSumTile) * 4u : kOutOfRange;
-    }
+    const uint32_t off_s[1] = {lane >> 3 < NB ? min(static_cast<uint32_t>(lane) >> 3, here - 1) * quads * kFourbitQuad + 16 * (lane & 7)
+                                                  : kOutOfRange};
+    const uint32_t off_b[1] = {4 * lane < C::BM ? static_cast<uint32_t>(lane / 4 * groups * kSumTile * 4 + 16 * (lane % 4)) : kOutOfRange};
+    static_assert(kSumTile == 16, "");
+    const bool has_bias = !SUMS && wave == 0;
     const uint32_t base = __builtin_amdgcn_readfirstlane(
-        static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)&lds[0][0])));
-    const auto issue = [&](int g, int stage) {
-        const uint32_t to = base + stage * C::kStage;
+        static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)&lds[0])));
+    constexpr int kOwnAt = C::kStages * C::kShared;
+    const auto issue_shared = [&](int g, int stage) {
+        const uint32_t to = base + stage * C::kShared;
         load_lds<16 * C::kThreads>(to + wave * 1024, off_x, rx, static_cast<uint32_t>(g) * C::kRow);
+        if (has_bias) load_lds<0>(to + C::kX, off_b, rb, static_cast<uint32_t>(g) * (kSumTile * 4));
+    };
+    const auto issue_own = [&](int g, int stage) {
+        const uint32_t to = base + kOwnAt + (wave * C::kCodeStages + stage) * C::kOwn;
 #pragma unroll
-        for (int i = 0; i < C::kLoadsCodes; ++i) {
-            const int r = i * C::kWaves + wave;
-            load_lds<0>(to + C::kX + r * 1024, at16, rw, static_cast<uint32_t>(min(r, rbs - 1) * groups + g) * kFourbitTile);
-        }
-        if (has_scales) load_lds<0>(to + C::kX + C::kCodes + wave * 1024, off_s, rs, static_cast<uint32_t>(g >> 2) * kFourbitQuad);
-        if (has_bias)
-            load_lds<0>(to + C::kX + C::kCodes + C::kScales + (wave - (C::kWaves - C::kWavesBias)) * 1024, off_b, rb,
-                        static_cast<uint32_t>(g * kSumTile * 4));
+        for (uint32_t i = 0; i < C::kLoadsCodes; ++i)
+            load_lds<0>(to + i * 1024, at16, rw, __builtin_amdgcn_readfirstlane((min(i, here - 1) * groups + g) * kFourbitTile));
+        load_lds<0>(to + C::kCodes, off_s, rs, static_cast<uint32_t>(g >> 2) * kFourbitQuad);
     };
 
+    typename Q::Operand minus8 = Q::minus8();
     f32x4 acc[MT][NB] = {};
-    if (g0 < g1) issue(g0, 0);
+    // groups under way, and this wave's loads of one
+    constexpr int kAhead = C::kStages - 1, kAheadOwn = C::kCodeStages == 1 ? 1 : kAhead;
+    constexpr int kLoads = C::kLoadsX + C::kLoadsCodes + 1;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+        if (g0 + i < g1) {
+            issue_shared(g0 + i, i);
+            issue_own(g0 + i, C::kCodeStages == 1 ? 0 : i);
+        }
+    int stage = 0;
     for (int g = g0; g < g1; ++g) {
-        const int stage = (g - g0) & 1;
+        // this group is there, and the last one has been read by all
         __builtin_amdgcn_sched_barrier(0);
-        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");  // this group is there, the last one read by all
+        if (kAhead == 1 || g + kAhead > g1)
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        else if (has_bias)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kAhead - 1) * (kLoads + 1)) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kAhead - 1) * kLoads) : "memory");
+        asm volatile("s_barrier" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        if (g + 1 < g1) issue(g + 1, stage ^ 1);
-        const uint8_t* from = lds[stage];
+        const int before = stage ? stage - 1 : kAhead;
+        if (g + kAhead < g1) issue_shared(g + kAhead, before);
+        const uint8_t* own = lds + kOwnAt + (wave * C::kCodeStages + (C::kCodeStages == 1 ? 0 : stage)) * C::kOwn;
         typename Q::Operand w[NB][Q::kSteps];
         float s[NB];
+        uint4 q[NB];
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
-            const int r = wn * NB + j;
-            Q::decode(*reinterpret_cast<const uint4*>(from + C::kX + r * 1024 + 16 * lane), w[j]);
-            s[j] = static_cast<float>(*reinterpret_cast<const _Float16*>(from + C::kX + C::kCodes + r * 128 + 8 * n + 2 * (g & 3)));
+            q[j] = *reinterpret_cast<const uint4*>(own + j * 1024 + 16 * lane);
+            s[j] = static_cast<float>(*reinterpret_cast<const _Float16*>(own + C::kCodes + j * 128 + 8 * n + 2 * (g & 3)));
         }
+        if constexpr (C::kCodeStages == 1) {  // (read before they are overwritten)
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const int row = (wm * MT + m) * 16 + n;
-            typename Q::Operand x[Q::kSteps];
+            for (int j = 0; j < NB; ++j) asm volatile("" : "+v"(s[j]));
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+        if (g + kAheadOwn < g1) issue_own(g + kAheadOwn, C::kCodeStages == 1 ? 0 : before);
 #pragma unroll
-            for (int k = 0; k < Q::kSteps; ++k) {
-                const int chunk = (Q::kChunk * c + Q::at(k)) / 16;
-                x[k] = *reinterpret_cast<const typename Q::Operand*>(from + row * C::kRow + 16 * (chunk ^ (row >> kTurn) % kChunks));
+        for (int j = 0; j < NB; ++j) Q::decode(q[j], w[j]);
+        const uint8_t* from = lds + stage * C::kShared;
+#pragma unroll
+        for (int m0 = 0; m0 < MT; m0 += C::kPass) {
+            typename Q::Operand x[C::kPass][Q::kSteps];
+            typename Q::Sum bias[C::kPass], sum[C::kPass][NB];
+#pragma unroll
+            for (int m = 0; m < C::kPass; ++m) {
+                const int row = 16 * (m0 + m) + n;
+#pragma unroll
+                for (int k = 0; k < Q::kSteps; ++k) {
+                    const int chunk = (Q::kChunk * c + Q::at(k)) / 16;
+                    x[m][k] = *reinterpret_cast<const typename Q::Operand*>(from + row * C::kRow + 16 * (chunk ^ (row >> kTurn) % kChunks));
+                }
+                bias[m] = typename Q::Sum{};
+                if constexpr (!SUMS) bias[m] = *reinterpret_cast<const typename Q::Sum*>(from + C::kX + 4 * (row - n + 4 * c));
             }
-            const typename Q::Sum bias = *reinterpret_cast<const typename Q::Sum*>(
-                from + C::kX + C::kCodes + C::kScales + 4 * ((wm * MT + m) * 16 + 4 * c));
-            typename Q::Sum sum[NB];
+            if constexpr (SUMS)
+#pragma unroll
+                for (int k = 0; k < Q::kSteps; ++k)
+#pragma unroll
+                    for (int m = 0; m < C::kPass; ++m) bias[m] = Q::mma(x[m][k], minus8, bias[m]);
 #pragma unroll
             for (int k = 0; k < Q::kSteps; ++k)
 #pragma unroll
-                for (int j = 0; j < NB; ++j) sum[j] = Q::mma(x[k], w[j][k], k ? sum[j] : bias);
+                for (int m = 0; m < C::kPass; ++m)
 #pragma unroll
-            for (int j = 0; j < NB; ++j)
+                    for (int j = 0; j < NB; ++j) sum[m][j] = Q::mma(x[m][k], w[j][k], k ? sum[m][j] : bias[m]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[m][j][i] = fmaf(s[j], static_cast<float>(sum[j][i]), acc[m][j][i]);
+            for (int m = 0; m < C::kPass; ++m)
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[m0 + m][j][i] = fmaf(s[j], static_cast<float>(sum[m][j][i]), acc[m0 + m][j][i]);
         }
+        stage = stage == kAhead ? 0 : stage + 1;
     }
     __syncthreads();
 
-    // Outputs: a tile of sixteen tokens at a time through the wave's own part of
-    // LDS, and from there in pieces of 16 bytes of tokens' rows.
-    const bool partial = p.partial != nullptr, wide = partial || tb.y_dtype == UNISVQ_F32;
-    void* out = partial ? p.partial + sp * tb.M * p.N : p.y;
-    const int y_dtype = partial ? UNISVQ_F32 : tb.y_dtype;
-    const bool whole = (reinterpret_cast<uintptr_t>(out) & 15) == 0;
-    const int rows = min(16 * NB, (rbs - wn * NB) * 16);  // of the wave's that are there
-    uint8_t* mine = &lds[0][0] + wave * 16 * C::kPitch;
+    // Outputs (all scales asked for at once)
+    const bool partial = p.partial != nullptr;
+    f32x4 unit[MT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        const int t0 = (wm * MT + m) * 16;
-        float unit[4];
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int t = min(t0 + 4 * c + i, toks - 1);
-            unit[i] = Q::kI8 ? (partial ? 1.0f : p.x_scales[tok0 + t]) : Q::kUnit;
-        }
-        const int64_t at = (tok0 + t0) * p.N + (rb0 + wn * NB) * 16;
-        if (!whole) {
+        for (int i = 0; i < 4; ++i)
+            unit[m][i] = Q::kI8 ? (partial ? 1.0f : p.x_scales[tok0 + min(16 * m + 4 * c + i, toks - 1)]) : Q::kUnit;
 #pragma unroll
-            for (int j = 0; j < NB; ++j)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (16 * j < rows && t0 + 4 * c + i < toks)
-                        store_out(out, at + (4 * c + i) * p.N + 16 * j + n, acc[m][j][i] * unit[i], y_dtype);
-            continue;
-        }
-#pragma unroll
-        for (int j = 0; j < NB; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) store_out(mine + (4 * c + i) * C::kPitch, 16 * j + n, acc[m][j][i] * unit[i], y_dtype);
-        __builtin_amdgcn_wave_barrier();
-        const int size = wide ? 4 : 2, pieces = 16 * NB * size / 16;  // of 16 bytes, a token
-        for (int e = lane; e < 16 * pieces; e += 64) {
-            const int t = e / pieces, piece = e % pieces;
-            if (t0 + t < toks && piece * 16 < rows * size)
-                *reinterpret_cast<uint4*>(static_cast<uint8_t*>(out) + (at + t * p.N) * size + 16 * piece) =
-                    *reinterpret_cast<const uint4*>(mine + t * C::kPitch + 16 * piece);
-        }
-        __builtin_amdgcn_wave_barrier();
-    }
+        for (int j = 0; j < NB; ++j) acc[m][j] *= unit[m];
+    const int64_t at = tok0 * p.N + rb0 * 16;
+    uint8_t* mine = lds + wave * 16 * C::kPitch;
+    if (partial)
+        store_tiles<MT, NB>(p.partial + sp * tb.M * p.N + at, p.N, acc, toks, 16 * rbs, mine, lane);
+    else if (tb.y_dtype == UNISVQ_F32)
+        store_tiles<MT, NB>(static_cast<float*>(p.y) + at, p.N, acc, toks, 16 * rbs, mine, lane);
+    else if (tb.y_dtype == UNISVQ_F16)
+        store_tiles<MT, NB>(static_cast<_Float16*>(p.y) + at, p.N, acc, toks, 16 * rbs, mine, lane);
+    else
+        store_tiles<MT, NB>(static_cast<__bf16*>(p.y) + at, p.N, acc, toks, 16 * rbs, mine, lane);
 }
 
 // Sums of the parts of a K that was split, in their order; four columns a thread.
@@ -482,38 +548,62 @@ __global__ __launch_bounds__(256) void join_kernel(const JoinBatch b) {
 
 // How a batch is split: tokens and rows of a workgroup, and parts of K.
 constexpr int64_t kCUs = 256;
-constexpr int64_t kFewTokens = 64;
+constexpr int64_t kFewTokens = 16;
 
 struct Plan {
-    int mt;      // token tiles of a wave: 2 mt tiles of 16 a workgroup, 256 rows
+    int mt, nb;  // a workgroup has 16 mt tokens and 64 nb rows
     int splits[kMaxBatch];
-    bool split;
+    bool split, sums;  // whether any K is split, and the product makes its own sums
+    double us;
 };
 
+// Measured times of a group of columns in us (K 1024 and 4096, rows for 128 to 512
+// workgroups), [nb 2, 4][mt 2, 4, 6, 8]: a CU with one workgroup, and with two.
+constexpr float kAlone16[2][4] = {{0.59f, 0.77f, 1.02f, 0.0f}, {1.04f, 1.27f, 1.71f, 0.0f}};
+constexpr float kPaired16[2][4] = {{0.90f, 1.18f, 1.56f, 0.0f}, {1.82f, 2.13f, 2.83f, 0.0f}};
+constexpr float kAlone8[2][4] = {{0.46f, 0.61f, 0.73f, 0.85f}, {0.83f, 1.06f, 1.20f, 1.41f}};
+constexpr float kPaired8[2][4] = {{0.82f, 0.92f, 1.13f, 1.30f}, {1.56f, 1.84f, 2.01f, 2.55f}};
+
+// The plan with the least expected time: what the workgroups take, two to a CU,
+// which start and end in 4 to 10 us; a launch for the sums of activations or a
+// fifth more products (8 bits: a twentieth, and none where a CU has one
+// workgroup); parts of K and the launch that joins them.
 Plan plan_of(const FourbitProblem* probs, int count, int64_t M, bool i8) {
     Plan best{};
-    double least = 1e30;
-    for (int mt : {2, 4, 6, 8}) {
-        if (mt == 8 && !i8) continue;  // (LDS)
-        int64_t tiles = 0;
-        for (int i = 0; i < count; ++i) tiles += (probs[i].N + 255) / 256 * ((M + 32 * mt - 1) / (32 * mt));
-        for (int splits = 1; splits <= 8 && (splits == 1 || tiles < 2 * kCUs); ++splits) {
-            int64_t wgs = 0;
-            int groups = 0;
-            Plan p{mt, {}, splits > 1};
-            for (int i = 0; i < count; ++i) {
-                const int g = static_cast<int>(probs[i].K / kGroup);
-                p.splits[i] = std::max(1, std::min(splits, g / 4));
-                wgs += (probs[i].N + 255) / 256 * ((M + 32 * mt - 1) / (32 * mt)) * p.splits[i];
-                groups = std::max(groups, (g + p.splits[i] - 1) / p.splits[i]);
+    best.us = 1e30;
+    double read = 0;
+    for (int i = 0; i < count; ++i) read = std::max(read, static_cast<double>(M * probs[i].K) * (i8 ? 1 : 2));
+    for (int n = 0; n < 2; ++n)
+        for (int m = 0; m < (i8 ? 4 : 3); ++m) {
+            const int64_t BM = 32 * (m + 1), BN = 128 * (n + 1), m_tiles = (M + BM - 1) / BM;
+            if (m && BM >= 2 * M) continue;
+            int64_t tiles = 0;
+            for (int i = 0; i < count; ++i) tiles += (probs[i].N + BN - 1) / BN * m_tiles;
+            for (int splits = 1; splits == 1 || (splits <= 12 && tiles * splits <= 2 * kCUs); ++splits) {
+                Plan p{2 * (m + 1), 2 * (n + 1), {}, false, false, 0};
+                int64_t wgs = 0;
+                int groups = 0;
+                double parts = 0;
+                for (int i = 0; i < count; ++i) {
+                    const int g = static_cast<int>(probs[i].K / kGroup);
+                    p.splits[i] = std::max(1, std::min(splits, g / 4));
+                    p.split |= p.splits[i] > 1;
+                    wgs += (probs[i].N + BN - 1) / BN * m_tiles * p.splits[i];
+                    groups = std::max(groups, (g + p.splits[i] - 1) / p.splits[i]);
+                    if (p.splits[i] > 1) parts += 8.0 * p.splits[i] * static_cast<double>(M * probs[i].N);
+                }
+                const double alone = (i8 ? kAlone8 : kAlone16)[n][m], paired = (i8 ? kPaired8 : kPaired16)[n][m];
+                // up to two rounds are rounds; of more, workgroups begin as others end
+                const int64_t rest = wgs % (2 * kCUs);
+                const double rounds = wgs > 4 * kCUs ? 0.97 * static_cast<double>(wgs) / (2 * kCUs) * paired
+                                                     : static_cast<double>(wgs / (2 * kCUs)) * paired + (rest > kCUs ? paired : rest ? alone : 0.0);
+                const double steps = groups * rounds;
+                const double more = wgs <= kCUs ? 0.03 * steps : (i8 ? 0.05 : 0.2) * steps, launch = 2.2 + read / 4e6;
+                p.sums = more < launch;
+                p.us = 3.0 + 0.25 * (m + 1) * (n + 1) + steps + std::min(more, launch) + (p.split ? 2.0 + parts / 6e6 : 0.0);
+                if (p.us < best.us) best = p;
             }
-            const double rounds = static_cast<double>((wgs + kCUs - 1) / kCUs);
-            double outs = 0;
-            for (int i = 0; i < count; ++i) outs += static_cast<double>(M * probs[i].N) * (p.splits[i] > 1 ? 8.0 * p.splits[i] : 0.0);
-            const double us = rounds * (2.0 + groups * (0.4 + 0.25 * mt)) + (splits > 1 ? 3.0 + outs / 4e6 : 0.0);
-            if (us < least) least = us, best = p;
         }
-    }
     return best;
 }
 
@@ -534,7 +624,7 @@ Places places_of(const FourbitProblem* probs, int count, int64_t M, const Plan& 
             if (probs[i].x && probs[j].x == probs[i].x && probs[j].K == probs[i].K) same = j;
         p.first[i] = same == i;
         p.bias[i] = p.first[i] ? p.bytes : p.bias[same];
-        if (p.first[i]) p.bytes += static_cast<size_t>((M + kSumTile - 1) / kSumTile * (probs[i].K / kGroup)) * kSumTile * 4;
+        if (p.first[i] && !plan.sums) p.bytes += static_cast<size_t>((M + kSumTile - 1) / kSumTile * (probs[i].K / kGroup)) * kSumTile * 4;
     }
     for (int i = 0; i < count; ++i)
         if (plan.splits[i] > 1) {
@@ -544,9 +634,9 @@ Places places_of(const FourbitProblem* probs, int count, int64_t M, const Plan& 
     return p;
 }
 
-template <typename X, int MT>
+template <typename X, int MT, int NB, bool SUMS>
 int launch_tiles(TileBatch& tb, hipStream_t s) {
-    typedef Tiled<X, MT, 4, 2, 4> C;
+    typedef Tiled<X, MT, NB, SUMS> C;
     int64_t wgs = 0;
     tb.m_tiles = static_cast<int>((tb.M + C::BM - 1) / C::BM);
     for (int i = 0; i < tb.count; ++i) {
@@ -554,21 +644,25 @@ int launch_tiles(TileBatch& tb, hipStream_t s) {
         wgs += (tb.p[i].N + C::BN - 1) / C::BN * tb.m_tiles * tb.p[i].splits;
         if (wgs > (int64_t{1} << 32) / C::kThreads - 1) return UNISVQ_EUNSUP;
     }
-    tiled_kernel<X, MT, 4, 2, 4><<<static_cast<uint32_t>(wgs), C::kThreads, 0, s>>>(tb);
+    tiled_kernel<X, MT, NB, SUMS><<<static_cast<uint32_t>(wgs), C::kThreads, 0, s>>>(tb);
     return hipGetLastError() == hipSuccess ? UNISVQ_OK : UNISVQ_EHIP;
 }
 
-template <typename X>
-int launch_most(int mt, TileBatch& tb, hipStream_t s) {
+template <typename X, int NB, bool SUMS>
+int launch_tokens(int mt, TileBatch& tb, hipStream_t s) {
+    if (mt == 2) return launch_tiles<X, 2, NB, SUMS>(tb, s);
+    if (mt == 4) return launch_tiles<X, 4, NB, SUMS>(tb, s);
     if constexpr (Kind<X>::kI8)
-        if (mt == 8) return launch_tiles<X, 8>(tb, s);
-    return launch_tiles<X, 6>(tb, s);
+        if (mt == 8) return launch_tiles<X, 8, NB, SUMS>(tb, s);
+    return launch_tiles<X, 6, NB, SUMS>(tb, s);
 }
 
 template <typename X>
-int launch_tiled(const FourbitProblem* probs, int count, int64_t M, int y_dtype, uint8_t* workspace, hipStream_t s) {
+int launch_tiled(const FourbitProblem* probs, int count, int64_t M, int y_dtype, uint8_t* workspace, size_t room, hipStream_t s) {
     const Plan plan = plan_of(probs, count, M, Kind<X>::kI8);
     const Places at = places_of(probs, count, M, plan);
+    if (at.bytes && (!workspace || room < at.bytes)) return UNISVQ_EWORKSPACE;
+    if (at.bytes && (reinterpret_cast<uintptr_t>(workspace) & 15) != 0) return UNISVQ_EALIGN;
     TileBatch tb{};
     tb.count = count, tb.y_dtype = y_dtype, tb.M = M;
     for (int i = 0; i < count; ++i) {
@@ -576,13 +670,13 @@ int launch_tiled(const FourbitProblem* probs, int count, int64_t M, int y_dtype,
         tb.p[i] = TileProb{probs[i].packed, probs[i].x, workspace + at.bias[i], probs[i].x_scales, probs[i].y,
                            plan.splits[i] > 1 ? reinterpret_cast<float*>(workspace + at.partial[i]) : nullptr, probs[i].N,
                            static_cast<int>(probs[i].K), plan.splits[i], 0};
-        if (at.first[i]) {
+        if (at.first[i] && !plan.sums) {
             const Sums a{probs[i].x, workspace + at.bias[i], M, groups};
             sums_kernel<X><<<static_cast<uint32_t>((M * groups + 15) / 16), 256, 0, s>>>(a);
         }
     }
-    const int st = plan.mt == 2 ? launch_tiles<X, 2>(tb, s) : plan.mt == 4 ? launch_tiles<X, 4>(tb, s)
-                 : launch_most<X>(plan.mt, tb, s);
+    const int st = plan.nb == 2 ? (plan.sums ? launch_tokens<X, 2, true>(plan.mt, tb, s) : launch_tokens<X, 2, false>(plan.mt, tb, s))
+                                : (plan.sums ? launch_tokens<X, 4, true>(plan.mt, tb, s) : launch_tokens<X, 4, false>(plan.mt, tb, s));
     if (st != UNISVQ_OK || !plan.split) return st;
     JoinBatch jb{};
     jb.y_dtype = y_dtype, jb.i8 = Kind<X>::kI8, jb.M = M;
@@ -599,8 +693,8 @@ int launch_tiled(const FourbitProblem* probs, int count, int64_t M, int y_dtype,
 }
 
 template <typename X>
-int launch_kind(const FourbitProblem* probs, int count, int64_t M, int y_dtype, uint8_t* workspace, hipStream_t s) {
-    if (M > kFewTokens) return launch_tiled<X>(probs, count, M, y_dtype, workspace, s);
+int launch_kind(const FourbitProblem* probs, int count, int64_t M, int y_dtype, uint8_t* workspace, size_t room, hipStream_t s) {
+    if (M > kFewTokens) return launch_tiled<X>(probs, count, M, y_dtype, workspace, room, s);
     Batch b{};
     b.count = count, b.y_dtype = y_dtype, b.M = M;
     for (int i = 0; i < count; ++i)
@@ -617,11 +711,11 @@ size_t fourbit_workspace_bytes(const FourbitProblem* probs, int count, int64_t M
 }
 
 int launch_fourbit_batch(const FourbitProblem* probs, int count, int64_t M, int x_dtype, int y_dtype, void* workspace,
-                         hipStream_t s) {
+                         size_t workspace_bytes, hipStream_t s) {
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    if (x_dtype == UNISVQ_F16) return launch_kind<_Float16>(probs, count, M, y_dtype, ws, s);
-    if (x_dtype == UNISVQ_BF16) return launch_kind<__bf16>(probs, count, M, y_dtype, ws, s);
-    return launch_kind<int8_t>(probs, count, M, y_dtype, ws, s);
+    if (x_dtype == UNISVQ_F16) return launch_kind<_Float16>(probs, count, M, y_dtype, ws, workspace_bytes, s);
+    if (x_dtype == UNISVQ_BF16) return launch_kind<__bf16>(probs, count, M, y_dtype, ws, workspace_bytes, s);
+    return launch_kind<int8_t>(probs, count, M, y_dtype, ws, workspace_bytes, s);
 }
 
 }  // namespace unisvq

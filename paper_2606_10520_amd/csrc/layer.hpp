@@ -57,9 +57,10 @@ struct FourbitProblem {
     int64_t N, K;
 };
 size_t fourbit_workspace_bytes(const FourbitProblem* probs, int count, int64_t M, int x_dtype);
-// UNISVQ_OK, or UNISVQ_EUNSUP where the launch would be too large, or UNISVQ_EHIP.
+// UNISVQ_OK, UNISVQ_EWORKSPACE or UNISVQ_EALIGN (the workspace), UNISVQ_EUNSUP where
+// the launch would be too large, or UNISVQ_EHIP.
 int launch_fourbit_batch(const FourbitProblem* probs, int count, int64_t M, int x_dtype, int y_dtype, void* workspace,
-                    hipStream_t s);
+                         size_t workspace_bytes, hipStream_t s);
 
 // ---- device helpers ----
 

@@ -144,10 +144,8 @@ int unisvq_fourbit_gemm_batched(const unisvq_fourbit_problem* problems, int coun
     }
     FourbitProblem p[UNISVQ_MAX_BATCH];
     fourbit_batch(problems, count, p);
-    const size_t need = unisvq::fourbit_workspace_bytes(p, count, M, x_dtype);
-    if (need && (!workspace || workspace_bytes < need)) return UNISVQ_EWORKSPACE;
-    if (need && !aligned(workspace, 16)) return UNISVQ_EALIGN;
-    return unisvq::launch_fourbit_batch(p, count, M, x_dtype, y_dtype, workspace, static_cast<hipStream_t>(stream));
+    return unisvq::launch_fourbit_batch(p, count, M, x_dtype, y_dtype, workspace, workspace_bytes,
+                                        static_cast<hipStream_t>(stream));
 }
 
 size_t unisvq_fourbit_gemm_workspace_bytes(int64_t N, int64_t K, int64_t M, int x_dtype) {
