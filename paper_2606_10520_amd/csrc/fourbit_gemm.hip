@@ -17,13 +17,16 @@
 namespace unisvq {
 namespace {
 
+constexpr int64_t kCUs = 256;
+constexpr int kMostLds = 160 * 1024;  // of a CU
+
 struct Prob {
     const uint8_t* packed;
     const void* x;
     const float* x_scales;
     void* y;
     int64_t N;
-    int K, wg_begin;
+    int K, wg_begin, wgs;
 };
 
 struct Batch {
@@ -100,114 +103,242 @@ struct Kind<int8_t> {
     static constexpr uint32_t kChunk = 16;
 };
 
-// Few tokens: a workgroup has RB blocks of 16 rows and MT tiles of 16 tokens, its
-// waves share K out in runs of groups, and their sums meet in LDS.
-template <typename X, int MT, int RB, int WAVES>
+// ---- few tokens ----
+// Bound by the weights' read: x has to come from somewhere near.  A workgroup's
+// waves share K out in runs of groups; every wave keeps its part of x in LDS (TOK
+// tokens, 16-byte chunks turned by the token so that those that are read together
+// lie in different banks) and -8 times its groups' sums, and passes over blocks of
+// sixteen rows with them, gridDim.x apart, DEEP tiles of codes on their way.  The
+// waves' sums of a block meet in LDS, one of the waves adds and stores them while
+// the others go on.
+template <typename X, int TOK, int WAVES, int DEEP>
 __global__ __launch_bounds__(64 * WAVES) void few_kernel(const Batch b) {
     typedef Kind<X> Q;
-    __shared__ f32x4 parts[WAVES][RB * MT][64];
+    constexpr int kRow = kGroup * Q::kBytes, kChunks = kRow / 16, kGroupBytes = TOK * kRow + 64;
+    extern __shared__ __attribute__((aligned(16))) uint8_t few_lds[];
+    f32x4(*parts)[WAVES][64] = reinterpret_cast<f32x4(*)[WAVES][64]>(few_lds);
+    Prob p = b.p[0];
+#pragma unroll
+    for (int i = 1; i < kMaxBatch; ++i)
+        if (i < b.count && static_cast<int>(blockIdx.x) >= b.p[i].wg_begin) p = b.p[i];
+    const int wgs = p.wgs;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 15, c = lane >> 4, tok = n & (TOK - 1);
+    const int blocks = static_cast<int>(p.N / kRowBlock), first = static_cast<int>(blockIdx.x) - p.wg_begin;
+    const int K = p.K, groups = K / kGroup, quads = (groups + 3) / 4;
+    const int g0 = __builtin_amdgcn_readfirstlane(groups * wave / WAVES), g1 = __builtin_amdgcn_readfirstlane(groups * (wave + 1) / WAVES);
+    const int share = g1 - g0;
+    uint8_t* mine = few_lds + 2 * WAVES * 1024 + g0 * kGroupBytes;
+
+    // a tile: codes and scale of (block, group), by running offsets
+    const uint8_t* tail = p.packed + p.N * (K / 2);
+    struct Tile {
+        uint4 q;
+        uint32_t s;
+    } ring[DEEP];
+    // (a block's tiles are taken DEEP at a time; those past the share read nothing:
+    // their scales are zeros)
+    const int padded = (share + DEEP - 1) / DEEP * DEEP;
+    int rb = first, next = 0;  // of the next tile to ask for
+    const auto ask = [&](Tile& t) {
+        const uint32_t out = rb < blocks && next < share ? 0u : kOutOfRange;
+        const int g = g0 + next;
+        const int64_t at = min(rb, blocks - 1);
+        const __amdgpu_buffer_rsrc_t rw = make_rsrc(p.packed + at * groups * kFourbitTile, groups * kFourbitTile);
+        const __amdgpu_buffer_rsrc_t rs = make_rsrc(tail + at * quads * kFourbitQuad, quads * kFourbitQuad);
+        t.q = ld128_stream(rw, out | static_cast<uint32_t>(g * kFourbitTile + 16 * lane));
+        t.s = ld16(rs, out | static_cast<uint32_t>((g >> 2) * kFourbitQuad + 8 * n + 2 * (g & 3)));
+        const bool last = next + 1 >= padded;
+        next = last ? 0 : next + 1;
+        rb += last ? wgs : 0;
+    };
+#pragma unroll
+    for (int i = 0; i < DEEP; ++i) ask(ring[i]);
+
+    // x and the sums
+    {
+        const __amdgpu_buffer_rsrc_t rx = make_rsrc(p.x, static_cast<uint32_t>(b.M) * K * Q::kBytes);
+        for (int i = lane; i < share * TOK * kChunks; i += 64) {
+            const int chunk = i % kChunks, t = i / kChunks % TOK, h = i / (kChunks * TOK);
+            const int turn = Q::kI8 ? (t >> 1 & 1) << 2 | t >> 2 : (t & 1) | (t >> 1 & 1) << 3 | (t >> 2) << 1;
+            const uint4 v = ld128(rx, t < b.M ? static_cast<uint32_t>((t * K + (g0 + h) * kGroup) * Q::kBytes + 16 * chunk) : kOutOfRange);
+            *reinterpret_cast<uint4*>(mine + h * kGroupBytes + t * kRow + 16 * (chunk ^ turn)) = v;
+        }
+    }
+    const int turn = Q::kI8 ? (tok >> 1 & 1) << 2 | tok >> 2 : (tok & 1) | (tok >> 1 & 1) << 3 | (tok >> 2) << 1;
+    const uint8_t* at[Q::kSteps];
+#pragma unroll
+    for (int j = 0; j < Q::kSteps; ++j) at[j] = mine + tok * kRow + 16 * (((Q::kChunk * c + Q::at(j)) / 16) ^ turn);
+    {
+        const typename Q::Operand minus8 = Q::minus8();
+        for (int h = 0; h < share; ++h) {
+            typename Q::Sum bias{};
+#pragma unroll
+            for (int j = 0; j < Q::kSteps; ++j)
+                bias = Q::mma(*reinterpret_cast<const typename Q::Operand*>(at[j] + h * kGroupBytes), minus8, bias);
+            if (n == 0) *reinterpret_cast<typename Q::Sum*>(mine + h * kGroupBytes + TOK * kRow + 16 * c) = bias;
+        }
+    }
+    __builtin_amdgcn_wave_barrier();  // (a wave reads what it wrote itself)
+
+    for (int block = first, turnover = 0; block < blocks; block += wgs, ++turnover) {
+        f32x4 acc{};
+        for (int h0 = 0; h0 < padded; h0 += DEEP)
+#pragma unroll
+            for (int i = 0; i < DEEP; ++i) {
+                const int h = min(h0 + i, share - 1);
+                typename Q::Operand w[Q::kSteps];
+                Q::decode(ring[i].q, w);
+                const float s = static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(ring[i].s)));
+                ask(ring[i]);
+                typename Q::Sum sum = *reinterpret_cast<const typename Q::Sum*>(mine + h * kGroupBytes + TOK * kRow + 16 * c);
+#pragma unroll
+                for (int j = 0; j < Q::kSteps; ++j)
+                    sum = Q::mma(*reinterpret_cast<const typename Q::Operand*>(at[j] + h * kGroupBytes), w[j], sum);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] = fmaf(s, static_cast<float>(sum[e]), acc[e]);
+            }
+        parts[turnover & 1][wave][lane] = acc;
+        __syncthreads();
+        if (wave == turnover % WAVES && 4 * c < b.M) {
+            f32x4 sum = parts[turnover & 1][0][lane];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) sum += parts[turnover & 1][w][lane];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (4 * c + i < b.M) {
+                    const float unit = Q::kI8 ? p.x_scales[4 * c + i] : Q::kUnit;
+                    store_out(p.y, (4 * c + i) * p.N + block * kRowBlock + n, sum[i] * unit, b.y_dtype);
+                }
+        }
+    }
+}
+
+// Bytes of LDS: two rounds of the waves' sums, x and its groups' sums.
+int64_t few_lds_bytes(int64_t K, int tok, int waves, int size) {
+    return 2 * waves * 1024 + K / kGroup * (tok * kGroup * size + 64);
+}
+
+template <typename X, int TOK, int WAVES, int DEEP>
+int launch_few(Batch b, int64_t K, hipStream_t s) {
+    const int lds = static_cast<int>(few_lds_bytes(K, TOK, WAVES, Kind<X>::kBytes));
+    static std::atomic<uint64_t> done{0};
+    if (lds > 65536) {
+        const int st = ensure_lds_limit(reinterpret_cast<const void*>(few_kernel<X, TOK, WAVES, DEEP>), kMostLds, done);
+        if (st != UNISVQ_OK) return st;
+    }
+    // as many workgroups as the GPU holds, every one with as many blocks as any
+    const int64_t slots = kCUs * (WAVES == 8 && lds <= kMostLds / 2 ? 2 : 1);
+    int64_t total = 0;
+    for (int i = 0; i < b.count; ++i) total += b.p[i].N / kRowBlock;
+    const int64_t passes = (total + slots - 1) / slots;
+    int64_t blocks = 0;
+    for (int i = 0; i < b.count; ++i) {
+        b.p[i].wg_begin = static_cast<int>(blocks);
+        b.p[i].wgs = static_cast<int>((b.p[i].N / kRowBlock + passes - 1) / passes);
+        blocks += b.p[i].wgs;
+    }
+    few_kernel<X, TOK, WAVES, DEEP><<<static_cast<uint32_t>(blocks), 64 * WAVES, lds, s>>>(b);
+    return hipGetLastError() == hipSuccess ? UNISVQ_OK : UNISVQ_EHIP;
+}
+
+// Eight waves, and two workgroups on a CU, up to 32 groups, sixteen above: one
+// token, 57344 rows of 8192: 44.8 us with sixteen, 4096 rows of 11008: 9.0 (eight:
+// 10.2), 22016 rows of 4096: 13.0 (eight: 12.6).  A wave's share is taken in fours
+// of tiles where it is a multiple of four (8192 rows of 28672, shares of 14: 26.0 us
+// in twos, 30.2 in fours).
+template <typename X, int TOK>
+int launch_few(const Batch& b, int64_t K, hipStream_t s) {
+    const int64_t groups = K / kGroup;
+    if (groups <= 8) return launch_few<X, TOK, 8, 1>(b, K, s);
+    if (groups <= 16) return launch_few<X, TOK, 8, 2>(b, K, s);
+    if (groups <= 32) return launch_few<X, TOK, 8, 4>(b, K, s);
+    if ((groups + 15) / 16 % 4 == 0) return launch_few<X, TOK, 16, 4>(b, K, s);
+    return launch_few<X, TOK, 16, 2>(b, K, s);
+}
+
+int tok_of(int64_t M) { return M == 1 ? 1 : M == 2 ? 2 : 4; }
+
+// Up to sixteen tokens and few rows: a workgroup has a block of sixteen rows, its
+// waves share K out in runs of groups and read x from the L2, and their sums meet
+// in LDS; one launch, where tiles would have to be joined by a second.
+constexpr int kSomeWaves = 8;
+
+template <typename X>
+__global__ __launch_bounds__(64 * kSomeWaves) void some_kernel(const Batch b) {
+    typedef Kind<X> Q;
+    __shared__ f32x4 parts[kSomeWaves][64];
     Prob p = b.p[0];
 #pragma unroll
     for (int i = 1; i < kMaxBatch; ++i)
         if (i < b.count && static_cast<int>(blockIdx.x) >= b.p[i].wg_begin) p = b.p[i];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, c = lane >> 4;
-    const int64_t blocks = p.N / kRowBlock;
-    const int64_t L = static_cast<int>(blockIdx.x) - p.wg_begin, across = (blocks + RB - 1) / RB;
-    const int64_t rb0 = L % across * RB, tok0 = L / across * (16 * MT);
+    const int64_t rb = static_cast<int>(blockIdx.x) - p.wg_begin;
     const int K = p.K, groups = K / kGroup, quads = (groups + 3) / 4;
-    const int rbs = static_cast<int>(min(static_cast<int64_t>(RB), blocks - rb0));
-    const int toks = static_cast<int>(min(static_cast<int64_t>(16 * MT), b.M - tok0));
-    const __amdgpu_buffer_rsrc_t rw = make_rsrc(p.packed + rb0 * groups * kFourbitTile, static_cast<uint32_t>(rbs) * groups * kFourbitTile);
-    const __amdgpu_buffer_rsrc_t rs =
-        make_rsrc(p.packed + p.N * (K / 2) + rb0 * quads * kFourbitQuad, static_cast<uint32_t>(rbs) * quads * kFourbitQuad);
-    const __amdgpu_buffer_rsrc_t rx = make_rsrc(static_cast<const uint8_t*>(p.x) + tok0 * K * Q::kBytes,
-                                                static_cast<uint32_t>(toks) * K * Q::kBytes);
-    const int g0 = groups * wave / WAVES, g1 = groups * (wave + 1) / WAVES;
+    const __amdgpu_buffer_rsrc_t rw = make_rsrc(p.packed + rb * groups * kFourbitTile, groups * kFourbitTile);
+    const __amdgpu_buffer_rsrc_t rs = make_rsrc(p.packed + p.N * (K / 2) + rb * quads * kFourbitQuad, quads * kFourbitQuad);
+    const __amdgpu_buffer_rsrc_t rx = make_rsrc(p.x, static_cast<uint32_t>(b.M) * K * Q::kBytes);
+    const int g0 = groups * wave / kSomeWaves, g1 = groups * (wave + 1) / kSomeWaves;
 
     struct Step {
-        uint4 q[RB], x[MT][Q::kSteps];
-        uint32_t s[RB];
+        uint4 q, x[Q::kSteps];
+        uint32_t s;
     };
     const auto load = [&](int g, Step& t) {
         const uint32_t out = g < g1 ? 0u : kOutOfRange;
+        t.q = ld128_stream(rw, out | static_cast<uint32_t>(g * kFourbitTile + 16 * lane));
+        t.s = ld16(rs, out | static_cast<uint32_t>((g >> 2) * kFourbitQuad + 8 * n + 2 * (g & 3)));
 #pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            t.q[r] = ld128_stream(rw, out | static_cast<uint32_t>((r * groups + g) * kFourbitTile + 16 * lane));
-            t.s[r] = ld16(rs, out | static_cast<uint32_t>((r * quads + (g >> 2)) * kFourbitQuad + 8 * n + 2 * (g & 3)));
-        }
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int j = 0; j < Q::kSteps; ++j)
-                t.x[m][j] = ld128(rx, out | (static_cast<uint32_t>((16 * m + n) * K + g * kGroup) * Q::kBytes + Q::kChunk * c + Q::at(j)));
+        for (int j = 0; j < Q::kSteps; ++j)
+            t.x[j] = ld128(rx, out | (static_cast<uint32_t>(n * K + g * kGroup) * Q::kBytes + Q::kChunk * c + Q::at(j)));
     };
-    f32x4 acc[RB][MT] = {};
+    f32x4 acc{};
     const typename Q::Operand minus8 = Q::minus8();
-    const auto compute = [&](const Step& t) {
-        typename Q::Sum bias[MT];
+    const auto use = [&](const Step& t) {
+        typename Q::Operand x[Q::kSteps], w[Q::kSteps];
+        typename Q::Sum sum{};
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            bias[m] = typename Q::Sum{};
-#pragma unroll
-            for (int j = 0; j < Q::kSteps; ++j)
-                bias[m] = Q::mma(__builtin_bit_cast(typename Q::Operand, t.x[m][j]), minus8, bias[m]);
+        for (int j = 0; j < Q::kSteps; ++j) {
+            x[j] = __builtin_bit_cast(typename Q::Operand, t.x[j]);
+            sum = Q::mma(x[j], minus8, sum);
         }
+        Q::decode(t.q, w);
 #pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            typename Q::Operand w[Q::kSteps];
-            Q::decode(t.q[r], w);
-            const float s = static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(t.s[r])));
+        for (int j = 0; j < Q::kSteps; ++j) sum = Q::mma(x[j], w[j], sum);
+        const float s = static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(t.s)));
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                typename Q::Sum sum = bias[m];
-#pragma unroll
-                for (int j = 0; j < Q::kSteps; ++j) sum = Q::mma(__builtin_bit_cast(typename Q::Operand, t.x[m][j]), w[j], sum);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[r][m][i] = fmaf(s, static_cast<float>(sum[i]), acc[r][m][i]);
-            }
-        }
+        for (int i = 0; i < 4; ++i) acc[i] = fmaf(s, static_cast<float>(sum[i]), acc[i]);
     };
     Step even, odd;
     load(g0, even);
     for (int g = g0; g < g1; g += 2) {
         load(g + 1, odd);
-        compute(even);
+        use(even);
         load(g + 2, even);
-        if (g + 1 < g1) compute(odd);
+        if (g + 1 < g1) use(odd);
     }
 
-#pragma unroll
-    for (int r = 0; r < RB; ++r)
-#pragma unroll
-        for (int m = 0; m < MT; ++m) parts[wave][r * MT + m][lane] = acc[r][m];
+    parts[wave][lane] = acc;
     __syncthreads();
-    for (int i = threadIdx.x; i < RB * MT * 64; i += 64 * WAVES) {
-        const int tile = i >> 6, at = i & 63;
-        f32x4 sum = parts[0][tile][at];
+    if (wave) return;
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) sum += parts[w][tile][at];
-        const int r = tile / MT, row = at & 15, t0 = 16 * (tile % MT) + 4 * (at >> 4);
-        if (r >= rbs) continue;
+    for (int w = 1; w < kSomeWaves; ++w) acc += parts[w][lane];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (t0 + j < toks) {
-                const int64_t t = tok0 + t0 + j;
-                const float unit = Q::kI8 ? p.x_scales[t] : Q::kUnit;
-                store_out(p.y, t * p.N + (rb0 + r) * kRowBlock + row, sum[j] * unit, b.y_dtype);
-            }
+    for (int i = 0; i < 4; ++i) {
+        const int64_t t = 4 * c + i;
+        if (t < b.M) store_out(p.y, t * p.N + rb * kRowBlock + n, acc[i] * (Q::kI8 ? p.x_scales[t] : Q::kUnit), b.y_dtype);
     }
 }
 
-template <typename X, int MT, int RB, int WAVES>
-int launch_few(Batch b, hipStream_t s) {
-    int64_t blocks = 0;
+template <typename X>
+int launch_some(Batch b, hipStream_t s) {
+    int blocks = 0;
     for (int i = 0; i < b.count; ++i) {
-        b.p[i].wg_begin = static_cast<int>(blocks);
-        blocks += (b.p[i].N / kRowBlock + RB - 1) / RB * ((b.M + 16 * MT - 1) / (16 * MT));
-        if (blocks > (int64_t{1} << 32) / (64 * WAVES) - 1) return UNISVQ_EUNSUP;
+        b.p[i].wg_begin = blocks;
+        blocks += static_cast<int>(b.p[i].N / kRowBlock);
     }
-    few_kernel<X, MT, RB, WAVES><<<static_cast<uint32_t>(blocks), 64 * WAVES, 0, s>>>(b);
+    some_kernel<X><<<blocks, 64 * kSomeWaves, 0, s>>>(b);
     return hipGetLastError() == hipSuccess ? UNISVQ_OK : UNISVQ_EHIP;
 }
 
@@ -297,16 +428,16 @@ struct Tiled {
     static constexpr int kRow = kGroup * Q::kBytes;  // bytes of a token's group
     // bytes of activations, of sums (whole loads: what is behind the tokens becomes
     // zeros), and of a wave's codes and scales
-    static constexpr int kX = BM * kRow, kBias = SUMS ? 0 : 1024, kCodes = NB * 1024, kScales = 1024;
+    static constexpr int kX = (BM * kRow + 16 * kThreads - 1) / (16 * kThreads) * (16 * kThreads), kBias = SUMS ? 0 : 1024, kCodes = NB * 1024, kScales = 1024;
     static constexpr int kShared = kX + kBias, kOwn = kCodes + kScales;
     // Groups in LDS; where there is no room for two of everything, codes and
     // scales are one deep: their next ones are asked for when they have been read.
-    static constexpr int kRoom = 80 * 1024, kGroups = kRoom / (kShared + kWaves * kOwn);
+    static constexpr int kRoom = kMostLds / 2, kGroups = kRoom / (kShared + kWaves * kOwn);
     static constexpr int kStages = kGroups < 2 ? 2 : kGroups < 3 ? kGroups : 3, kCodeStages = kGroups < 2 ? 1 : kStages;
     static constexpr int kLds = kStages * kShared + kWaves * kCodeStages * kOwn;
     static_assert(kLds <= kRoom, "");
     static constexpr int kLoadsX = kX / (16 * kThreads), kLoadsCodes = kCodes / 1024;
-    static_assert(kX % (16 * kThreads) == 0 && BM <= 256, "");
+    static_assert(BM <= 256, "");
     static constexpr int kPass = NB <= 2 && MT % 2 == 0 ? 2 : 1;  // tiles of tokens at a time: independent products to follow one another
     // a wave's outputs of one tile of tokens, staged for whole-line stores
     static constexpr int kPitch = 16 * NB * 4 + 16;
@@ -395,7 +526,7 @@ __global__ __launch_bounds__(256, 2) void tiled_kernel(const TileBatch tb) {
 #pragma unroll
     for (int i = 0; i < C::kLoadsX; ++i) {
         const int at = i * C::kThreads + threadIdx.x, row = at / kChunks, chunk = at % kChunks ^ (row >> kTurn) % kChunks;
-        off_x[i] = static_cast<uint32_t>(min(row, toks - 1)) * K * Q::kBytes + 16 * chunk;
+        off_x[i] = row < C::BM ? static_cast<uint32_t>(min(row, toks - 1)) * K * Q::kBytes + 16 * chunk : kOutOfRange;
     }
     const uint32_t at16[1] = {16u * lane};
     const uint32_t off_s[1] = {lane >> 3 < NB ? min(static_cast<uint32_t>(lane) >> 3, here - 1) * quads * kFourbitQuad + 16 * (lane & 7)
@@ -547,9 +678,6 @@ __global__ __launch_bounds__(256) void join_kernel(const JoinBatch b) {
 }
 
 // How a batch is split: tokens and rows of a workgroup, and parts of K.
-constexpr int64_t kCUs = 256;
-constexpr int64_t kFewTokens = 16;
-
 struct Plan {
     int mt, nb;  // a workgroup has 16 mt tokens and 64 nb rows
     int splits[kMaxBatch];
@@ -558,11 +686,11 @@ struct Plan {
 };
 
 // Measured times of a group of columns in us (K 1024 and 4096, rows for 128 to 512
-// workgroups), [nb 2, 4][mt 2, 4, 6, 8]: a CU with one workgroup, and with two.
-constexpr float kAlone16[2][4] = {{0.59f, 0.77f, 1.02f, 0.0f}, {1.04f, 1.27f, 1.71f, 0.0f}};
-constexpr float kPaired16[2][4] = {{0.90f, 1.18f, 1.56f, 0.0f}, {1.82f, 2.13f, 2.83f, 0.0f}};
-constexpr float kAlone8[2][4] = {{0.46f, 0.61f, 0.73f, 0.85f}, {0.83f, 1.06f, 1.20f, 1.41f}};
-constexpr float kPaired8[2][4] = {{0.82f, 0.92f, 1.13f, 1.30f}, {1.56f, 1.84f, 2.01f, 2.55f}};
+// workgroups), [nb 2, 4][mt 1, 2, 4, 6, 8]: a CU with one workgroup, and with two.
+constexpr float kAlone16[2][5] = {{0.45f, 0.54f, 0.77f, 1.02f, 0.0f}, {0.90f, 1.04f, 1.27f, 1.71f, 0.0f}};
+constexpr float kPaired16[2][5] = {{0.78f, 0.95f, 1.18f, 1.56f, 0.0f}, {1.57f, 1.85f, 2.13f, 2.83f, 0.0f}};
+constexpr float kAlone8[2][5] = {{0.35f, 0.42f, 0.61f, 0.73f, 0.85f}, {0.82f, 0.88f, 1.06f, 1.20f, 1.41f}};
+constexpr float kPaired8[2][5] = {{0.80f, 0.82f, 0.92f, 1.13f, 1.30f}, {1.51f, 1.60f, 1.84f, 2.01f, 2.55f}};
 
 // The plan with the least expected time: what the workgroups take, two to a CU,
 // which start and end in 4 to 10 us; a launch for the sums of activations or a
@@ -574,13 +702,14 @@ Plan plan_of(const FourbitProblem* probs, int count, int64_t M, bool i8) {
     double read = 0;
     for (int i = 0; i < count; ++i) read = std::max(read, static_cast<double>(M * probs[i].K) * (i8 ? 1 : 2));
     for (int n = 0; n < 2; ++n)
-        for (int m = 0; m < (i8 ? 4 : 3); ++m) {
-            const int64_t BM = 32 * (m + 1), BN = 128 * (n + 1), m_tiles = (M + BM - 1) / BM;
+        for (int m = 0; m < (i8 ? 5 : 4); ++m) {
+            const int mt = m ? 2 * m : 1;
+            const int64_t BM = 16 * mt, BN = 128 * (n + 1), m_tiles = (M + BM - 1) / BM;
             if (m && BM >= 2 * M) continue;
             int64_t tiles = 0;
             for (int i = 0; i < count; ++i) tiles += (probs[i].N + BN - 1) / BN * m_tiles;
             for (int splits = 1; splits == 1 || (splits <= 12 && tiles * splits <= 2 * kCUs); ++splits) {
-                Plan p{2 * (m + 1), 2 * (n + 1), {}, false, false, 0};
+                Plan p{mt, 2 * (n + 1), {}, false, false, 0};
                 int64_t wgs = 0;
                 int groups = 0;
                 double parts = 0;
@@ -599,8 +728,8 @@ Plan plan_of(const FourbitProblem* probs, int count, int64_t M, bool i8) {
                                                      : static_cast<double>(wgs / (2 * kCUs)) * paired + (rest > kCUs ? paired : rest ? alone : 0.0);
                 const double steps = groups * rounds;
                 const double more = wgs <= kCUs ? 0.03 * steps : (i8 ? 0.05 : 0.2) * steps, launch = 2.2 + read / 4e6;
-                p.sums = more < launch;
-                p.us = 3.0 + 0.25 * (m + 1) * (n + 1) + steps + std::min(more, launch) + (p.split ? 2.0 + parts / 6e6 : 0.0);
+                p.sums = mt == 1 || more < launch;
+                p.us = 3.0 + 0.125 * mt * (n + 1) + steps + (p.sums ? more : launch) + (p.split ? 2.0 + parts / 6e6 : 0.0);
                 if (p.us < best.us) best = p;
             }
         }
@@ -650,6 +779,7 @@ int launch_tiles(TileBatch& tb, hipStream_t s) {
 
 template <typename X, int NB, bool SUMS>
 int launch_tokens(int mt, TileBatch& tb, hipStream_t s) {
+    if (mt == 1) return launch_tiles<X, 1, NB, true>(tb, s);
     if (mt == 2) return launch_tiles<X, 2, NB, SUMS>(tb, s);
     if (mt == 4) return launch_tiles<X, 4, NB, SUMS>(tb, s);
     if constexpr (Kind<X>::kI8)
@@ -692,22 +822,41 @@ int launch_tiled(const FourbitProblem* probs, int count, int64_t M, int y_dtype,
     return hipGetLastError() == hipSuccess ? UNISVQ_OK : UNISVQ_EHIP;
 }
 
+// Which kernel serves a batch: x in LDS for up to four tokens, where it fits; up to
+// sixteen tokens and 256 blocks of rows without a second launch (16 tokens, 4096 x
+// 4096: 7.6 us, tiles 9.1; 8192 x 8192 and twice 1024, 8 tokens of 8 bits: 16.4, tiles
+// 14.0); else tiles.
+enum Way { kFew, kSome, kTiled };
+
+Way way_of(const FourbitProblem* probs, int count, int64_t M, int size) {
+    int64_t most = 0, blocks = 0;
+    for (int i = 0; i < count; ++i) most = std::max(most, probs[i].K), blocks += probs[i].N / kRowBlock;
+    if (M <= 4 && blocks < (1 << 30) && few_lds_bytes(most, tok_of(M), most <= 4096 ? 8 : 16, size) <= kMostLds) return kFew;
+    return M <= 16 && blocks <= kCUs && most <= 8192 ? kSome : kTiled;
+}
+
 template <typename X>
 int launch_kind(const FourbitProblem* probs, int count, int64_t M, int y_dtype, uint8_t* workspace, size_t room, hipStream_t s) {
-    if (M > kFewTokens) return launch_tiled<X>(probs, count, M, y_dtype, workspace, room, s);
+    const Way way = way_of(probs, count, M, Kind<X>::kBytes);
+    if (way == kTiled) return launch_tiled<X>(probs, count, M, y_dtype, workspace, room, s);
     Batch b{};
     b.count = count, b.y_dtype = y_dtype, b.M = M;
-    for (int i = 0; i < count; ++i)
-        b.p[i] = Prob{probs[i].packed, probs[i].x, probs[i].x_scales, probs[i].y, probs[i].N, static_cast<int>(probs[i].K), 0};
-    if (M <= 16) return launch_few<X, 1, 1, 8>(b, s);
-    if (M <= 32) return launch_few<X, 2, 2, 8>(b, s);
-    return launch_few<X, 4, 2, 8>(b, s);
+    int64_t most = 0;
+    for (int i = 0; i < count; ++i) {
+        b.p[i] = Prob{probs[i].packed, probs[i].x, probs[i].x_scales, probs[i].y, probs[i].N, static_cast<int>(probs[i].K), 0, 0};
+        most = std::max(most, probs[i].K);
+    }
+    if (way == kSome) return launch_some<X>(b, s);
+    const int tok = tok_of(M);
+    return tok == 1 ? launch_few<X, 1>(b, most, s) : tok == 2 ? launch_few<X, 2>(b, most, s) : launch_few<X, 4>(b, most, s);
 }
 
 }  // namespace
 
 size_t fourbit_workspace_bytes(const FourbitProblem* probs, int count, int64_t M, int x_dtype) {
-    return M > kFewTokens ? places_of(probs, count, M, plan_of(probs, count, M, x_dtype == UNISVQ_I8)).bytes : 0;
+    const bool i8 = x_dtype == UNISVQ_I8;
+    if (way_of(probs, count, M, i8 ? 1 : 2) != kTiled) return 0;
+    return places_of(probs, count, M, plan_of(probs, count, M, i8)).bytes;
 }
 
 int launch_fourbit_batch(const FourbitProblem* probs, int count, int64_t M, int x_dtype, int y_dtype, void* workspace,
