@@ -357,25 +357,27 @@ struct Sums {
 
 template <typename X>
 __global__ __launch_bounds__(256) void sums_kernel(Sums a) {
-    const int64_t i = blockIdx.x * 16ll + (threadIdx.x >> 4), count = a.M * a.groups;
-    const int64_t at = min(i, count - 1), t = at / a.groups, g = at - t * a.groups;
-    const int64_t to = (t / kSumTile * a.groups + g) * kSumTile + t % kSumTile;
-    const int64_t from = t * a.groups * kGroup + g * kGroup + 8 * (threadIdx.x & 15);
-    if constexpr (std::is_same_v<X, int8_t>) {
-        const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const int8_t*>(a.x) + from);
-        int sum = 0;
+    const int64_t count = a.M * a.groups;
+    const int lane = threadIdx.x & 15;
+    for (int64_t i0 = blockIdx.x * 16ll; i0 < count; i0 += gridDim.x * 16ll) {
+        const int64_t i = i0 + (threadIdx.x >> 4), at = min(i, count - 1), t = at / a.groups, g = at - t * a.groups;
+        const int64_t to = (t / kSumTile * a.groups + g) * kSumTile + t % kSumTile;
+        const X* x = static_cast<const X*>(a.x) + at * kGroup + 8 * lane;
+        if constexpr (Kind<X>::kI8) {
+            const uint2 v = *reinterpret_cast<const uint2*>(x);
+            int sum = 0;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) sum += static_cast<int8_t>(v.x >> 8 * b) + static_cast<int8_t>(v.y >> 8 * b);
-        sum = over_lanes(sum, 4, [](int p, int q) { return p + q; });
-        if ((threadIdx.x & 15) == 0 && i < count) static_cast<int*>(a.bias)[to] = -8 * sum;
-    } else {
-        float f[8], sum = 0.0f;
-        load8(static_cast<const X*>(a.x) + from, f);
+            for (int b = 0; b < 4; ++b) sum += static_cast<int8_t>(v.x >> 8 * b) + static_cast<int8_t>(v.y >> 8 * b);
+            sum = over_lanes(sum, 4, [](int p, int q) { return p + q; });
+            if (lane == 0 && i < count) static_cast<int*>(a.bias)[to] = -8 * sum;
+        } else {
+            float f[8], sum = 0.0f;
+            load8(x, f);
 #pragma unroll
-        for (int b = 0; b < 8; ++b) sum += f[b];
-        sum = over_lanes(sum, 4, [](float p, float q) { return p + q; });
-        if ((threadIdx.x & 15) == 0 && i < count)
-            static_cast<float*>(a.bias)[to] = -8.0f / Kind<X>::kUnit * sum;
+            for (int b = 0; b < 8; ++b) sum += f[b];
+            sum = over_lanes(sum, 4, [](float p, float q) { return p + q; });
+            if (lane == 0 && i < count) static_cast<float*>(a.bias)[to] = -8.0f / Kind<X>::kUnit * sum;
+        }
     }
 }
 
@@ -438,7 +440,6 @@ struct Tiled {
     static_assert(kLds <= kRoom, "");
     static constexpr int kLoadsX = kX / (16 * kThreads), kLoadsCodes = kCodes / 1024;
     static_assert(BM <= 256, "");
-    static constexpr int kPass = NB <= 2 && MT % 2 == 0 ? 2 : 1;  // tiles of tokens at a time: independent products to follow one another
     // a wave's outputs of one tile of tokens, staged for whole-line stores
     static constexpr int kPitch = 16 * NB * 4 + 16;
     static_assert(kWaves * 16 * kPitch <= kLds, "");
@@ -590,42 +591,45 @@ __global__ __launch_bounds__(256, 2) void tiled_kernel(const TileBatch tb) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
         if (g + kAheadOwn < g1) issue_own(g + kAheadOwn, C::kCodeStages == 1 ? 0 : before);
+        // Tokens' operands are read one tile ahead (instructions on LDS stay where they
+        // are put, all others may move over them): 333 tokens through 3 x 4096 x 4096,
+        // 8 bits, 36 us for 39.
+        const uint8_t* from = lds + stage * C::kShared;
+        typename Q::Operand x[2][Q::kSteps];
+        typename Q::Sum bias[2];
+        const auto read = [&](int m) {
+            const int row = 16 * m + n;
+#pragma unroll
+            for (int k = 0; k < Q::kSteps; ++k) {
+                const int chunk = (Q::kChunk * c + Q::at(k)) / 16;
+                x[m & 1][k] = *reinterpret_cast<const typename Q::Operand*>(from + row * C::kRow + 16 * (chunk ^ (row >> kTurn) % kChunks));
+            }
+            bias[m & 1] = typename Q::Sum{};
+            if constexpr (!SUMS) bias[m & 1] = *reinterpret_cast<const typename Q::Sum*>(from + C::kX + 4 * (row - n + 4 * c));
+            __builtin_amdgcn_sched_barrier(0x1f);
+        };
+        read(0);
 #pragma unroll
         for (int j = 0; j < NB; ++j) Q::decode(q[j], w[j]);
-        const uint8_t* from = lds + stage * C::kShared;
+        // (before a wave that turns codes: 2048 tokens of 8 bits 222 us for 226; of 16 no gain)
+        if (Q::kI8) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int m0 = 0; m0 < MT; m0 += C::kPass) {
-            typename Q::Operand x[C::kPass][Q::kSteps];
-            typename Q::Sum bias[C::kPass], sum[C::kPass][NB];
-#pragma unroll
-            for (int m = 0; m < C::kPass; ++m) {
-                const int row = 16 * (m0 + m) + n;
-#pragma unroll
-                for (int k = 0; k < Q::kSteps; ++k) {
-                    const int chunk = (Q::kChunk * c + Q::at(k)) / 16;
-                    x[m][k] = *reinterpret_cast<const typename Q::Operand*>(from + row * C::kRow + 16 * (chunk ^ (row >> kTurn) % kChunks));
-                }
-                bias[m] = typename Q::Sum{};
-                if constexpr (!SUMS) bias[m] = *reinterpret_cast<const typename Q::Sum*>(from + C::kX + 4 * (row - n + 4 * c));
-            }
+        for (int m = 0; m < MT; ++m) {
+            if (m + 1 < MT) read(m + 1);
+            typename Q::Sum sum[NB];
             if constexpr (SUMS)
 #pragma unroll
-                for (int k = 0; k < Q::kSteps; ++k)
-#pragma unroll
-                    for (int m = 0; m < C::kPass; ++m) bias[m] = Q::mma(x[m][k], minus8, bias[m]);
+                for (int k = 0; k < Q::kSteps; ++k) bias[m & 1] = Q::mma(x[m & 1][k], minus8, bias[m & 1]);
 #pragma unroll
             for (int k = 0; k < Q::kSteps; ++k)
 #pragma unroll
-                for (int m = 0; m < C::kPass; ++m)
+                for (int j = 0; j < NB; ++j) sum[j] = Q::mma(x[m & 1][k], w[j][k], k ? sum[j] : bias[m & 1]);
 #pragma unroll
-                    for (int j = 0; j < NB; ++j) sum[m][j] = Q::mma(x[m][k], w[j][k], k ? sum[m][j] : bias[m]);
+            for (int j = 0; j < NB; ++j)
 #pragma unroll
-            for (int m = 0; m < C::kPass; ++m)
-#pragma unroll
-                for (int j = 0; j < NB; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[m0 + m][j][i] = fmaf(s[j], static_cast<float>(sum[m][j][i]), acc[m0 + m][j][i]);
+                for (int i = 0; i < 4; ++i) acc[m][j][i] = fmaf(s[j], static_cast<float>(sum[j][i]), acc[m][j][i]);
         }
+        if (Q::kI8) __builtin_amdgcn_s_setprio(0);
         stage = stage == kAhead ? 0 : stage + 1;
     }
     __syncthreads();
@@ -686,10 +690,11 @@ struct Plan {
 };
 
 // Measured times of a group of columns in us (K 1024 and 4096, rows for 128 to 512
-// workgroups), [nb 2, 4][mt 1, 2, 4, 6, 8]: a CU with one workgroup, and with two.
-constexpr float kAlone16[2][5] = {{0.45f, 0.54f, 0.77f, 1.02f, 0.0f}, {0.90f, 1.04f, 1.27f, 1.71f, 0.0f}};
+// workgroups; the first two alone with K 28672), [nb 2, 4][mt 1, 2, 4, 6, 8]: a CU
+// with one workgroup, and with two.
+constexpr float kAlone16[2][5] = {{0.54f, 0.60f, 0.77f, 1.02f, 0.0f}, {0.90f, 1.04f, 1.27f, 1.71f, 0.0f}};
 constexpr float kPaired16[2][5] = {{0.78f, 0.95f, 1.18f, 1.56f, 0.0f}, {1.57f, 1.85f, 2.13f, 2.83f, 0.0f}};
-constexpr float kAlone8[2][5] = {{0.35f, 0.42f, 0.61f, 0.73f, 0.85f}, {0.82f, 0.88f, 1.06f, 1.20f, 1.41f}};
+constexpr float kAlone8[2][5] = {{0.45f, 0.50f, 0.61f, 0.73f, 0.85f}, {0.82f, 0.88f, 1.06f, 1.20f, 1.41f}};
 constexpr float kPaired8[2][5] = {{0.80f, 0.82f, 0.92f, 1.13f, 1.30f}, {1.51f, 1.60f, 1.84f, 2.01f, 2.55f}};
 
 // The plan with the least expected time: what the workgroups take, two to a CU,
@@ -802,7 +807,7 @@ int launch_tiled(const FourbitProblem* probs, int count, int64_t M, int y_dtype,
                            static_cast<int>(probs[i].K), plan.splits[i], 0};
         if (at.first[i] && !plan.sums) {
             const Sums a{probs[i].x, workspace + at.bias[i], M, groups};
-            sums_kernel<X><<<static_cast<uint32_t>((M * groups + 15) / 16), 256, 0, s>>>(a);
+            sums_kernel<X><<<static_cast<uint32_t>(std::min<int64_t>((M * groups + 15) / 16, 1 << 20)), 256, 0, s>>>(a);
         }
     }
     const int st = plan.nb == 2 ? (plan.sums ? launch_tokens<X, 2, true>(plan.mt, tb, s) : launch_tokens<X, 2, false>(plan.mt, tb, s))

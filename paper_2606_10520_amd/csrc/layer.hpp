@@ -102,17 +102,15 @@ __device__ inline V over_lanes(V x, int steps, F op) {
 }
 
 // The same over all threads of a workgroup of whole waves, by way of sixteen
-// words of LDS; `fresh` words for each use.
+// words of LDS (other ones for each use); of operations that zero does not change.
 template <typename V, typename F>
 __device__ inline V over_block(V x, V* words, F op) {
     x = over_lanes(x, 6, op);
-    const int waves = blockDim.x >> 6;
+    const int waves = blockDim.x >> 6, lane = threadIdx.x & 15;
     if (waves == 1) return x;
     if ((threadIdx.x & 63) == 0) words[threadIdx.x >> 6] = x;
     __syncthreads();
-    V all = words[0];
-    for (int i = 1; i < waves; ++i) all = op(all, words[i]);
-    return all;
+    return over_lanes(lane < waves ? words[lane] : V{}, 4, op);
 }
 
 // A row held in 8 bits: code * scale, scale = a / 127 with a the largest

@@ -1200,32 +1200,44 @@ def _types():
 def _flat(t, what: str, device: int, shape=None, dtypes=None):
     """A [tokens][n] device tensor of one of dtypes (None: fp16 or bf16), its last axis contiguous (the C entry refuses row
     strides that are not multiples of 8): checked, and as (pointer, row stride)."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1) or (shape is not None and t.shape != shape):
+    strides = t.stride()
+    if len(strides) != 2 or strides[1] != 1 or (shape is not None and t.shape != shape):
         raise ValueError(f"{what} must be [tokens][n]{'' if shape is None else ' ' + str(tuple(shape))} with contiguous rows, "
-                         f"got {tuple(t.shape)}, strides {t.stride()}")
+                         f"got {tuple(t.shape)}, strides {strides}")
     if t.dtype not in (_halves() if dtypes is None else dtypes):
         raise TypeError(f"{what} is {t.dtype}, expected {'fp16 or bf16' if dtypes is None else ' or '.join(map(str, dtypes))}")
     if t.get_device() != device or device < 0:
         _elsewhere(t, what, device)
-    return t.data_ptr(), t.stride(0)
+    return t.data_ptr(), strides[0]
+
+
+def _new_rows(like, dtype, stream):
+    """A new contiguous tensor of like's shape."""
+    if stream is None and like.is_contiguous():
+        return _torch().empty_like(like, dtype=dtype)
+    return _new(like.shape, dtype, like.device, stream)
 
 
 def _row_output(out, out_dtype, like, device: int, stream):
-    """The caller's out (a tensor, or a pair of bytes and scales) or a new one of out_dtype (None: like's): out itself,
-    (pointer, row stride), its type's code, and the pointer of its scales."""
+    """The caller's out (a tensor, or a pair of bytes and scales) or a new one of out_dtype (None: like's): out itself, its
+    pointer, row stride, type's code, and the pointer of its scales."""
     torch = _torch()
     tokens, n = like.shape
     if out is None:
         dt = out_dtype or like.dtype
-        out = _new((tokens, n), dt, like.device, stream)
-        if dt is torch.int8:
-            out = out, _new((tokens,), torch.float32, like.device, stream)
+        if dt not in _types():
+            raise TypeError(f"out_dtype is {dt}, expected {like.dtype}, fp32 or int8")
+        y = _new_rows(like, dt, stream)
+        if dt is not torch.int8:
+            return y, y.data_ptr(), n, _TYPES[dt], None
+        scales = _new((tokens,), torch.float32, like.device, stream)
+        return (y, scales), y.data_ptr(), n, I8, scales.data_ptr()
     pair = type(out) in (tuple, list)
     y, scales = out if pair else (out, None)
     if y.dtype not in _types() or (out_dtype is not None and y.dtype is not out_dtype) or (y.dtype is torch.int8) != pair:
         raise TypeError("out is fp16, bf16 or fp32 rows, or a pair of int8 rows and fp32 scales; and of out_dtype where that is given")
-    rows = _flat(y, "out", device, like.shape, (y.dtype,))
-    return out, rows, _TYPES[y.dtype], _words(scales, tokens, "the scales of out", torch.float32, device)
+    at, stride = _flat(y, "out", device, like.shape, (y.dtype,))
+    return out, at, stride, _TYPES[y.dtype], _words(scales, tokens, "the scales of out", torch.float32, device)
 
 
 def rmsnorm(x, weight, eps: float = 1e-5, residual=None, residual_out=None, weight_offset: float = 0.0, out=None,
@@ -1234,24 +1246,29 @@ def rmsnorm(x, weight, eps: float = 1e-5, residual=None, residual_out=None, weig
     the addition of residual [tokens][n] (x's type or fp32) where it is given.  Returns y, or with a residual (y, h), h =
     x + residual of residual's type (residual_out, which may be residual or x, or a new tensor).  y is of out_dtype: x's
     (None), fp32, or int8, and then a pair (codes, scales) that fourbit_gemm takes; out: a tensor or pair to write."""
-    torch = _torch()
-    device = x.get_device()
+    device, shape, dt = x.get_device(), x.shape, x.dtype
     xr = _flat(x, "x", device)
-    wide = (x.dtype, torch.float32)
+    wide = (dt, _torch().float32)
     if weight.dtype not in wide:
-        raise TypeError(f"weight is {weight.dtype}, expected {wide[0]} or fp32")
-    wp = _words(weight, x.shape[1], "weight", weight.dtype, device)
-    rr, hr, rt = (None, 0), (None, 0), F32
+        raise TypeError(f"weight is {weight.dtype}, expected {dt} or fp32")
+    wp = _words(weight, shape[1], "weight", weight.dtype, device)
+    types = _types()
+    rp = hp = None
+    rs = hs = 0
+    rt = F32
     if residual is not None:
-        rr = _flat(residual, "residual", device, x.shape, wide)
+        rp, rs = _flat(residual, "residual", device, shape, wide)
+        rt = types[residual.dtype]
         if residual_out is None:
-            residual_out = _new(x.shape, residual.dtype, x.device, stream)
-        hr, rt = _flat(residual_out, "residual_out", device, x.shape, (residual.dtype,)), _types()[residual.dtype]
+            residual_out = _new_rows(residual, residual.dtype, stream)
+            hp, hs = residual_out.data_ptr(), shape[1]
+        else:
+            hp, hs = _flat(residual_out, "residual_out", device, shape, (residual.dtype,))
     elif residual_out is not None:
         raise ValueError("residual_out without a residual")
-    out, yr, yt, scales = _row_output(out, out_dtype, x, device, stream)
-    _launch("unisvq_rmsnorm", device, stream, *x.shape, *xr, _types()[x.dtype], wp, _TYPES[weight.dtype], weight_offset,
-            eps, *rr, *hr, rt, *yr, yt, scales)
+    out, yp, ys, yt, scales = _row_output(out, out_dtype, x, device, stream)
+    _launch("unisvq_rmsnorm", device, stream, shape[0], shape[1], *xr, types[dt], wp, types[weight.dtype], weight_offset, eps,
+            rp, rs, hp, hs, rt, yp, ys, yt, scales)
     return out if residual is None else (out, residual_out)
 
 
@@ -1261,13 +1278,13 @@ ACTIVATIONS = {"silu": 0, "gelu": 1}
 def gated(gate, up, activation: str = "silu", out=None, out_dtype=None, stream=None):
     """act(gate) * up of rows [tokens][n] (fp16 or bf16, any row strides, so the halves of one fused row serve); activation
     "silu" or "gelu" (its tanh form).  out, out_dtype: as rmsnorm's; out may be gate or up."""
-    device = gate.get_device()
+    device, shape, dt = gate.get_device(), gate.shape, gate.dtype
     gr = _flat(gate, "gate", device)
-    ur = _flat(up, "up", device, gate.shape, (gate.dtype,))
+    ur = _flat(up, "up", device, shape, (dt,))
     if activation not in ACTIVATIONS:
         raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, got {activation!r}")
-    out, yr, yt, scales = _row_output(out, out_dtype, gate, device, stream)
-    _launch("unisvq_gated", device, stream, *gate.shape, *gr, *ur, _types()[gate.dtype], ACTIVATIONS[activation], *yr, yt,
+    out, yp, ys, yt, scales = _row_output(out, out_dtype, gate, device, stream)
+    _launch("unisvq_gated", device, stream, shape[0], shape[1], *gr, *ur, _types()[dt], ACTIVATIONS[activation], yp, ys, yt,
             scales)
     return out
 
@@ -1351,36 +1368,44 @@ def fourbit_gemm_batched(problems, out_dtype=None, workspace=None, stream=None):
     arr = (FourbitProblem * count)()
     outs, shapes = [], []
     device = problems[0][0].get_device()
-    M = kind = None
-    for i, (packed, N, K, x, out) in enumerate(problems):
-        pair = type(x) in (tuple, list)
-        v, scales = x if pair else (x, None)
-        if M is None:
-            M, kind = v.numel() // max(K, 1), v.dtype
-            if (kind is not torch.int8 if pair else kind not in _halves()):
-                raise TypeError(f"activations are fp16, bf16, or a pair of int8 codes and fp32 scales, got {kind}{' in a pair' if pair else ''}")
-            if M < 1:
-                raise ValueError("x holds no tokens")
-        if v.dtype is not kind or pair is not (kind is torch.int8):
-            raise ValueError("all problems need the same activation type")
-        xp = _words(v, M * K, f"x of {M} tokens", kind, device)
-        if v.shape[-1] != K:
-            raise ValueError(f"x has {v.shape[-1]} columns, the weights K = {K}")
-        shapes.append((N, K))
-        pp = _words(packed, _fourbit_size(N, K), "packed", torch.uint8, device)
+    last = kind = None
+    M = 0
+    types = _types()
+    for a, (packed, N, K, x, out) in zip(arr, problems):
+        if x is not last:  # (q, k and v read one x, and so do gate and up)
+            last = x
+            pair = type(x) in (tuple, list)
+            v, scales = x if pair else (x, None)
+            if kind is None:
+                kind, M = v.dtype, v.numel() // max(K, 1)
+                if kind is not torch.int8 if pair else kind not in _halves():
+                    raise TypeError(f"activations are fp16, bf16, or a pair of int8 codes and fp32 scales, got {kind}{' in a pair' if pair else ''}")
+                if M < 1:
+                    raise ValueError("x holds no tokens")
+            if v.dtype is not kind or pair is not (kind is torch.int8):
+                raise ValueError("all problems need the same activation type")
+            columns = v.shape[-1]
+            xp = _words(v, M * columns, f"x of {M} tokens", kind, device)
+            sp = _words(scales, M, "the scales of x", torch.float32, device) if pair else None
+        if columns != K:
+            raise ValueError(f"x has {columns} columns, the weights K = {K}")
+        a.N, a.K, a.x, a.x_scales = N, K, xp, sp
+        a.packed = _words(packed, _fourbit_size(N, K), "packed", torch.uint8, device)
         if out is None:
-            out = _new((M, N), out_dtype or (torch.float16 if pair else kind), v.device, stream)
-        elif out_dtype is not None and out.dtype is not out_dtype:
-            raise TypeError(f"out is {out.dtype}, out_dtype {out_dtype}")
-        outs.append(out)
-        if out.dtype is not outs[0].dtype or out.dtype is torch.int8 or out.dtype not in _types():
+            dt = out_dtype or (torch.float16 if pair else kind)
+            out = v.new_empty((M, N), dtype=dt) if stream is None else _new((M, N), dt, v.device, stream)
+            a.y = out.data_ptr()
+        else:
+            if out_dtype is not None and out.dtype is not out_dtype:
+                raise TypeError(f"out is {out.dtype}, out_dtype {out_dtype}")
+            a.y = _words(out, M * N, "out", out.dtype, device)
+        if out.dtype is not (outs[0] if outs else out).dtype or types.get(out.dtype, I8) == I8:
             raise TypeError("outputs are fp16, bf16 or fp32, all of one type")
-        a = arr[i]
-        a.N, a.K, a.packed, a.x, a.y = N, K, pp, xp, _words(out, M * N, "out", out.dtype, device)
-        a.x_scales = _words(scales, M, "the scales of x", torch.float32, device) if pair else None
-    code = _types()[kind]
+        outs.append(out)
+        shapes.append((N, K))
+    code = types[kind]
     ws, wp, size = _scratch(workspace, _fourbit_workspace(tuple(shapes), M, code), outs[0], stream)
-    _launch("unisvq_fourbit_gemm_batched", device, stream, arr, count, M, code, _TYPES[outs[0].dtype], wp, size)
+    _launch("unisvq_fourbit_gemm_batched", device, stream, arr, count, M, code, types[outs[0].dtype], wp, size)
     return outs
 
 

@@ -136,6 +136,9 @@ class On:
     def get_device(self):
         return self.index
 
+    def new_empty(self, shape, dtype):
+        return On(torch.empty(shape, dtype=dtype), self.index)
+
 
 @pytest.fixture
 def calls(monkeypatch):
@@ -164,6 +167,7 @@ def calls(monkeypatch):
     monkeypatch.setattr(u, "_current", (lambda: state.current, lambda index: 1000 + index), raising=False)
     monkeypatch.setattr(u, "_new", lambda shape, dtype, device, stream: On(torch.empty(shape, dtype=dtype), torch.device(device).index))
     monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(torch, "empty_like", lambda t, dtype: t.new_empty(t.shape, dtype))
     u._fourbit_workspace.cache_clear(), u._fourbit_size.cache_clear()
     yield made
     u._fourbit_workspace.cache_clear(), u._fourbit_size.cache_clear()
