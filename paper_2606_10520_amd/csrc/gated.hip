@@ -63,6 +63,39 @@ __global__ __launch_bounds__(1024) void gated_i8_kernel(GatedArgs a) {
     }
 }
 
+// Longer rows, gated twice: for the scale and for the codes.
+template <typename T>
+__global__ __launch_bounds__(1024) void long_gated_i8_kernel(GatedArgs a) {
+    __shared__ uint32_t tops[16];
+    const int runs = a.n / 8, lane = threadIdx.x;
+    for (int64_t t = blockIdx.x; t < a.tokens; t += gridDim.x) {
+        const auto run = [&](int r, float(&g)[8]) {
+            float u[8];
+            load8(static_cast<const T*>(a.gate) + t * a.gate_stride + 8 * r, g);
+            load8(static_cast<const T*>(a.up) + t * a.up_stride + 8 * r, u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) g[i] = gated(g[i], u[i], a.act == UNISVQ_GELU);
+        };
+        uint32_t most = 0;
+#pragma unroll 4
+        for (int r = lane; r < runs; r += 1024) {
+            float g[8];
+            run(r, g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) most = max(most, magnitude(g[i]));
+        }
+        const RowScale k = row_scale(over_block(most, tops, [](uint32_t p, uint32_t q) { return max(p, q); }));
+        if (lane == 0) a.scales[t] = k.scale;
+#pragma unroll 4
+        for (int r = lane; r < runs; r += 1024) {
+            float g[8];
+            run(r, g);
+            *reinterpret_cast<uint2*>(static_cast<int8_t*>(a.y) + t * a.y_stride + 8 * r) = codes_of(g, k.inv);
+        }
+        __syncthreads();  // (the words of LDS serve the next row)
+    }
+}
+
 template <typename T>
 void launch(const GatedArgs& a, hipStream_t s) {
     const int runs = a.n / 8;
@@ -80,7 +113,7 @@ void launch(const GatedArgs& a, hipStream_t s) {
     else if (runs <= 4096)
         gated_i8_kernel<T, 4><<<blocks, threads(4), 0, s>>>(a);
     else
-        gated_i8_kernel<T, 8><<<blocks, threads(8), 0, s>>>(a);
+        long_gated_i8_kernel<T><<<blocks, 1024, 0, s>>>(a);
 }
 
 }  // namespace

@@ -31,8 +31,7 @@ struct GatedArgs {
 };
 hipError_t launch_gated(const GatedArgs& a, hipStream_t s);
 
-// Longest row whose values a workgroup keeps in registers: 1024 threads of
-// eight runs of eight.
+// Longest row that a workgroup takes.
 constexpr int kMaxRow = 65536;
 
 // 4-bit weights: tiles of 16 rows x 128 columns of 1 KB, [row block][group],

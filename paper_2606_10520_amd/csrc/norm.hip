@@ -110,6 +110,105 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void norm_kernel(NormArgs a, int
     }
 }
 
+// Rows too long for registers (1024 threads have 128 each): a thread's runs four at
+// a time, read again from the L2 for the result, and once more for 8 bits.  The
+// stream is read back from where it was stored, by the thread that stored it.
+template <typename T>
+__device__ __forceinline__ void load_four(const void* p, int64_t row, bool wide, const int (&at)[4], float (&f)[4][8]) {
+    if (wide) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) load8(static_cast<const float*>(p) + row + at[v], f[v]);
+    } else {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) load8(static_cast<const T*>(p) + row + at[v], f[v]);
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(1024) void long_norm_kernel(NormArgs a) {
+    __shared__ float sums[16];
+    __shared__ uint32_t tops[16];
+    const int lane = threadIdx.x, runs = a.n / 8;
+    const bool wide = a.r && a.r_dtype == UNISVQ_F32;
+    const auto places = [&](int r0, int (&at)[4]) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) at[v] = 8 * min(r0 + v * 1024 + lane, runs - 1);
+    };
+    for (int64_t t = blockIdx.x; t < a.tokens; t += gridDim.x) {
+        float sum = 0.0f;
+        for (int r0 = 0; r0 < runs; r0 += 4096) {
+            int at[4];
+            float h[4][8];
+            places(r0, at);
+            load_four<T>(a.x, t * a.x_stride, false, at, h);
+            if (a.r) {
+                float r[4][8];
+                load_four<T>(a.r, t * a.r_stride, wide, at, r);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        h[v][i] += r[v][i];
+                        if (!wide) h[v][i] = static_cast<float>(static_cast<T>(h[v][i]));
+                    }
+                    if (r0 + v * 1024 + lane < runs) store_row8<T>(a.h, t * a.h_stride + at[v], h[v], wide);
+                }
+            }
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                float s = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s = fmaf(h[v][i], h[v][i], s);
+                sum += r0 + v * 1024 + lane < runs ? s : 0.0f;
+            }
+        }
+        sum = over_block(sum, sums, [](float p, float q) { return p + q; });
+        const float f = __builtin_amdgcn_rsqf(sum / static_cast<float>(a.n) + a.eps);
+        const void* from = a.r ? a.h : a.x;
+        const int64_t row = t * (a.r ? a.h_stride : a.x_stride);
+        const auto result = [&](const int(&at)[4], float(&h)[4][8]) {
+            float w[4][8];
+            load_four<T>(from, row, wide, at, h);
+            load_four<T>(a.w, 0, a.w_dtype == UNISVQ_F32, at, w);
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) h[v][i] = h[v][i] * f * (w[v][i] + a.offset);
+        };
+        RowScale k{};
+        if (a.y_dtype == UNISVQ_I8) {
+            uint32_t most = 0;
+            for (int r0 = 0; r0 < runs; r0 += 4096) {
+                int at[4];
+                float h[4][8];
+                places(r0, at);
+                result(at, h);
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) most = max(most, magnitude(h[v][i]));
+            }
+            k = row_scale(over_block(most, tops, [](uint32_t p, uint32_t q) { return max(p, q); }));
+            if (lane == 0) a.scales[t] = k.scale;
+        }
+        for (int r0 = 0; r0 < runs; r0 += 4096) {
+            int at[4];
+            float h[4][8];
+            places(r0, at);
+            result(at, h);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                if (r0 + v * 1024 + lane >= runs) continue;
+                if (a.y_dtype == UNISVQ_I8)
+                    *reinterpret_cast<uint2*>(static_cast<int8_t*>(a.y) + t * a.y_stride + at[v]) = codes_of(h[v], k.inv);
+                else
+                    store_row8<T>(a.y, t * a.y_stride + at[v], h[v], a.y_dtype == UNISVQ_F32);
+            }
+        }
+        __syncthreads();  // (the words of LDS serve the next row)
+    }
+}
+
 template <typename T>
 void launch(const NormArgs& a, hipStream_t s) {
     constexpr int64_t kMostBlocks = 1 << 20;  // the rest of the rows in turn
@@ -128,10 +227,8 @@ void launch(const NormArgs& a, hipStream_t s) {
         norm_kernel<T, 1, true><<<blocks, threads(1), 0, s>>>(a, 0);
     else if (runs <= 2048)
         norm_kernel<T, 2, true><<<blocks, threads(2), 0, s>>>(a, 0);
-    else if (runs <= 4096)
-        norm_kernel<T, 4, true><<<blocks, threads(4), 0, s>>>(a, 0);
     else
-        norm_kernel<T, 8, true><<<blocks, threads(8), 0, s>>>(a, 0);
+        long_norm_kernel<T><<<blocks, 1024, 0, s>>>(a);
 }
 
 }  // namespace
