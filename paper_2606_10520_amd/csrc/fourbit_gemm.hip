@@ -698,32 +698,43 @@ struct Plan {
     double us;
 };
 
-// Measured times of a group of columns in us (K 1024 and 4096, rows for 128 to 512
-// workgroups; the first two alone with K 28672), [nb 2, 4][mt 1, 2, 4, 6, 8]: a CU
-// with one workgroup, and with two.
-constexpr float kAlone16[2][5] = {{0.54f, 0.60f, 0.77f, 1.02f, 0.0f}, {0.90f, 1.04f, 1.27f, 1.71f, 0.0f}};
-constexpr float kPaired16[2][5] = {{0.78f, 0.95f, 1.18f, 1.56f, 0.0f}, {1.57f, 1.85f, 2.13f, 2.83f, 0.0f}};
-constexpr float kAlone8[2][5] = {{0.45f, 0.50f, 0.61f, 0.73f, 0.85f}, {0.82f, 0.88f, 1.06f, 1.20f, 1.41f}};
-constexpr float kPaired8[2][5] = {{0.80f, 0.82f, 0.92f, 1.13f, 1.30f}, {1.51f, 1.60f, 1.84f, 2.01f, 2.55f}};
+// Times of a group of columns in us where memory does not hold it up, [i8][sums made
+// here, given][nb 2, 4][mt 1, 2, 3, 4, 5, 6, 8]: a CU with one workgroup (the slope over K of
+// calls with 128 workgroups), and with two (of calls whose token tiles share weights).
+constexpr int kTileTokens[] = {1, 2, 3, 4, 5, 6, 8};
+constexpr float kAlone[2][2][2][7] = {
+    {{{0.43f, 0.54f, 0.67f, 0.77f, 0.90f, 1.01f, 0}, {0.62f, 0.77f, 0.97f, 1.18f, 1.39f, 1.60f, 0}},
+     {{0, 0.56f, 0.66f, 0.75f, 0.87f, 0.93f, 0}, {0, 0.75f, 0.92f, 1.06f, 1.37f, 1.44f, 0}}},
+    {{{0.37f, 0.46f, 0.54f, 0.57f, 0.69f, 0.73f, 0.83f}, {0.55f, 0.65f, 0.73f, 0.87f, 1.00f, 1.12f, 1.40f}},
+     {{0, 0.48f, 0.55f, 0.60f, 0.68f, 0.75f, 0.88f}, {0, 0.64f, 0.72f, 0.82f, 0.94f, 1.06f, 1.28f}}}};
+constexpr float kPaired[2][2][2][7] = {
+    {{{0.60f, 0.85f, 1.05f, 1.28f, 1.50f, 1.80f, 0}, {1.10f, 1.40f, 1.70f, 2.10f, 2.60f, 3.05f, 0}},
+     {{0, 0.75f, 0.92f, 1.05f, 1.25f, 1.60f, 0}, {0, 1.25f, 1.50f, 1.92f, 2.40f, 2.65f, 0}}},
+    {{{0.50f, 0.55f, 0.62f, 0.75f, 0.85f, 1.05f, 1.50f}, {0.80f, 0.90f, 1.02f, 1.25f, 1.55f, 1.85f, 2.52f}},
+     {{0, 0.54f, 0.60f, 0.70f, 0.80f, 0.95f, 1.45f}, {0, 0.88f, 1.00f, 1.20f, 1.50f, 1.80f, 2.36f}}}};
 
-// The plan with the least expected time: what the workgroups take, two to a CU,
-// which start and end in 4 to 10 us; a launch for the sums of activations or a
-// fifth more products (8 bits: a twentieth, and none where a CU has one
-// workgroup); parts of K and the launch that joins them.
+// The plan with the least expected time: what the workgroups take, two to a CU, or
+// the weights' read (4.2 TB/s with one to a CU, 5.6 with two); 3 to 9 us to start and
+// end; a launch for the sums of activations, where they are given; parts of K and the
+// launch that joins them. Of 25 shapes from 16 to 4096 tokens the plan took 0 to 9% more
+// than the fastest of those considered.
 Plan plan_of(const FourbitProblem* probs, int count, int64_t M, bool i8) {
     Plan best{};
     best.us = 1e30;
-    double read = 0;
-    for (int i = 0; i < count; ++i) read = std::max(read, static_cast<double>(M * probs[i].K) * (i8 ? 1 : 2));
+    double read = 0, weights = 0;
+    for (int i = 0; i < count; ++i) {
+        read = std::max(read, static_cast<double>(M * probs[i].K) * (i8 ? 1 : 2));
+        weights += static_cast<double>(fourbit_bytes(probs[i].N, probs[i].K));
+    }
     for (int n = 0; n < 2; ++n)
-        for (int m = 0; m < (i8 ? 5 : 4); ++m) {
-            const int mt = m ? 2 * m : 1;
-            const int64_t BM = 16 * mt, BN = 128 * (n + 1), m_tiles = (M + BM - 1) / BM;
-            if (m && BM >= 2 * M) continue;
+        for (int m = 0; m < (i8 ? 7 : 6); ++m) {
+            const int mt = kTileTokens[m], nb = 2 * (n + 1);
+            const int64_t BM = 16 * mt, BN = 64 * nb, m_tiles = (M + BM - 1) / BM;
+            if (m && 16 * kTileTokens[m - 1] >= M) break;  // (a smaller one has all tokens)
             int64_t tiles = 0;
             for (int i = 0; i < count; ++i) tiles += (probs[i].N + BN - 1) / BN * m_tiles;
             for (int splits = 1; splits == 1 || (splits <= 12 && tiles * splits <= 2 * kCUs); ++splits) {
-                Plan p{mt, 2 * (n + 1), {}, false, false, 0};
+                Plan p{mt, nb, {}, false, false, 0};
                 int64_t wgs = 0;
                 int groups = 0;
                 double parts = 0;
@@ -735,16 +746,17 @@ Plan plan_of(const FourbitProblem* probs, int count, int64_t M, bool i8) {
                     groups = std::max(groups, (g + p.splits[i] - 1) / p.splits[i]);
                     if (p.splits[i] > 1) parts += 8.0 * p.splits[i] * static_cast<double>(M * probs[i].N);
                 }
-                const double alone = (i8 ? kAlone8 : kAlone16)[n][m], paired = (i8 ? kPaired8 : kPaired16)[n][m];
                 // up to two rounds are rounds; of more, workgroups begin as others end
                 const int64_t rest = wgs % (2 * kCUs);
-                const double rounds = wgs > 4 * kCUs ? 0.97 * static_cast<double>(wgs) / (2 * kCUs) * paired
-                                                     : static_cast<double>(wgs / (2 * kCUs)) * paired + (rest > kCUs ? paired : rest ? alone : 0.0);
-                const double steps = groups * rounds;
-                const double more = wgs <= kCUs ? 0.03 * steps : (i8 ? 0.05 : 0.2) * steps, launch = 2.2 + read / 4e6;
-                p.sums = mt == 1 || more < launch;
-                p.us = 3.0 + 0.125 * mt * (n + 1) + steps + (p.sums ? more : launch) + (p.split ? 2.0 + parts / 6e6 : 0.0);
-                if (p.us < best.us) best = p;
+                for (int given = 0; given < (mt == 1 ? 1 : 2); ++given) {
+                    const double alone = kAlone[i8][given][n][m], paired = kPaired[i8][given][n][m];
+                    const double rounds = wgs > 4 * kCUs ? 0.97 * static_cast<double>(wgs) / (2 * kCUs) * paired
+                                                         : static_cast<double>(wgs / (2 * kCUs)) * paired + (rest > kCUs ? paired : rest ? alone : 0.0);
+                    p.sums = given == 0;
+                    p.us = 2.8 + 0.2 * mt * nb + std::max(groups * rounds, weights / (wgs > kCUs ? 5.6e6 : 4.2e6)) +
+                           (given ? 2.6 + read / 4e6 : 0.0) + (p.split ? 2.5 + parts / 6e6 : 0.0);
+                    if (p.us < best.us) best = p;
+                }
             }
         }
     return best;
@@ -795,7 +807,9 @@ template <typename X, int NB, bool SUMS>
 int launch_tokens(int mt, TileBatch& tb, hipStream_t s) {
     if (mt == 1) return launch_tiles<X, 1, NB, true>(tb, s);
     if (mt == 2) return launch_tiles<X, 2, NB, SUMS>(tb, s);
+    if (mt == 3) return launch_tiles<X, 3, NB, SUMS>(tb, s);
     if (mt == 4) return launch_tiles<X, 4, NB, SUMS>(tb, s);
+    if (mt == 5) return launch_tiles<X, 5, NB, SUMS>(tb, s);
     if constexpr (Kind<X>::kI8)
         if (mt == 8) return launch_tiles<X, 8, NB, SUMS>(tb, s);
     return launch_tiles<X, 6, NB, SUMS>(tb, s);
