@@ -701,17 +701,18 @@ struct Plan {
 // Times of a group of columns in us where memory does not hold it up, [i8][sums made
 // here, given][nb 2, 4][mt 1, 2, 3, 4, 5, 6, 8]: a CU with one workgroup (the slope over K of
 // calls with 128 workgroups), and with two (of calls whose token tiles share weights).
+// 0: not a variant, as other tiles or sums were faster on all or nearly all shapes.
 constexpr int kTileTokens[] = {1, 2, 3, 4, 5, 6, 8};
 constexpr float kAlone[2][2][2][7] = {
     {{{0.43f, 0.54f, 0.67f, 0.77f, 0.90f, 1.01f, 0}, {0.62f, 0.77f, 0.97f, 1.18f, 1.39f, 1.60f, 0}},
-     {{0, 0.56f, 0.66f, 0.75f, 0.87f, 0.93f, 0}, {0, 0.75f, 0.92f, 1.06f, 1.37f, 1.44f, 0}}},
-    {{{0.37f, 0.46f, 0.54f, 0.57f, 0.69f, 0.73f, 0.83f}, {0.55f, 0.65f, 0.73f, 0.87f, 1.00f, 1.12f, 1.40f}},
-     {{0, 0.48f, 0.55f, 0.60f, 0.68f, 0.75f, 0.88f}, {0, 0.64f, 0.72f, 0.82f, 0.94f, 1.06f, 1.28f}}}};
+     {{0, 0, 0.66f, 0.75f, 0.87f, 0, 0}, {0, 0, 0.92f, 1.06f, 1.37f, 1.44f, 0}}},
+    {{{0.37f, 0.46f, 0.54f, 0.57f, 0.69f, 0.73f, 0}, {0.55f, 0.65f, 0.73f, 0.87f, 1.00f, 1.12f, 0}},
+     {{0, 0, 0, 0.60f, 0.68f, 0.75f, 0}, {0, 0, 0, 0.82f, 0.94f, 1.06f, 1.28f}}}};
 constexpr float kPaired[2][2][2][7] = {
     {{{0.60f, 0.85f, 1.05f, 1.28f, 1.50f, 1.80f, 0}, {1.10f, 1.40f, 1.70f, 2.10f, 2.60f, 3.05f, 0}},
-     {{0, 0.75f, 0.92f, 1.05f, 1.25f, 1.60f, 0}, {0, 1.25f, 1.50f, 1.92f, 2.40f, 2.65f, 0}}},
-    {{{0.50f, 0.55f, 0.62f, 0.75f, 0.85f, 1.05f, 1.50f}, {0.80f, 0.90f, 1.02f, 1.25f, 1.55f, 1.85f, 2.52f}},
-     {{0, 0.54f, 0.60f, 0.70f, 0.80f, 0.95f, 1.45f}, {0, 0.88f, 1.00f, 1.20f, 1.50f, 1.80f, 2.36f}}}};
+     {{0, 0, 0.92f, 1.05f, 1.25f, 0, 0}, {0, 0, 1.50f, 1.92f, 2.40f, 2.65f, 0}}},
+    {{{0.50f, 0.55f, 0.62f, 0.75f, 0.85f, 1.05f, 0}, {0.80f, 0.90f, 1.02f, 1.25f, 1.55f, 1.85f, 0}},
+     {{0, 0, 0, 0.70f, 0.80f, 0.95f, 0}, {0, 0, 0, 1.20f, 1.50f, 1.80f, 2.36f}}}};
 
 // The plan with the least expected time: what the workgroups take, two to a CU, or
 // the weights' read (4.2 TB/s with one to a CU, 5.6 with two); 3 to 9 us to start and
@@ -748,8 +749,9 @@ Plan plan_of(const FourbitProblem* probs, int count, int64_t M, bool i8) {
                 }
                 // up to two rounds are rounds; of more, workgroups begin as others end
                 const int64_t rest = wgs % (2 * kCUs);
-                for (int given = 0; given < (mt == 1 ? 1 : 2); ++given) {
+                for (int given = 0; given < 2; ++given) {
                     const double alone = kAlone[i8][given][n][m], paired = kPaired[i8][given][n][m];
+                    if (alone == 0) continue;
                     const double rounds = wgs > 4 * kCUs ? 0.97 * static_cast<double>(wgs) / (2 * kCUs) * paired
                                                          : static_cast<double>(wgs / (2 * kCUs)) * paired + (rest > kCUs ? paired : rest ? alone : 0.0);
                     p.sums = given == 0;
@@ -803,16 +805,14 @@ int launch_tiles(TileBatch& tb, hipStream_t s) {
     return hipGetLastError() == hipSuccess ? UNISVQ_OK : UNISVQ_EHIP;
 }
 
-template <typename X, int NB, bool SUMS>
+template <typename X, int NB, bool SUMS, int I = 0>
 int launch_tokens(int mt, TileBatch& tb, hipStream_t s) {
-    if (mt == 1) return launch_tiles<X, 1, NB, true>(tb, s);
-    if (mt == 2) return launch_tiles<X, 2, NB, SUMS>(tb, s);
-    if (mt == 3) return launch_tiles<X, 3, NB, SUMS>(tb, s);
-    if (mt == 4) return launch_tiles<X, 4, NB, SUMS>(tb, s);
-    if (mt == 5) return launch_tiles<X, 5, NB, SUMS>(tb, s);
-    if constexpr (Kind<X>::kI8)
-        if (mt == 8) return launch_tiles<X, 8, NB, SUMS>(tb, s);
-    return launch_tiles<X, 6, NB, SUMS>(tb, s);
+    if constexpr (I < 7) {
+        if constexpr (kAlone[Kind<X>::kI8][!SUMS][NB / 2 - 1][I] > 0)
+            if (mt == kTileTokens[I]) return launch_tiles<X, kTileTokens[I], NB, SUMS>(tb, s);
+        return launch_tokens<X, NB, SUMS, I + 1>(mt, tb, s);
+    }
+    return UNISVQ_EUNSUP;
 }
 
 template <typename X>
