@@ -1,6 +1,7 @@
 // C entry points of the norm, the gated activation and the 4-bit products:
 // argument validation (host only, before any HIP call) and dispatch.
 #include <cmath>
+#include <limits>
 
 #include "layer.hpp"
 
@@ -15,13 +16,20 @@ constexpr int64_t kMostColumns = int64_t{1} << 20;
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 int status(hipError_t e) { return e == hipSuccess ? UNISVQ_OK : UNISVQ_EHIP; }
 bool half_type(int t) { return t == UNISVQ_F16 || t == UNISVQ_BF16; }
-bool row_aligned(const void* p, int64_t stride) { return aligned(p, 16) && stride % 8 == 0; }
+// (a single row's stride says nothing)
+bool row_aligned(const void* p, int64_t stride, int64_t tokens) { return aligned(p, 16) && (tokens <= 1 || stride % 8 == 0); }
+
+// Rows of an output lie apart, and where an input lies there they are its rows.
+bool rows_apart(int64_t stride, int64_t n, int64_t tokens) { return tokens <= 1 || stride >= n || stride <= -n; }
+bool in_place_ok(const void* out, int out_type, int64_t out_stride, const void* in, int type, int64_t stride, int64_t tokens) {
+    return out != in || (out_type == type && (tokens <= 1 || out_stride == stride));
+}
 
 // Rows of outputs: as x, fp32, or bytes with a scale a row.
-int check_output(const void* y, int64_t stride, int y_dtype, int x_dtype, const float* scales) {
+int check_output(const void* y, int64_t stride, int64_t tokens, int y_dtype, int x_dtype, const float* scales) {
     if (y_dtype != x_dtype && y_dtype != UNISVQ_F32 && y_dtype != UNISVQ_I8)
         return half_type(y_dtype) ? UNISVQ_EUNSUP : UNISVQ_EINVAL;
-    if (!row_aligned(y, stride) || !aligned(scales, 4)) return UNISVQ_EALIGN;
+    if (!row_aligned(y, stride, tokens) || !aligned(scales, 4)) return UNISVQ_EALIGN;
     return UNISVQ_OK;
 }
 
@@ -56,19 +64,25 @@ int unisvq_rmsnorm(int64_t tokens, int64_t n, const void* x, int64_t x_stride, i
                    void* residual_out, int64_t residual_out_stride, int residual_dtype, void* y, int64_t y_stride,
                    int y_dtype, float* y_scales, void* stream) {
     if (tokens < 0 || tokens > kMost || n < 1 || !half_type(x_dtype)) return UNISVQ_EINVAL;
-    if (!(eps > 0) || !std::isfinite(eps) || !std::isfinite(weight_offset)) return UNISVQ_EINVAL;
+    if (!(eps >= std::numeric_limits<float>::min()) || !std::isfinite(eps) || !std::isfinite(weight_offset)) return UNISVQ_EINVAL;
     if ((residual == nullptr) != (residual_out == nullptr)) return UNISVQ_EINVAL;
     if (tokens > 0 && (!x || !weight || !y || (y_dtype == UNISVQ_I8 && !y_scales))) return UNISVQ_EINVAL;
     if (weight_dtype != x_dtype && weight_dtype != UNISVQ_F32) return half_type(weight_dtype) ? UNISVQ_EUNSUP : UNISVQ_EINVAL;
     if (residual && residual_dtype != x_dtype && residual_dtype != UNISVQ_F32)
         return half_type(residual_dtype) ? UNISVQ_EUNSUP : UNISVQ_EINVAL;
-    const int st = check_output(y, y_stride, y_dtype, x_dtype, y_scales);
+    const int st = check_output(y, y_stride, tokens, y_dtype, x_dtype, y_scales);
     if (st != UNISVQ_OK) return st;
-    if (!row_aligned(x, x_stride) || !aligned(weight, 16) || !row_aligned(residual, residual ? residual_stride : 0) ||
-        !row_aligned(residual_out, residual ? residual_out_stride : 0))
+    if (!row_aligned(x, x_stride, tokens) || !aligned(weight, 16) || !row_aligned(residual, residual ? residual_stride : 0, tokens) ||
+        !row_aligned(residual_out, residual ? residual_out_stride : 0, tokens))
         return UNISVQ_EALIGN;
     if (n % 8 != 0 || n > unisvq::kMaxRow) return UNISVQ_EUNSUP;
     if (tokens == 0) return UNISVQ_OK;
+    if (!rows_apart(y_stride, n, tokens) || !in_place_ok(y, y_dtype, y_stride, x, x_dtype, x_stride, tokens)) return UNISVQ_EINVAL;
+    if (residual && (y == residual_out || !rows_apart(residual_out_stride, n, tokens) ||
+                     !in_place_ok(y, y_dtype, y_stride, residual, residual_dtype, residual_stride, tokens) ||
+                     !in_place_ok(residual_out, residual_dtype, residual_out_stride, residual, residual_dtype, residual_stride, tokens) ||
+                     !in_place_ok(residual_out, residual_dtype, residual_out_stride, x, x_dtype, x_stride, tokens)))
+        return UNISVQ_EINVAL;
     return status(unisvq::launch_rmsnorm(
         unisvq::NormArgs{tokens, static_cast<int>(n), x, weight, residual, residual_out, y, x_stride, residual_stride,
                          residual_out_stride, y_stride, x_dtype, weight_dtype, residual_dtype, y_dtype, weight_offset,
@@ -81,12 +95,15 @@ int unisvq_gated(int64_t tokens, int64_t n, const void* gate, int64_t gate_strid
     if (tokens < 0 || tokens > kMost || n < 1 || !half_type(x_dtype)) return UNISVQ_EINVAL;
     if (activation != UNISVQ_SILU && activation != UNISVQ_GELU) return UNISVQ_EINVAL;
     if (tokens > 0 && (!gate || !up || !y || (y_dtype == UNISVQ_I8 && !y_scales))) return UNISVQ_EINVAL;
-    const int st = check_output(y, y_stride, y_dtype, x_dtype, y_scales);
+    const int st = check_output(y, y_stride, tokens, y_dtype, x_dtype, y_scales);
     if (st != UNISVQ_OK) return st;
-    if (!row_aligned(gate, gate_stride) || !row_aligned(up, up_stride)) return UNISVQ_EALIGN;
+    if (!row_aligned(gate, gate_stride, tokens) || !row_aligned(up, up_stride, tokens)) return UNISVQ_EALIGN;
     if (n % 8 != 0 || (y_dtype == UNISVQ_I8 ? n > unisvq::kMaxRow : n > kMost || tokens * (n / 8) > kMost))
         return UNISVQ_EUNSUP;
     if (tokens == 0) return UNISVQ_OK;
+    if (!rows_apart(y_stride, n, tokens) || !in_place_ok(y, y_dtype, y_stride, gate, x_dtype, gate_stride, tokens) ||
+        !in_place_ok(y, y_dtype, y_stride, up, x_dtype, up_stride, tokens))
+        return UNISVQ_EINVAL;
     return status(unisvq::launch_gated(unisvq::GatedArgs{tokens, static_cast<int>(n), gate, up, y, gate_stride, up_stride,
                                                          y_stride, x_dtype, y_dtype, activation, y_scales},
                                        static_cast<hipStream_t>(stream)));

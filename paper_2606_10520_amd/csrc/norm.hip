@@ -88,12 +88,13 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void norm_kernel(NormArgs a, int
                 if (there && lane + v * lanes < runs)
                     store_row8<T>(a.y, t * a.y_stride + at[v], h[v], a.y_dtype == UNISVQ_F32);
         } else {
-            // (runs past the end are copies of the row's last: they change no maximum)
+            // (runs past the end are left out: where the stream is written in place another
+            // wave may have stored its last run before they read it)
             uint32_t most = 0;
 #pragma unroll
             for (int v = 0; v < V; ++v)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) most = max(most, magnitude(h[v][i]));
+                for (int i = 0; i < 8; ++i) most = max(most, lane + v * lanes < runs ? magnitude(h[v][i]) : 0u);
             const auto larger = [](uint32_t p, uint32_t q) { return max(p, q); };
             if constexpr (WIDE)
                 most = over_block(most, tops, larger);

@@ -109,6 +109,34 @@ def test_norm_in_place(u, stream, n):
         assert torch.equal(a, h) and torch.equal(b, y)
 
 
+@pytest.mark.parametrize("stream", ["f16", "f32"])
+@pytest.mark.parametrize("n", [72, 520, 4160, 8200, 8704, 9224, 12808, 16376, 16392, 20488])
+def test_norm_in_place_in_eight_bits(u, stream, n):
+    """The stream written where it was read, by other waves than those that read its last run again."""
+    x, r = rows(300, n, torch.float16, 3), rows(300, n, T[stream], 4)
+    r[:, -8:] += 50.0  # (the sum with x twice would be the row's largest)
+    x[:, -8:] += 50.0
+    w = rows(1, n, torch.float16, 5)[0].abs().contiguous()
+    (codes, scales), h = u.rmsnorm(x, w, residual=r, out_dtype=torch.int8)
+    want = held(u.rmsnorm(x, w, residual=r, out_dtype=torch.float32)[0])
+    assert torch.equal(codes, want[0]) and torch.equal(scales, want[1])
+    for place in ("stream", "x") if stream == "f16" else ("stream",):
+        a, b = x.clone(), r.clone()
+        to = b if place == "stream" else a
+        (c, s), k = u.rmsnorm(a, w, residual=b, residual_out=to, out_dtype=torch.int8)
+        assert k is to and torch.equal(k, h) and torch.equal(c, codes) and torch.equal(s, scales)
+
+
+def test_a_single_row_has_any_stride(u):
+    x, r = (rows(4096, 1, torch.float16, i).contiguous().t() for i in (1, 2))
+    assert x.shape == (1, 4096) and x.stride() == (1, 1)
+    w = torch.ones(4096, dtype=torch.float16, device="cuda")
+    y, h = u.rmsnorm(x, w, residual=r, residual_out=r.clone())
+    want, k = u.rmsnorm(x.contiguous().view(4096).view(1, 4096), w, residual=r.reshape(4096).view(1, 4096))
+    assert torch.equal(y, want) and torch.equal(h, k)
+    assert torch.equal(u.gated(x, r), u.gated(x.reshape(4096).view(1, 4096), r.reshape(4096).view(1, 4096)))
+
+
 def test_norm_rows_of_views_leave_the_rest(u):
     """Rows of a wider tensor, in and out; what lies between them stays."""
     big = rows(20, 640, torch.float16, 1)

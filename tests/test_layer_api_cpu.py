@@ -54,6 +54,23 @@ def test_gated_refusals(args, want):
     assert gated(**args) == want
 
 
+@built
+@pytest.mark.parametrize("args", [
+    dict(), dict(r=None, h=None, ys=512), dict(r=None, h=None, yt=u.F32), dict(r=None, h=None, yt=u.I8), dict(y=2 * GOOD, hs=512),
+    dict(y=2 * GOOD, rt=u.F32), dict(h=2 * GOOD, rt=u.F32), dict(h=2 * GOOD, rs=512), dict(y=2 * GOOD, ys=128),
+    dict(y=2 * GOOD, ys=0), dict(y=2 * GOOD, ys=-248), dict(y=2 * GOOD, x=3 * GOOD, r=4 * GOOD, hs=0), dict(eps=1e-39)])
+def test_norm_refuses_outputs_that_overlap(args):
+    """Outputs on one another's or their own other rows, or on an input that is not the same rows of the same type; and an
+    eps below the normal numbers."""
+    assert norm(**args) == EINVAL
+
+
+@built
+@pytest.mark.parametrize("args", [dict(yt=u.F32), dict(yt=u.I8), dict(ys=512), dict(g=2 * GOOD, vs=512), dict(y=2 * GOOD, ys=248)])
+def test_gated_refuses_outputs_that_overlap(args):
+    assert gated(**args) == EINVAL
+
+
 def gemm(N=256, K=256, p=GOOD, M=4, x=GOOD, xt=u.F16, xs=None, y=GOOD, yt=u.F16, ws=GOOD, size=1 << 40):
     return u.load().unisvq_fourbit_gemm(N, K, p, M, x, xt, xs, y, yt, ws, size, None)
 
