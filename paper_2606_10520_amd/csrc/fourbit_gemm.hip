@@ -792,25 +792,17 @@ Places places_of(const FourbitProblem* probs, int count, int64_t M, const Plan& 
 }
 
 template <typename X, int MT, int NB, bool SUMS>
-int launch_tiles(TileBatch& tb, hipStream_t s) {
-    typedef Tiled<X, MT, NB, SUMS> C;
-    int64_t wgs = 0;
-    tb.m_tiles = static_cast<int>((tb.M + C::BM - 1) / C::BM);
-    for (int i = 0; i < tb.count; ++i) {
-        tb.p[i].wg_begin = static_cast<int>(wgs);
-        wgs += (tb.p[i].N + C::BN - 1) / C::BN * tb.m_tiles * tb.p[i].splits;
-        if (wgs > (int64_t{1} << 32) / C::kThreads - 1) return UNISVQ_EUNSUP;
-    }
-    tiled_kernel<X, MT, NB, SUMS><<<static_cast<uint32_t>(wgs), C::kThreads, 0, s>>>(tb);
+int launch_tiles(const TileBatch& tb, uint32_t wgs, hipStream_t s) {
+    tiled_kernel<X, MT, NB, SUMS><<<wgs, Tiled<X, MT, NB, SUMS>::kThreads, 0, s>>>(tb);
     return hipGetLastError() == hipSuccess ? UNISVQ_OK : UNISVQ_EHIP;
 }
 
 template <typename X, int NB, bool SUMS, int I = 0>
-int launch_tokens(int mt, TileBatch& tb, hipStream_t s) {
+int launch_tokens(int mt, const TileBatch& tb, uint32_t wgs, hipStream_t s) {
     if constexpr (I < 7) {
         if constexpr (kAlone[Kind<X>::kI8][!SUMS][NB / 2 - 1][I] > 0)
-            if (mt == kTileTokens[I]) return launch_tiles<X, kTileTokens[I], NB, SUMS>(tb, s);
-        return launch_tokens<X, NB, SUMS, I + 1>(mt, tb, s);
+            if (mt == kTileTokens[I]) return launch_tiles<X, kTileTokens[I], NB, SUMS>(tb, wgs, s);
+        return launch_tokens<X, NB, SUMS, I + 1>(mt, tb, wgs, s);
     }
     return UNISVQ_EUNSUP;
 }
@@ -823,22 +815,29 @@ int launch_tiled(const FourbitProblem* probs, int count, int64_t M, int y_dtype,
     if (at.bytes && (reinterpret_cast<uintptr_t>(workspace) & 15) != 0) return UNISVQ_EALIGN;
     TileBatch tb{};
     tb.count = count, tb.y_dtype = y_dtype, tb.M = M;
+    const int64_t BM = 16 * plan.mt, BN = 64 * plan.nb, m_tiles = (M + BM - 1) / BM;
+    int64_t wgs = 0;
     for (int i = 0; i < count; ++i) {
-        const int groups = static_cast<int>(probs[i].K / kGroup);
         tb.p[i] = TileProb{probs[i].packed, probs[i].x, workspace + at.bias[i], probs[i].x_scales, probs[i].y,
                            plan.splits[i] > 1 ? reinterpret_cast<float*>(workspace + at.partial[i]) : nullptr, probs[i].N,
-                           static_cast<int>(probs[i].K), plan.splits[i], 0};
+                           static_cast<int>(probs[i].K), plan.splits[i], static_cast<int>(wgs)};
+        wgs += (probs[i].N + BN - 1) / BN * m_tiles * plan.splits[i];
+        if (wgs >= int64_t{1} << 24) return UNISVQ_EUNSUP;  // (a grid has below 2^32 threads)
+    }
+    tb.m_tiles = static_cast<int>(m_tiles);
+    for (int i = 0; i < count; ++i)
         if (at.first[i] && !plan.sums) {
+            const int groups = static_cast<int>(probs[i].K / kGroup);
             const Sums a{probs[i].x, workspace + at.bias[i], M, groups};
             sums_kernel<X><<<static_cast<uint32_t>(std::min<int64_t>((M * groups + 15) / 16, 1 << 20)), 256, 0, s>>>(a);
         }
-    }
-    const int st = plan.nb == 2 ? (plan.sums ? launch_tokens<X, 2, true>(plan.mt, tb, s) : launch_tokens<X, 2, false>(plan.mt, tb, s))
-                                : (plan.sums ? launch_tokens<X, 4, true>(plan.mt, tb, s) : launch_tokens<X, 4, false>(plan.mt, tb, s));
+    const uint32_t grid = static_cast<uint32_t>(wgs);
+    const int st = plan.nb == 2 ? (plan.sums ? launch_tokens<X, 2, true>(plan.mt, tb, grid, s) : launch_tokens<X, 2, false>(plan.mt, tb, grid, s))
+                                : (plan.sums ? launch_tokens<X, 4, true>(plan.mt, tb, grid, s) : launch_tokens<X, 4, false>(plan.mt, tb, grid, s));
     if (st != UNISVQ_OK || !plan.split) return st;
     JoinBatch jb{};
     jb.y_dtype = y_dtype, jb.i8 = Kind<X>::kI8, jb.M = M;
-    int64_t wgs = 0;
+    wgs = 0;
     for (int i = 0; i < count; ++i)
         if (plan.splits[i] > 1) {
             jb.p[jb.count] = tb.p[i];

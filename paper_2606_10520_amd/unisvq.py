@@ -233,6 +233,7 @@ def _check(fn: str, status: int) -> None:
         raise UniSVQError(fn, status)
 
 
+@functools.lru_cache(maxsize=None)
 def _torch():
     import torch
     return torch
