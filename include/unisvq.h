@@ -759,7 +759,8 @@ int unisvq_attn_prompt(int64_t sequences, int64_t q_tokens, int64_t k_tokens, co
  * Rows of activations are given as (pointer, row stride in elements): element
  * i of row t is at t * stride + i.  Such pointers are 16-byte aligned and their
  * strides multiples of 8 elements, row lengths n multiples of 8 (UNISVQ_EALIGN,
- * UNISVQ_EUNSUP otherwise).
+ * UNISVQ_EUNSUP otherwise); the stride of a single row is not looked at.  Rows of
+ * an output do not overlap (UNISVQ_EINVAL), those of an input may.
  * An output of type UNISVQ_I8 is bytes with one fp32 scale a row (scales[t], row
  * t): value = code * scale, scale = a / 127 with a the row's largest magnitude
  * in fp32, code = round-to-even(v * (1 / scale)).  a < 1e-30: scale 0 and codes
@@ -775,12 +776,12 @@ int unisvq_attn_prompt(int64_t sequences, int64_t q_tokens, int64_t k_tokens, co
  *   x             device [tokens][n], F16 or BF16
  *   weight        device [n], contiguous, x_dtype or F32, 16-byte aligned
  *   weight_offset 0, or 1 for weights that are kept as differences from one
- *   eps           above 0
+ *   eps           a normal fp32 number above 0
  *   residual      the stream, device [tokens][n], x_dtype or F32, or NULL;
  *   residual_out  the stream after the addition, same type: NULL exactly where
  *                 residual is.  May be residual, or x where the types are the
- *                 same, each with the same stride, and may not overlap an input
- *                 otherwise
+ *                 same, each with the same stride (UNISVQ_EINVAL otherwise), and
+ *                 may not overlap an input in any other way
  *   y             device [tokens][n], x_dtype, F32 or I8; may be x or residual
  *                 on the same terms, and not residual_out
  *   y_scales      device fp32 [tokens] for I8, ignored otherwise
@@ -800,8 +801,10 @@ typedef enum {
  *   gate, up  device [tokens][n], F16 or BF16 (the two outputs of a gate and up
  *             product, or the halves of one fused row)
  *   y         device [tokens][n], x_dtype, F32 or I8; may be gate or up with the
- *             same type and stride, and may not overlap them otherwise
- *   y_scales  device fp32 [tokens] for I8, ignored otherwise */
+ *             same type and stride (UNISVQ_EINVAL otherwise), and may not overlap
+ *             them in any other way
+ *   y_scales  device fp32 [tokens] for I8, ignored otherwise
+ * act(gate) of magnitudes below 10^-36 may be taken as 0. */
 int unisvq_gated(int64_t tokens, int64_t n, const void* gate, int64_t gate_stride, const void* up, int64_t up_stride,
                  int x_dtype, int activation, void* y, int64_t y_stride, int y_dtype, float* y_scales, void* stream);
 
@@ -841,14 +844,18 @@ int unisvq_fourbit_quantize(int64_t N, int64_t K, const void* W, int w_dtype, vo
  *             x_scales device fp32 [M] (a token's value = code * scale, as
  *             unisvq_rmsnorm and unisvq_gated give them).  x_scales is NULL for
  *             the 16-bit types (UNISVQ_EINVAL otherwise, and for I8 without them)
- *   y         device [M][N] contiguous, F16, BF16 or F32, whatever x is
+ *   y         device [M][N] contiguous, F16, BF16 or F32, whatever x is; overlaps
+ *             neither x, packed nor another y
  *   workspace device, >= unisvq_fourbit_gemm_workspace_bytes(N, K, M, x_dtype) bytes,
  *             16-byte aligned (UNISVQ_EWORKSPACE / UNISVQ_EALIGN); may be NULL
  *             when that size is 0.  Overwritten
  * Codes are exact operands of the matrix cores; a group's sum is fp32 (I8: an
  * exact integer), multiplied by its scale in fp32; y is rounded once.  Sums are
- * added in an order that depends on shapes alone: results are reproducible bit
- * for bit.  A token with an Inf or NaN among its activations gets NaN. */
+ * added in an order that depends on the types and shapes of the call alone (of a
+ * batched one on all of its shapes): the same call gives the same bits.  A token
+ * with an Inf or NaN among its activations gets NaN, and so may one with bf16
+ * activations above 2^119, whose sums can pass fp32's range.  UNISVQ_EUNSUP for
+ * products of more than 2^24 workgroups (above 10^10 outputs). */
 size_t unisvq_fourbit_gemm_workspace_bytes(int64_t N, int64_t K, int64_t M, int x_dtype);
 int unisvq_fourbit_gemm(int64_t N, int64_t K, const void* packed, int64_t M, const void* x, int x_dtype,
                    const float* x_scales, void* y, int y_dtype, void* workspace, size_t workspace_bytes, void* stream);
@@ -863,9 +870,12 @@ typedef struct {
 } unisvq_fourbit_problem;
 
 /* Several independent products of the same M and types (a layer's q, k and v, or
- * gate and up) in one launch.  problems: HOST array of 1..UNISVQ_MAX_BATCH
- * descriptors, read before the call returns, all validated before anything is
- * enqueued. */
+ * gate and up) together: in one launch to 4 tokens where they fit the LDS, and to
+ * 16 where they have 4096 rows together and 8192 columns at most; else one launch
+ * for all, before it one for the sums of each x where many rows share them, and
+ * after it one that joins the parts of a K that was split.  problems: HOST array of
+ * 1..UNISVQ_MAX_BATCH descriptors, read before the call returns, all validated
+ * before anything is enqueued. */
 size_t unisvq_fourbit_gemm_batched_workspace_bytes(const unisvq_fourbit_problem* problems, int count, int64_t M, int x_dtype);
 int unisvq_fourbit_gemm_batched(const unisvq_fourbit_problem* problems, int count, int64_t M, int x_dtype, int y_dtype,
                            void* workspace, size_t workspace_bytes, void* stream);

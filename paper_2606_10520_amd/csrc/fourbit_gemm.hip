@@ -110,7 +110,8 @@ struct Kind<int8_t> {
 // lie in different banks) and -8 times its groups' sums, and passes over blocks of
 // sixteen rows with them, gridDim.x apart, DEEP tiles of codes on their way.  The
 // waves' sums of a block meet in LDS, one of the waves adds and stores them while
-// the others go on.
+// the others go on.  One token, 57344 rows of 8192: 44 us (5.4 TB/s); 4096 rows of
+// 4096: 5.2; four tokens, 22016 rows of 4096: 14.5.
 template <typename X, int TOK, int WAVES, int DEEP>
 __global__ __launch_bounds__(64 * WAVES) void few_kernel(const Batch b) {
     typedef Kind<X> Q;
@@ -345,7 +346,7 @@ int launch_some(Batch b, hipStream_t s) {
 // ---- many tokens ----
 // -8 times the sums of every token's groups, bias[token / 16][group][token % 16]
 // (fp32, or i8's integers), sixteen lanes a sum: what the tiled product's sums of
-// a group start from.
+// a group start from.  Bound by memory; 2048 tokens of 4096 bf16: 5 us.
 constexpr int kSumTile = 16;
 
 struct Sums {
@@ -422,6 +423,13 @@ __device__ __forceinline__ void load_lds(uint32_t to, const uint32_t (&off)[LOAD
 //
 // SUMS: the sums that a group starts from are made here, by one product more for
 // every NB; else they come from sums_kernel.
+//
+// 2048 tokens, 22016 rows of 4096: bf16 335 to 360 us (1.03 to 1.10 PFLOP/s; the matrix
+// cores are busy 51% of the cycles at the clock that the power leaves, and products
+// wait for their operands' conversion); 8 bits 215 to 225 us (1.7 POP/s): the two waves
+// of a SIMD issue in 98% of the cycles, five vector instructions a product, most of
+// them a sum's conversion and its product with the scale.  61 tokens, 10240 rows of
+// 8192: 21 us, of which a wave lives 14, a third of that waiting for loads.
 template <typename X, int MT, int NB, bool SUMS>
 struct Tiled {
     typedef Kind<X> Q;
@@ -430,7 +438,8 @@ struct Tiled {
     static constexpr int kRow = kGroup * Q::kBytes;  // bytes of a token's group
     // bytes of activations, of sums (whole loads: what is behind the tokens becomes
     // zeros), and of a wave's codes and scales
-    static constexpr int kX = (BM * kRow + 16 * kThreads - 1) / (16 * kThreads) * (16 * kThreads), kBias = SUMS ? 0 : 1024, kCodes = NB * 1024, kScales = 1024;
+    static constexpr int kX = (BM * kRow + 16 * kThreads - 1) / (16 * kThreads) * (16 * kThreads);
+    static constexpr int kBias = SUMS ? 0 : 1024, kCodes = NB * 1024, kScales = 1024;
     static constexpr int kShared = kX + kBias, kOwn = kCodes + kScales;
     // Groups in LDS; where there is no room for two of everything, codes and
     // scales are one deep: their next ones are asked for when they have been read.
@@ -752,8 +761,9 @@ Plan plan_of(const FourbitProblem* probs, int count, int64_t M, bool i8) {
                 for (int given = 0; given < 2; ++given) {
                     const double alone = kAlone[i8][given][n][m], paired = kPaired[i8][given][n][m];
                     if (alone == 0) continue;
+                    const double last = rest > kCUs ? paired : rest ? alone : 0.0;
                     const double rounds = wgs > 4 * kCUs ? 0.97 * static_cast<double>(wgs) / (2 * kCUs) * paired
-                                                         : static_cast<double>(wgs / (2 * kCUs)) * paired + (rest > kCUs ? paired : rest ? alone : 0.0);
+                                                         : static_cast<double>(wgs / (2 * kCUs)) * paired + last;
                     p.sums = given == 0;
                     p.us = 2.8 + 0.2 * mt * nb + std::max(groups * rounds, weights / (wgs > kCUs ? 5.6e6 : 4.2e6)) +
                            (given ? 2.6 + read / 4e6 : 0.0) + (p.split ? 2.5 + parts / 6e6 : 0.0);
@@ -832,8 +842,11 @@ int launch_tiled(const FourbitProblem* probs, int count, int64_t M, int y_dtype,
             sums_kernel<X><<<static_cast<uint32_t>(std::min<int64_t>((M * groups + 15) / 16, 1 << 20)), 256, 0, s>>>(a);
         }
     const uint32_t grid = static_cast<uint32_t>(wgs);
-    const int st = plan.nb == 2 ? (plan.sums ? launch_tokens<X, 2, true>(plan.mt, tb, grid, s) : launch_tokens<X, 2, false>(plan.mt, tb, grid, s))
-                                : (plan.sums ? launch_tokens<X, 4, true>(plan.mt, tb, grid, s) : launch_tokens<X, 4, false>(plan.mt, tb, grid, s));
+    int st;
+    if (plan.nb == 2)
+        st = plan.sums ? launch_tokens<X, 2, true>(plan.mt, tb, grid, s) : launch_tokens<X, 2, false>(plan.mt, tb, grid, s);
+    else
+        st = plan.sums ? launch_tokens<X, 4, true>(plan.mt, tb, grid, s) : launch_tokens<X, 4, false>(plan.mt, tb, grid, s);
     if (st != UNISVQ_OK || !plan.split) return st;
     JoinBatch jb{};
     jb.y_dtype = y_dtype, jb.i8 = Kind<X>::kI8, jb.M = M;
@@ -851,8 +864,8 @@ int launch_tiled(const FourbitProblem* probs, int count, int64_t M, int y_dtype,
 
 // Which kernel serves a batch: x in LDS for up to four tokens, where it fits; up to
 // sixteen tokens and 256 blocks of rows without a second launch (16 tokens, 4096 x
-// 4096: 7.6 us, tiles 9.1; 8192 x 8192 and twice 1024, 8 tokens of 8 bits: 16.4, tiles
-// 14.0); else tiles.
+// 4096: 7.6 us, tiles 9.1; more rows, 8192 x 8192 and twice 1024, 8 tokens of 8 bits:
+// 16.4, tiles 14.0); else tiles.
 enum Way { kFew, kSome, kTiled };
 
 Way way_of(const FourbitProblem* probs, int count, int64_t M, int size) {

@@ -1,5 +1,7 @@
 // 4-bit weights on gfx950: packing, its inverse, and rounding to the nearest
-// codes.  Set-up work: simple kernels, a word of eight codes a thread.
+// codes.  Set-up work, once for a model's weights: simple kernels, a word of eight
+// codes a thread.  8192 x 28672: pack 105 + 11 us, unpack 152, rounding from f16 225 to
+// 250 (2.5 TB/s; an exact division for each weight).
 #include <algorithm>
 
 #include "layer.hpp"

@@ -12,7 +12,10 @@ namespace {
 // Bound by memory: x, r, h and y pass once, so a row stays in registers from its
 // loads to its stores, V runs of eight a thread.  WIDE: a workgroup a row, else
 // 2^steps lanes of a wave.  Runs past the row's end read its last run again and
-// count as zeros, so that no load waits behind a branch.
+// count as zeros, so that no load waits behind a branch.  h, rounded to the stream's
+// type, is what a later layer reads, and so what is normalised; y is rounded once.
+// 4096 rows of 8192 bf16: 45 us (5.9 TB/s), with an fp32 stream 73 us (5.5 TB/s);
+// one row of 4096 2.4 us.
 template <typename T, int V, bool WIDE>
 __global__ __launch_bounds__(WIDE ? 1024 : 256) void norm_kernel(NormArgs a, int steps) {
     __shared__ float sums[16];
@@ -112,8 +115,10 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void norm_kernel(NormArgs a, int
 }
 
 // Rows too long for registers (1024 threads have 128 each): a thread's runs four at
-// a time, read again from the L2 for the result, and once more for 8 bits.  The
-// stream is read back from where it was stored, by the thread that stored it.
+// a time, read again from the L2 for the result, and once more for 8 bits (with four
+// and eight runs a thread the registers went to memory instead).  The stream is read
+// back from where it was stored, by the thread that stored it (or, past the row's end,
+// by one whose value is not used).
 template <typename T>
 __device__ __forceinline__ void load_four(const void* p, int64_t row, bool wide, const int (&at)[4], float (&f)[4][8]) {
     if (wide) {

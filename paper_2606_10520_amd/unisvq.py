@@ -1358,7 +1358,7 @@ def _fourbit_workspace(shapes, M: int, code: int) -> int:
 
 
 def fourbit_gemm_batched(problems, out_dtype=None, workspace=None, stream=None):
-    """Several products y = x W^T with 4-bit weights in one launch: problems is a sequence of (packed, N, K, x, out-or-None)
+    """Several products y = x W^T with 4-bit weights together: problems is a sequence of (packed, N, K, x, out-or-None)
     of the same token count and types.  x is [M][K] fp16 or bf16, or a pair (codes int8 [M][K], scales fp32 [M]) as
     rmsnorm and gated return them.  out_dtype: fp16, bf16 or fp32 (None: x's type, fp16 for a pair).  Returns the list of
     outputs [M][N]."""
