@@ -845,7 +845,7 @@ int unisvq_fourbit_quantize(int64_t N, int64_t K, const void* W, int w_dtype, vo
  *             unisvq_rmsnorm and unisvq_gated give them).  x_scales is NULL for
  *             the 16-bit types (UNISVQ_EINVAL otherwise, and for I8 without them)
  *   y         device [M][N] contiguous, F16, BF16 or F32, whatever x is; overlaps
- *             neither x, packed nor another y
+ *             no x, packed or other y of the call (UNISVQ_EINVAL where one starts there)
  *   workspace device, >= unisvq_fourbit_gemm_workspace_bytes(N, K, M, x_dtype) bytes,
  *             16-byte aligned (UNISVQ_EWORKSPACE / UNISVQ_EALIGN); may be NULL
  *             when that size is 0.  Overwritten

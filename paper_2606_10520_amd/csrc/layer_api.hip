@@ -159,6 +159,10 @@ int unisvq_fourbit_gemm_batched(const unisvq_fourbit_problem* problems, int coun
         const int st = check_fourbit(problems[i], M, x_dtype, y_dtype);
         if (st != UNISVQ_OK) return st;
     }
+    for (int i = 0; i < count; ++i)
+        for (int j = 0; j < count; ++j)
+            if (problems[i].y == problems[j].x || problems[i].y == problems[j].packed || (i != j && problems[i].y == problems[j].y))
+                return UNISVQ_EINVAL;
     FourbitProblem p[UNISVQ_MAX_BATCH];
     fourbit_batch(problems, count, p);
     return unisvq::launch_fourbit_batch(p, count, M, x_dtype, y_dtype, workspace, workspace_bytes,

@@ -71,7 +71,7 @@ def test_gated_refuses_outputs_that_overlap(args):
     assert gated(**args) == EINVAL
 
 
-def gemm(N=256, K=256, p=GOOD, M=4, x=GOOD, xt=u.F16, xs=None, y=GOOD, yt=u.F16, ws=GOOD, size=1 << 40):
+def gemm(N=256, K=256, p=GOOD, M=4, x=GOOD, xt=u.F16, xs=None, y=2 * GOOD, yt=u.F16, ws=GOOD, size=1 << 40):
     return u.load().unisvq_fourbit_gemm(N, K, p, M, x, xt, xs, y, yt, ws, size, None)
 
 
@@ -93,11 +93,19 @@ def test_fourbit_gemm_refusals(args, want):
 @pytest.mark.parametrize("args,want", BAD)
 def test_fourbit_batched_refusals(args, want):
     """The last of a batch is looked at as the first is."""
-    a = dict(N=256, K=256, p=GOOD, M=4, x=GOOD, xt=u.F16, xs=None, y=GOOD, yt=u.F16)
+    a = dict(N=256, K=256, p=GOOD, M=4, x=GOOD, xt=u.F16, xs=None, y=2 * GOOD, yt=u.F16)
     a.update(args)
     good_scales = GOOD if a["xt"] == u.I8 else None
-    arr = (u.FourbitProblem * 2)((256, 256, GOOD, GOOD, good_scales, GOOD), (a["N"], a["K"], a["p"], a["x"], a["xs"], a["y"]))
+    arr = (u.FourbitProblem * 2)((256, 256, GOOD, GOOD, good_scales, 3 * GOOD), (a["N"], a["K"], a["p"], a["x"], a["xs"], a["y"]))
     assert u.load().unisvq_fourbit_gemm_batched(arr, 2, a["M"], a["xt"], a["yt"], GOOD, 1 << 40, None) == want
+
+
+@built
+@pytest.mark.parametrize("ys", [(2 * GOOD, 2 * GOOD), (GOOD, 2 * GOOD), (2 * GOOD, 5 * GOOD), (7 * GOOD, 2 * GOOD)])
+def test_fourbit_outputs_that_overlap(ys):
+    """Two problems' outputs, or an output and some problem's activations or weights, in one place."""
+    arr = (u.FourbitProblem * 2)((256, 256, 4 * GOOD, GOOD, None, ys[0]), (256, 256, 5 * GOOD, 7 * GOOD, None, ys[1]))
+    assert u.load().unisvq_fourbit_gemm_batched(arr, 2, 4, u.F16, u.F16, GOOD, 1 << 40, None) == EINVAL
 
 
 @built
