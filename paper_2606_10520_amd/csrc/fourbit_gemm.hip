@@ -110,8 +110,9 @@ struct Kind<int8_t> {
 // lie in different banks) and -8 times its groups' sums, and passes over blocks of
 // sixteen rows with them, gridDim.x apart, DEEP tiles of codes on their way.  The
 // waves' sums of a block meet in LDS, one of the waves adds and stores them while
-// the others go on.  One token, 57344 rows of 8192: 44 us (5.4 TB/s); 4096 rows of
-// 4096: 5.2; four tokens, 22016 rows of 4096: 14.5.
+// the others go on.  One token, 57344 rows of 8192: 40.6 us (5.9 TB/s); 4096 rows of
+// 4096: 5.0; four tokens, 22016 rows of 4096: 13.2 (two sets of tiles on their way: 42.8,
+// 5.7, 15.3).
 template <typename X, int TOK, int WAVES, int DEEP>
 __global__ __launch_bounds__(64 * WAVES) void few_kernel(const Batch b) {
     typedef Kind<X> Q;
@@ -139,7 +140,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(const Batch b) {
     } ring[DEEP];
     // (a block's tiles are taken DEEP at a time; those past the share read nothing:
     // their scales are zeros)
-    const int padded = (share + DEEP - 1) / DEEP * DEEP;
+    const int padded = max((share + DEEP - 1) / DEEP * DEEP, DEEP);
     int rb = first, next = 0;  // of the next tile to ask for
     const auto ask = [&](Tile& t) {
         const uint32_t out = rb < blocks && next < share ? 0u : kOutOfRange;
@@ -182,24 +183,29 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(const Batch b) {
     }
     __builtin_amdgcn_wave_barrier();  // (a wave reads what it wrote itself)
 
-    for (int block = first, turnover = 0; block < blocks; block += wgs, ++turnover) {
-        f32x4 acc{};
-        for (int h0 = 0; h0 < padded; h0 += DEEP)
+    int block = first, turnover = 0, h0 = 0;
+    f32x4 acc{};
+    const auto pass = [&](Tile(&r)[DEEP]) {
 #pragma unroll
-            for (int i = 0; i < DEEP; ++i) {
-                const int h = min(h0 + i, share - 1);
-                typename Q::Operand w[Q::kSteps];
-                Q::decode(ring[i].q, w);
-                const float s = static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(ring[i].s)));
-                ask(ring[i]);
-                typename Q::Sum sum = *reinterpret_cast<const typename Q::Sum*>(mine + h * kGroupBytes + TOK * kRow + 16 * c);
+        for (int i = 0; i < DEEP; ++i) {
+            const int h = max(min(h0 + i, share - 1), 0);
+            typename Q::Operand w[Q::kSteps];
+            Q::decode(r[i].q, w);
+            const float s = static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(r[i].s)));
+            ask(r[i]);
+            typename Q::Sum sum = *reinterpret_cast<const typename Q::Sum*>(mine + h * kGroupBytes + TOK * kRow + 16 * c);
 #pragma unroll
-                for (int j = 0; j < Q::kSteps; ++j)
-                    sum = Q::mma(*reinterpret_cast<const typename Q::Operand*>(at[j] + h * kGroupBytes), w[j], sum);
+            for (int j = 0; j < Q::kSteps; ++j)
+                sum = Q::mma(*reinterpret_cast<const typename Q::Operand*>(at[j] + h * kGroupBytes), w[j], sum);
+            if (share > 0)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[e] = fmaf(s, static_cast<float>(sum[e]), acc[e]);
-            }
+        }
+        h0 += DEEP;
+        if (h0 < padded) return;
+        h0 = 0;
         parts[turnover & 1][wave][lane] = acc;
+        acc = f32x4{};
         __syncthreads();
         if (wave == turnover % WAVES && 4 * c < b.M) {
             f32x4 sum = parts[turnover & 1][0][lane];
@@ -212,7 +218,9 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(const Batch b) {
                     store_out(p.y, (4 * c + i) * p.N + block * kRowBlock + n, sum[i] * unit, b.y_dtype);
                 }
         }
-    }
+        block += wgs, ++turnover;
+    };
+    while (block < blocks) pass(ring);
 }
 
 // Bytes of LDS: two rounds of the waves' sums, x and its groups' sums.
@@ -220,19 +228,64 @@ int64_t few_lds_bytes(int64_t K, int tok, int waves, int size) {
     return 2 * waves * 1024 + K / kGroup * (tok * kGroup * size + 64);
 }
 
+// How few tokens' work is shared out: waves of a workgroup, tiles that a wave asks for
+// together, and blocks of rows that a workgroup passes over.
+struct FewPlan {
+    int waves, deep, passes;
+};
+
+// A wave's share of the groups is taken DEEP tiles at a time, the last ones empty where
+// DEEP does not divide it: as few empty ones as can be (40 groups, 22016 rows, one token:
+// five of eight waves 13.5 us, threes of sixteen 14.0, fours of sixteen 18.0; 20 groups,
+// threes 9.2, fours 10.3).  Eight waves, two workgroups to a CU, or sixteen: 16 bits, more
+// than 32 groups: sixteen are faster by 3 to 8% where both have as many empty tiles (48
+// groups, one token: 14.6 us for 15.0), 8 bits slower by 6 to 10% (48 groups, four
+// tokens: 19.6 for 17.7); few rows, one block a workgroup: sixteen, by 10% (28 groups, 4096
+// rows, 8 bits: 5.3 us for 5.8), and no more than three at a time (64 groups: twos 6.7,
+// fours 7.0).
+FewPlan few_plan(const Batch& b, int64_t K, int tok, int size) {
+    const int groups = static_cast<int>(K / kGroup);
+    FewPlan best{};
+    double least = 1e30;
+    for (const int waves : {8, 16}) {
+        const int64_t lds = few_lds_bytes(K, tok, waves, size);
+        if (lds > (waves == 8 ? kMostLds / 2 : kMostLds)) continue;
+        // as many workgroups as the GPU holds, every one with as many blocks as any
+        const int64_t places = kCUs * 16 / waves;
+        int64_t total = 0;
+        for (int i = 0; i < b.count; ++i) total += b.p[i].N / kRowBlock;
+        int64_t passes = (total + places - 1) / places;
+        for (int64_t wgs = places + 1; wgs > places; ++passes) {
+            wgs = 0;
+            for (int i = 0; i < b.count; ++i) wgs += (b.p[i].N / kRowBlock + passes - 1) / passes;
+            if (wgs <= places) break;
+        }
+        const bool few_rows = total <= kCUs;
+        double factor = 1.0;
+        if (few_rows)
+            factor = waves == 8 ? 1.25 : 1.0;
+        else if (size == 1)
+            factor = waves == 16 ? 1.1 : 1.0;
+        else if (groups > 32)
+            factor = waves == 8 ? 1.1 : 1.0;
+        const int share = (groups + waves - 1) / waves;
+        for (int deep = waves == 8 ? share > 1 ? 5 : 1 : few_rows ? 3 : 4; deep >= (share > 1 ? 2 : 1); --deep) {
+            if (deep == 1 && waves == 16) continue;
+            const double cost = (share + deep - 1) / deep * deep * waves * factor;
+            if (cost < least) least = cost, best = FewPlan{waves, deep, static_cast<int>(passes)};
+        }
+    }
+    return best;
+}
+
 template <typename X, int TOK, int WAVES, int DEEP>
-int launch_few(Batch b, int64_t K, hipStream_t s) {
+int launch_few(Batch b, int64_t K, int64_t passes, hipStream_t s) {
     const int lds = static_cast<int>(few_lds_bytes(K, TOK, WAVES, Kind<X>::kBytes));
     static std::atomic<uint64_t> done{0};
     if (lds > 65536) {
         const int st = ensure_lds_limit(reinterpret_cast<const void*>(few_kernel<X, TOK, WAVES, DEEP>), kMostLds, done);
         if (st != UNISVQ_OK) return st;
     }
-    // as many workgroups as the GPU holds, every one with as many blocks as any
-    const int64_t slots = kCUs * (WAVES == 8 && lds <= kMostLds / 2 ? 2 : 1);
-    int64_t total = 0;
-    for (int i = 0; i < b.count; ++i) total += b.p[i].N / kRowBlock;
-    const int64_t passes = (total + slots - 1) / slots;
     int64_t blocks = 0;
     for (int i = 0; i < b.count; ++i) {
         b.p[i].wg_begin = static_cast<int>(blocks);
@@ -243,19 +296,18 @@ int launch_few(Batch b, int64_t K, hipStream_t s) {
     return hipGetLastError() == hipSuccess ? UNISVQ_OK : UNISVQ_EHIP;
 }
 
-// Eight waves, and two workgroups on a CU, up to 32 groups, sixteen above: one
-// token, 57344 rows of 8192: 44.8 us with sixteen, 4096 rows of 11008: 9.0 (eight:
-// 10.2), 22016 rows of 4096: 13.0 (eight: 12.6).  A wave's share is taken in fours
-// of tiles where it is a multiple of four (8192 rows of 28672, shares of 14: 26.0 us
-// in twos, 30.2 in fours).
 template <typename X, int TOK>
 int launch_few(const Batch& b, int64_t K, hipStream_t s) {
-    const int64_t groups = K / kGroup;
-    if (groups <= 8) return launch_few<X, TOK, 8, 1>(b, K, s);
-    if (groups <= 16) return launch_few<X, TOK, 8, 2>(b, K, s);
-    if (groups <= 32) return launch_few<X, TOK, 8, 4>(b, K, s);
-    if ((groups + 15) / 16 % 4 == 0) return launch_few<X, TOK, 16, 4>(b, K, s);
-    return launch_few<X, TOK, 16, 2>(b, K, s);
+    const FewPlan p = few_plan(b, K, TOK, Kind<X>::kBytes);
+    if (p.waves == 16)
+        return p.deep == 2   ? launch_few<X, TOK, 16, 2>(b, K, p.passes, s)
+               : p.deep == 3 ? launch_few<X, TOK, 16, 3>(b, K, p.passes, s)
+                             : launch_few<X, TOK, 16, 4>(b, K, p.passes, s);
+    return p.deep == 1   ? launch_few<X, TOK, 8, 1>(b, K, p.passes, s)
+           : p.deep == 2 ? launch_few<X, TOK, 8, 2>(b, K, p.passes, s)
+           : p.deep == 3 ? launch_few<X, TOK, 8, 3>(b, K, p.passes, s)
+           : p.deep == 4 ? launch_few<X, TOK, 8, 4>(b, K, p.passes, s)
+                         : launch_few<X, TOK, 8, 5>(b, K, p.passes, s);
 }
 
 int tok_of(int64_t M) { return M == 1 ? 1 : M == 2 ? 2 : 4; }
@@ -871,7 +923,7 @@ enum Way { kFew, kSome, kTiled };
 Way way_of(const FourbitProblem* probs, int count, int64_t M, int size) {
     int64_t most = 0, blocks = 0;
     for (int i = 0; i < count; ++i) most = std::max(most, probs[i].K), blocks += probs[i].N / kRowBlock;
-    if (M <= 4 && blocks < (1 << 30) && few_lds_bytes(most, tok_of(M), most <= 4096 ? 8 : 16, size) <= kMostLds) return kFew;
+    if (M <= 4 && blocks < (1 << 30) && few_lds_bytes(most, tok_of(M), 16, size) <= kMostLds) return kFew;
     return M <= 16 && blocks <= kCUs && most <= 8192 ? kSome : kTiled;
 }
 

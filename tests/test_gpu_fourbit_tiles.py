@@ -1,5 +1,6 @@
 """Products at sizes between which every tile of tokens and rows is taken, with K whole and in parts, and with the
-activations' sums made in the kernel and in a launch of their own; row and token counts end inside a tile."""
+activations' sums made in the kernel and in a launch of their own; row and token counts end inside a tile.  Of few tokens:
+every number of waves and of tiles asked for together, shares of K that they divide and do not, waves without a share."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -29,3 +30,30 @@ def test_tiles(u, kind, N, K, M):
     y = u.fourbit_gemm(u.fourbit_pack(codes, scales), N, K, x, out=room[:M])
     assert (room[M] == 7).all()
     check(y, x, codes, scales)
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16", "i8"])
+@pytest.mark.parametrize("N", [48, 4112, 22032])
+@pytest.mark.parametrize("K", [128, 640, 1152, 2048, 2560, 3584, 4608, 5120, 5632, 7168, 9216, 11008, 13824, 15360, 20480, 32768, 49152])
+def test_few_tokens(u, kind, N, K):
+    codes, scales = weights(N, K, N + K)
+    packed = u.fourbit_pack(codes, scales)
+    for M in (1, 2, 3):
+        x = activations(M, K, kind, M)
+        room = torch.full((M + 1, N), 7.0, device="cuda")
+        y = u.fourbit_gemm(packed, N, K, x, out=room[:M])
+        assert (room[M] == 7).all()
+        check(y, x, codes, scales)
+
+
+@pytest.mark.parametrize("kind", ["f16", "i8"])
+@pytest.mark.parametrize("shapes", [[(4096, 4096)] * 3, [(16, 128), (4112, 5120), (22032, 640)], [(16, 2560)] * 8, [(8208, 1152), (48, 11008)]])
+def test_few_tokens_in_batches(u, kind, shapes):
+    """Batches whose problems share the workgroups out unevenly, or have fewer groups than there are waves."""
+    made = [weights(N, K, i) for i, (N, K) in enumerate(shapes)]
+    packed = [u.fourbit_pack(*m) for m in made]
+    for M in (1, 2, 4):
+        xs = {K: activations(M, K, kind, K) for _, K in shapes}
+        ys = u.fourbit_gemm_batched([(p, N, K, xs[K], None) for p, (N, K) in zip(packed, shapes)], out_dtype=torch.float32)
+        for y, (N, K), m in zip(ys, shapes, made):
+            check(y, xs[K], *m)
