@@ -310,9 +310,9 @@ int launch_few(const Batch& b, int64_t K, hipStream_t s) {
                          : launch_few<X, TOK, 8, 5>(b, K, p.passes, s);
 }
 
-int tok_of(int64_t M) { return M == 1 ? 1 : M == 2 ? 2 : 4; }
+int tok_of(int64_t M) { return M == 1 ? 1 : M == 2 ? 2 : M <= 4 ? 4 : 8; }
 
-// Up to sixteen tokens and few rows: a workgroup has a block of sixteen rows, its
+// Up to sixteen tokens and not many rows: a workgroup has a block of sixteen rows, its
 // waves share K out in runs of groups and read x from the L2, and their sums meet
 // in LDS; one launch, where tiles would have to be joined by a second.
 constexpr int kSomeWaves = 8;
@@ -914,17 +914,25 @@ int launch_tiled(const FourbitProblem* probs, int count, int64_t M, int y_dtype,
     return hipGetLastError() == hipSuccess ? UNISVQ_OK : UNISVQ_EHIP;
 }
 
-// Which kernel serves a batch: x in LDS for up to four tokens, where it fits; up to
-// sixteen tokens and 256 blocks of rows without a second launch (16 tokens, 4096 x
-// 4096: 7.6 us, tiles 9.1; more rows, 8192 x 8192 and twice 1024, 8 tokens of 8 bits:
-// 16.4, tiles 14.0); else tiles.
+// Which kernel serves a batch.
+// x in LDS: up to four tokens, where it fits; up to eight of 16 bits on 2048 to 4096
+// columns, of 4097 to 24576 rows (8 tokens, 8192 rows of 4096: 7.8 us, tiles 9.7; 22016
+// rows: 14.0, 16.4; 28672 rows of 2048: 10.8, 9.9; 22016 of 5120: 17.1, 16.5).
+// Else up to sixteen tokens without a second launch, x from the L2: 4096 rows of up to 8192
+// columns (16 tokens, 4096 x 4096: 7.6 us, tiles 9.1; 8 bits, 1024 rows of 12288: 10.1,
+// 9.1), and 8192 rows, two workgroups to a CU, of up to 1024 columns or 4096 of 8 bits (8192
+// rows, 8 tokens of 16 bits, 1024 columns: 5.1, 5.9; 2048, 16 tokens: 8.2, 7.7; 8 bits,
+// 4096 columns, 16 tokens: 8.9, 10.1; 6144: 11.5, 11.0).
+// Else tiles.
 enum Way { kFew, kSome, kTiled };
 
 Way way_of(const FourbitProblem* probs, int count, int64_t M, int size) {
     int64_t most = 0, blocks = 0;
     for (int i = 0; i < count; ++i) most = std::max(most, probs[i].K), blocks += probs[i].N / kRowBlock;
-    if (M <= 4 && blocks < (1 << 30) && few_lds_bytes(most, tok_of(M), 16, size) <= kMostLds) return kFew;
-    return M <= 16 && blocks <= kCUs && most <= 8192 ? kSome : kTiled;
+    const bool eight = M <= 8 && size == 2 && blocks > kCUs && blocks <= 6 * kCUs && most >= 2048 && most <= 4096;
+    if ((M <= 4 || eight) && blocks < (1 << 30) && few_lds_bytes(most, tok_of(M), 16, size) <= kMostLds) return kFew;
+    if (M > 16 || blocks > 2 * kCUs) return kTiled;
+    return most <= (blocks <= kCUs ? 8192 : size == 1 ? 4096 : 1024) ? kSome : kTiled;
 }
 
 template <typename X>
@@ -940,6 +948,8 @@ int launch_kind(const FourbitProblem* probs, int count, int64_t M, int y_dtype, 
     }
     if (way == kSome) return launch_some<X>(b, s);
     const int tok = tok_of(M);
+    if constexpr (!Kind<X>::kI8)
+        if (tok == 8) return launch_few<X, 8>(b, most, s);
     return tok == 1 ? launch_few<X, 1>(b, most, s) : tok == 2 ? launch_few<X, 2>(b, most, s) : launch_few<X, 4>(b, most, s);
 }
 

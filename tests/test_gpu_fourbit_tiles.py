@@ -57,3 +57,18 @@ def test_few_tokens_in_batches(u, kind, shapes):
         ys = u.fourbit_gemm_batched([(p, N, K, xs[K], None) for p, (N, K) in zip(packed, shapes)], out_dtype=torch.float32)
         for y, (N, K), m in zip(ys, shapes, made):
             check(y, xs[K], *m)
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16", "i8"])
+@pytest.mark.parametrize("N", [272, 4096, 4112, 8192, 8208, 22032])
+@pytest.mark.parametrize("K", [512, 1024, 1152, 2048, 2560, 4096, 4224, 8192, 8320, 16384, 16512])
+def test_five_to_sixteen_tokens(u, kind, N, K):
+    """Both sides of where one kernel takes over from another."""
+    codes, scales = weights(N, K, N + K)
+    packed = u.fourbit_pack(codes, scales)
+    for M in (5, 8, 9, 16):
+        x = activations(M, K, kind, M)
+        room = torch.full((M + 1, N), 7.0, device="cuda")
+        y = u.fourbit_gemm(packed, N, K, x, out=room[:M])
+        assert (room[M] == 7).all()
+        check(y, x, codes, scales)
