@@ -871,7 +871,7 @@ typedef struct {
 
 /* Several independent products of the same M and types (a layer's q, k and v, or
  * gate and up) together: in one launch to 4 tokens where they fit the LDS, and to
- * 16 where they have few rows or columns (4096 rows together of 8192 columns, for
+ * 16 where they have few rows or columns (4096 rows together of 4096 columns, for
  * instance); else one launch for all, before it one for the sums of each x where
  * many rows share them, and after it one that joins the parts of a K that was
  * split.  problems: HOST array of 1..UNISVQ_MAX_BATCH descriptors, read before the

@@ -315,7 +315,7 @@ int tok_of(int64_t M) { return M == 1 ? 1 : M == 2 ? 2 : M <= 4 ? 4 : 8; }
 // Up to sixteen tokens and not many rows: a workgroup has a block of sixteen rows, its
 // waves share K out in runs of groups and read x from the L2, and their sums meet
 // in LDS; one launch, where tiles would have to be joined by a second.
-constexpr int kSomeWaves = 8;
+constexpr int kSomeWaves = 8;  // (16 tokens, 4096 x 4096: 7.6 us, four waves 8.4, sixteen 8.2)
 
 template <typename X>
 __global__ __launch_bounds__(64 * kSomeWaves) void some_kernel(const Batch b) {
@@ -918,11 +918,12 @@ int launch_tiled(const FourbitProblem* probs, int count, int64_t M, int y_dtype,
 // x in LDS: up to four tokens, where it fits; up to eight of 16 bits on 2048 to 4096
 // columns, of 4097 to 24576 rows (8 tokens, 8192 rows of 4096: 7.8 us, tiles 9.7; 22016
 // rows: 14.0, 16.4; 28672 rows of 2048: 10.8, 9.9; 22016 of 5120: 17.1, 16.5).
-// Else up to sixteen tokens without a second launch, x from the L2: 4096 rows of up to 8192
-// columns (16 tokens, 4096 x 4096: 7.6 us, tiles 9.1; 8 bits, 1024 rows of 12288: 10.1,
-// 9.1), and 8192 rows, two workgroups to a CU, of up to 1024 columns or 4096 of 8 bits (8192
-// rows, 8 tokens of 16 bits, 1024 columns: 5.1, 5.9; 2048, 16 tokens: 8.2, 7.7; 8 bits,
-// 4096 columns, 16 tokens: 8.9, 10.1; 6144: 11.5, 11.0).
+// Else up to sixteen tokens without a second launch, every workgroup with x from the L2:
+// 4096 rows while x is at most 128 KB (16 bits, 1024 rows: 16 tokens of 4096 columns 7.2 us,
+// tiles 7.0, of 6144 9.7 and 7.6; 8 of 8192 8.7 and 8.2; 8 bits, 16 of 8192 7.9 and 8.3, of
+// 12288 10.1 and 9.1), and 8192 rows, two workgroups to a CU, while it is at most 32 KB, of
+// 8 bits 64 (16 tokens of 16 bits, 1024 columns 5.5 us, tiles 5.9, 2048 8.2 and 7.7; of 8
+// bits, 4096 8.9 and 10.1, 6144 11.5 and 11.0).
 // Else tiles.
 enum Way { kFew, kSome, kTiled };
 
@@ -932,7 +933,7 @@ Way way_of(const FourbitProblem* probs, int count, int64_t M, int size) {
     const bool eight = M <= 8 && size == 2 && blocks > kCUs && blocks <= 6 * kCUs && most >= 2048 && most <= 4096;
     if ((M <= 4 || eight) && blocks < (1 << 30) && few_lds_bytes(most, tok_of(M), 16, size) <= kMostLds) return kFew;
     if (M > 16 || blocks > 2 * kCUs) return kTiled;
-    return most <= (blocks <= kCUs ? 8192 : size == 1 ? 4096 : 1024) ? kSome : kTiled;
+    return M * most * size <= (blocks <= kCUs ? 131072 : size == 1 ? 65536 : 32768) ? kSome : kTiled;
 }
 
 template <typename X>

@@ -61,7 +61,7 @@ def test_few_tokens_in_batches(u, kind, shapes):
 
 @pytest.mark.parametrize("kind", ["f16", "bf16", "i8"])
 @pytest.mark.parametrize("N", [272, 4096, 4112, 8192, 8208, 22032])
-@pytest.mark.parametrize("K", [512, 1024, 1152, 2048, 2560, 4096, 4224, 8192, 8320, 16384, 16512])
+@pytest.mark.parametrize("K", [512, 1024, 1152, 2048, 2560, 4096, 4224, 5888, 8192, 8320, 14592, 16384, 16512])
 def test_five_to_sixteen_tokens(u, kind, N, K):
     """Both sides of where one kernel takes over from another."""
     codes, scales = weights(N, K, N + K)
