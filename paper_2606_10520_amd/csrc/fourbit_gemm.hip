@@ -108,11 +108,11 @@ struct Kind<int8_t> {
 // waves share K out in runs of groups; every wave keeps its part of x in LDS (TOK
 // tokens, 16-byte chunks turned by the token so that those that are read together
 // lie in different banks) and -8 times its groups' sums, and passes over blocks of
-// sixteen rows with them, gridDim.x apart, DEEP tiles of codes on their way.  The
-// waves' sums of a block meet in LDS, one of the waves adds and stores them while
-// the others go on.  One token, 57344 rows of 8192: 40.6 us (5.9 TB/s); 4096 rows of
-// 4096: 5.0; four tokens, 22016 rows of 4096: 13.2 (two sets of tiles on their way: 42.8,
-// 5.7, 15.3).
+// sixteen rows with them, as far apart as its problem has workgroups, DEEP tiles of
+// codes on their way.  The waves' sums of a block meet in LDS, one of the waves adds and
+// stores them while the others go on.  One token, 57344 rows of 8192: 40.6 us (5.9 TB/s);
+// 4096 rows of 4096: 5.0; four tokens, 22016 rows of 4096: 13.2 (two sets of tiles on
+// their way: 42.8, 5.7, 15.3).
 template <typename X, int TOK, int WAVES, int DEEP>
 __global__ __launch_bounds__(64 * WAVES) void few_kernel(const Batch b) {
     typedef Kind<X> Q;
