@@ -776,7 +776,7 @@ constexpr float kPaired[2][2][2][7] = {
      {{0, 0, 0, 0.70f, 0.80f, 0.95f, 0}, {0, 0, 0, 1.20f, 1.50f, 1.80f, 2.36f}}}};
 
 // The plan with the least expected time: what the workgroups take, two to a CU, or
-// the weights' read (4.2 TB/s with one to a CU, 5.6 with two); 3 to 9 us to start and
+// the weights' read (4.2 TB/s with one to a CU, 5.8 with two); 3 to 9 us to start and
 // end; a launch for the sums of activations, where they are given; parts of K and the
 // launch that joins them. Of 25 shapes from 16 to 4096 tokens the plan took 0 to 9% more
 // than the fastest of those considered.
@@ -810,6 +810,7 @@ Plan plan_of(const FourbitProblem* probs, int count, int64_t M, bool i8) {
                 }
                 // up to two rounds are rounds; of more, workgroups begin as others end
                 const int64_t rest = wgs % (2 * kCUs);
+                const double rate = wgs > 3 * kCUs / 2 ? 5.8e6 : wgs > kCUs ? 5.0e6 : 4.2e6;
                 for (int given = 0; given < 2; ++given) {
                     const double alone = kAlone[i8][given][n][m], paired = kPaired[i8][given][n][m];
                     if (alone == 0) continue;
@@ -817,7 +818,7 @@ Plan plan_of(const FourbitProblem* probs, int count, int64_t M, bool i8) {
                     const double rounds = wgs > 4 * kCUs ? 0.97 * static_cast<double>(wgs) / (2 * kCUs) * paired
                                                          : static_cast<double>(wgs / (2 * kCUs)) * paired + last;
                     p.sums = given == 0;
-                    p.us = 2.8 + 0.2 * mt * nb + std::max(groups * rounds, weights / (wgs > kCUs ? 5.6e6 : 4.2e6)) +
+                    p.us = 2.8 + 0.2 * mt * nb + std::max(groups * rounds, weights / rate) +
                            (given ? 2.6 + read / 4e6 : 0.0) + (p.split ? 2.5 + parts / 6e6 : 0.0);
                     if (p.us < best.us) best = p;
                 }

@@ -18,7 +18,7 @@ SIZES = [  # N, K, M
     (4112, 1152, 1300), (6032, 1152, 1300), (4112, 2048, 1500), (1040, 11008, 1500), (272, 28672, 2000),
     (28688, 384, 2000), (2064, 4096, 2000), (11024, 2048, 2000), (6032, 8192, 2000), (28688, 2048, 2000),
     (1040, 28672, 2300), (28688, 1152, 2300), (2064, 4096, 2600), (8208, 1152, 2600), (528, 8192, 3300),
-    (28688, 2048, 3300), (1040, 1152, 5000)]
+    (28688, 2048, 3300), (1040, 1152, 5000), (10848, 9472, 94), (10832, 25984, 106)]
 
 
 @pytest.mark.parametrize("kind", ["f16", "bf16", "i8"])
