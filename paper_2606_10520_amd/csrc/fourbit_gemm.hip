@@ -234,6 +234,13 @@ struct FewPlan {
     int waves, deep, passes;
 };
 
+// The variants there are.  (Eight tokens come with 16 to 32 groups of 16 bits alone, which
+// take these by the plan below.)
+constexpr bool few_variant(int tok, int waves, int deep) {
+    if (tok == 8) return waves == 16 ? deep == 2 : deep >= 2 && deep <= 4;
+    return waves == 16 ? deep >= 2 && deep <= 4 : deep >= 1 && deep <= 5;
+}
+
 // A wave's share of the groups is taken DEEP tiles at a time, the last ones empty where
 // DEEP does not divide it: as few empty ones as can be (40 groups, 22016 rows, one token:
 // five of eight waves 13.5 us, threes of sixteen 14.0, fours of sixteen 18.0; 20 groups,
@@ -270,7 +277,7 @@ FewPlan few_plan(const Batch& b, int64_t K, int tok, int size) {
             factor = waves == 8 ? 1.1 : 1.0;
         const int share = (groups + waves - 1) / waves;
         for (int deep = waves == 8 ? share > 1 ? 5 : 1 : few_rows ? 3 : 4; deep >= (share > 1 ? 2 : 1); --deep) {
-            if (deep == 1 && waves == 16) continue;
+            if (!few_variant(tok, waves, deep)) continue;
             const double cost = (share + deep - 1) / deep * deep * waves * factor;
             if (cost < least) least = cost, best = FewPlan{waves, deep, static_cast<int>(passes)};
         }
@@ -296,18 +303,20 @@ int launch_few(Batch b, int64_t K, int64_t passes, hipStream_t s) {
     return hipGetLastError() == hipSuccess ? UNISVQ_OK : UNISVQ_EHIP;
 }
 
+template <typename X, int TOK, int WAVES, int DEEP = 1>
+int launch_deep(const Batch& b, int64_t K, const FewPlan& p, hipStream_t s) {
+    if constexpr (DEEP <= 5) {
+        if constexpr (few_variant(TOK, WAVES, DEEP))
+            if (p.deep == DEEP) return launch_few<X, TOK, WAVES, DEEP>(b, K, p.passes, s);
+        return launch_deep<X, TOK, WAVES, DEEP + 1>(b, K, p, s);
+    }
+    return UNISVQ_EUNSUP;
+}
+
 template <typename X, int TOK>
 int launch_few(const Batch& b, int64_t K, hipStream_t s) {
     const FewPlan p = few_plan(b, K, TOK, Kind<X>::kBytes);
-    if (p.waves == 16)
-        return p.deep == 2   ? launch_few<X, TOK, 16, 2>(b, K, p.passes, s)
-               : p.deep == 3 ? launch_few<X, TOK, 16, 3>(b, K, p.passes, s)
-                             : launch_few<X, TOK, 16, 4>(b, K, p.passes, s);
-    return p.deep == 1   ? launch_few<X, TOK, 8, 1>(b, K, p.passes, s)
-           : p.deep == 2 ? launch_few<X, TOK, 8, 2>(b, K, p.passes, s)
-           : p.deep == 3 ? launch_few<X, TOK, 8, 3>(b, K, p.passes, s)
-           : p.deep == 4 ? launch_few<X, TOK, 8, 4>(b, K, p.passes, s)
-                         : launch_few<X, TOK, 8, 5>(b, K, p.passes, s);
+    return p.waves == 16 ? launch_deep<X, TOK, 16>(b, K, p, s) : launch_deep<X, TOK, 8>(b, K, p, s);
 }
 
 int tok_of(int64_t M) { return M == 1 ? 1 : M == 2 ? 2 : M <= 4 ? 4 : 8; }
