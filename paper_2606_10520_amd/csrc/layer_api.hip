@@ -10,7 +10,7 @@ namespace {
 using unisvq::FourbitProblem;
 
 constexpr int64_t kMost = (int64_t{1} << 31) - 1;
-// Columns of 4-bit weights: 64 tokens' rows stay within 32-bit offsets.
+// Columns of 4-bit weights: 128 tokens' rows stay within 32-bit offsets.
 constexpr int64_t kMostColumns = int64_t{1} << 20;
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }

@@ -192,7 +192,7 @@ __global__ __launch_bounds__(1024) void long_norm_kernel(NormArgs a) {
 #pragma unroll
                 for (int v = 0; v < 4; ++v)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) most = max(most, magnitude(h[v][i]));
+                    for (int i = 0; i < 8; ++i) most = max(most, r0 + v * 1024 + lane < runs ? magnitude(h[v][i]) : 0u);
             }
             k = row_scale(over_block(most, tops, [](uint32_t p, uint32_t q) { return max(p, q); }));
             if (lane == 0) a.scales[t] = k.scale;
