@@ -818,7 +818,8 @@ int unisvq_gated(int64_t tokens, int64_t n, const void* gate, int64_t gate_strid
  * for every row block and four groups 128 bytes, 8 a row (its groups' fp16
  * scales, zeros behind the last group).  A slot is one lane's operands of either
  * width of activations, so every load is a coalesced 16-byte-per-lane read.
- * Shapes: N % 16 == 0, K % 128 == 0; K to 2^20 (UNISVQ_EUNSUP above). */
+ * Shapes: N % 16 == 0, K % 128 == 0; K to 2^20 (UNISVQ_EUNSUP above).  What a call
+ * writes overlaps nothing else that it is given (UNISVQ_EINVAL). */
 
 /* Bytes of the packed buffer, N*K/2 + N*8*ceil(K/512); 0 for an invalid shape.
  * Host-only. */
@@ -845,10 +846,10 @@ int unisvq_fourbit_quantize(int64_t N, int64_t K, const void* W, int w_dtype, vo
  *             unisvq_rmsnorm and unisvq_gated give them).  x_scales is NULL for
  *             the 16-bit types (UNISVQ_EINVAL otherwise, and for I8 without them)
  *   y         device [M][N] contiguous, F16, BF16 or F32, whatever x is; overlaps
- *             no x, packed or other y of the call (UNISVQ_EINVAL where one starts there)
+ *             no x, x_scales, packed, workspace or other y of the call (UNISVQ_EINVAL)
  *   workspace device, >= unisvq_fourbit_gemm_workspace_bytes(N, K, M, x_dtype) bytes,
  *             16-byte aligned (UNISVQ_EWORKSPACE / UNISVQ_EALIGN); may be NULL
- *             when that size is 0.  Overwritten
+ *             when that size is 0.  Overwritten; overlaps no operand (UNISVQ_EINVAL)
  * Codes are exact operands of the matrix cores; a group's sum is fp32 (I8: an
  * exact integer), multiplied by its scale in fp32; y is rounded once.  Sums are
  * added in an order that depends on the types and shapes of the call alone (of a

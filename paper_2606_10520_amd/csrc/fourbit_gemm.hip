@@ -836,6 +836,27 @@ Plan plan_of(const FourbitProblem* probs, int count, int64_t M, bool i8) {
     return best;
 }
 
+// No output shares memory with another operand of the batch, nor does the workspace.
+// (Looked at once its size is known; a batch that fits a grid has less than 2^42 bytes of outputs.)
+bool apart(const FourbitProblem* probs, int count, int64_t M, int size, int y_dtype, const void* workspace, size_t room) {
+    const int64_t out = y_dtype == UNISVQ_F32 ? 4 : 2, ws = static_cast<int64_t>(room);
+    for (int i = 0; i < count; ++i) {
+        const int64_t y_bytes = M * probs[i].N * out;
+        if (bytes_meet(probs[i].y, y_bytes, workspace, ws)) return false;
+        for (int j = 0; j < count; ++j) {
+            const FourbitProblem& p = probs[j];
+            if (bytes_meet(probs[i].y, y_bytes, p.x, M * p.K * size) || bytes_meet(probs[i].y, y_bytes, p.x_scales, 4 * M) ||
+                bytes_meet(probs[i].y, y_bytes, p.packed, fourbit_bytes(p.N, p.K)) ||
+                (i < j && bytes_meet(probs[i].y, y_bytes, p.y, M * p.N * out)))
+                return false;
+        }
+        if (bytes_meet(workspace, ws, probs[i].x, M * probs[i].K * size) || bytes_meet(workspace, ws, probs[i].x_scales, 4 * M) ||
+            bytes_meet(workspace, ws, probs[i].packed, fourbit_bytes(probs[i].N, probs[i].K)))
+            return false;
+    }
+    return true;
+}
+
 size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 
 // A batch's workspace: sums of each distinct x, then parts of the problems whose K is split.
@@ -896,6 +917,7 @@ int launch_tiled(const FourbitProblem* probs, int count, int64_t M, int y_dtype,
         wgs += (probs[i].N + BN - 1) / BN * m_tiles * plan.splits[i];
         if (wgs >= int64_t{1} << 24) return UNISVQ_EUNSUP;  // (a grid has below 2^32 threads)
     }
+    if (!apart(probs, count, M, Kind<X>::kBytes, y_dtype, at.bytes ? workspace : nullptr, at.bytes)) return UNISVQ_EINVAL;
     tb.m_tiles = static_cast<int>(m_tiles);
     for (int i = 0; i < count; ++i)
         if (at.first[i] && !plan.sums) {
@@ -950,6 +972,7 @@ template <typename X>
 int launch_kind(const FourbitProblem* probs, int count, int64_t M, int y_dtype, uint8_t* workspace, size_t room, hipStream_t s) {
     const Way way = way_of(probs, count, M, Kind<X>::kBytes);
     if (way == kTiled) return launch_tiled<X>(probs, count, M, y_dtype, workspace, room, s);
+    if (!apart(probs, count, M, Kind<X>::kBytes, y_dtype, nullptr, 0)) return UNISVQ_EINVAL;
     Batch b{};
     b.count = count, b.y_dtype = y_dtype, b.M = M;
     int64_t most = 0;

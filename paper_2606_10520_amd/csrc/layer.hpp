@@ -48,6 +48,12 @@ hipError_t launch_fourbit_unpack(int64_t N, int64_t K, const uint8_t* packed, ui
                             hipStream_t s);
 hipError_t launch_fourbit_quantize(int64_t N, int64_t K, const void* W, int w_dtype, uint8_t* packed, hipStream_t s);
 
+// Whether na bytes at a and nb at b have one in common (absent operands have none).
+inline bool bytes_meet(const void* a, int64_t na, const void* b, int64_t nb) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+    return p && q && p < q + static_cast<uintptr_t>(nb) && q < p + static_cast<uintptr_t>(na);
+}
+
 struct FourbitProblem {
     const uint8_t* packed;
     const void* x;
@@ -57,7 +63,8 @@ struct FourbitProblem {
 };
 size_t fourbit_workspace_bytes(const FourbitProblem* probs, int count, int64_t M, int x_dtype);
 // UNISVQ_OK, UNISVQ_EWORKSPACE or UNISVQ_EALIGN (the workspace), UNISVQ_EUNSUP where
-// the launch would be too large, or UNISVQ_EHIP.
+// the launch would be too large, UNISVQ_EINVAL where an output or the workspace shares
+// memory with another operand, or UNISVQ_EHIP.
 int launch_fourbit_batch(const FourbitProblem* probs, int count, int64_t M, int x_dtype, int y_dtype, void* workspace,
                          size_t workspace_bytes, hipStream_t s);
 

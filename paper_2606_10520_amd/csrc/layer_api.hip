@@ -8,6 +8,7 @@
 namespace {
 
 using unisvq::FourbitProblem;
+using unisvq::bytes_meet;
 
 constexpr int64_t kMost = (int64_t{1} << 31) - 1;
 // Columns of 4-bit weights: 128 tokens' rows stay within 32-bit offsets.
@@ -120,6 +121,11 @@ int unisvq_fourbit_pack(int64_t N, int64_t K, const uint8_t* codes, const uint16
     if (!fourbit_shape_ok(N, K)) return UNISVQ_ESHAPE;
     if (!aligned(packed, 16) || !aligned(scales, 2) || !aligned(bad_codes, 4)) return UNISVQ_EALIGN;
     if (K > kMostColumns) return UNISVQ_EUNSUP;
+    const int64_t size = unisvq::fourbit_bytes(N, K);
+    if (bytes_meet(packed, size, codes, N * K) || bytes_meet(packed, size, scales, N * (K / unisvq::kGroup) * 2) ||
+        bytes_meet(packed, size, bad_codes, 4) || bytes_meet(bad_codes, 4, codes, N * K) ||
+        bytes_meet(bad_codes, 4, scales, N * (K / unisvq::kGroup) * 2))
+        return UNISVQ_EINVAL;
     return status(unisvq::launch_fourbit_pack(N, K, codes, scales, static_cast<uint8_t*>(packed), bad_codes,
                                          static_cast<hipStream_t>(stream)));
 }
@@ -129,6 +135,10 @@ int unisvq_fourbit_unpack(int64_t N, int64_t K, const void* packed, uint8_t* cod
     if (!fourbit_shape_ok(N, K)) return UNISVQ_ESHAPE;
     if (!aligned(packed, 16) || !aligned(scales, 2)) return UNISVQ_EALIGN;
     if (K > kMostColumns) return UNISVQ_EUNSUP;
+    const int64_t size = unisvq::fourbit_bytes(N, K), scale_bytes = N * (K / unisvq::kGroup) * 2;
+    if (bytes_meet(packed, size, codes, N * K) || bytes_meet(packed, size, scales, scale_bytes) ||
+        bytes_meet(codes, N * K, scales, scale_bytes))
+        return UNISVQ_EINVAL;
     return status(unisvq::launch_fourbit_unpack(N, K, static_cast<const uint8_t*>(packed), codes, scales,
                                            static_cast<hipStream_t>(stream)));
 }
@@ -138,6 +148,7 @@ int unisvq_fourbit_quantize(int64_t N, int64_t K, const void* W, int w_dtype, vo
     if (!fourbit_shape_ok(N, K)) return UNISVQ_ESHAPE;
     if (!aligned(packed, 16) || !aligned(W, 16)) return UNISVQ_EALIGN;
     if (K > kMostColumns) return UNISVQ_EUNSUP;
+    if (bytes_meet(packed, unisvq::fourbit_bytes(N, K), W, N * K * (w_dtype == UNISVQ_F32 ? 4 : 2))) return UNISVQ_EINVAL;
     return status(unisvq::launch_fourbit_quantize(N, K, W, w_dtype, static_cast<uint8_t*>(packed),
                                              static_cast<hipStream_t>(stream)));
 }
@@ -159,10 +170,6 @@ int unisvq_fourbit_gemm_batched(const unisvq_fourbit_problem* problems, int coun
         const int st = check_fourbit(problems[i], M, x_dtype, y_dtype);
         if (st != UNISVQ_OK) return st;
     }
-    for (int i = 0; i < count; ++i)
-        for (int j = 0; j < count; ++j)
-            if (problems[i].y == problems[j].x || problems[i].y == problems[j].packed || (i != j && problems[i].y == problems[j].y))
-                return UNISVQ_EINVAL;
     FourbitProblem p[UNISVQ_MAX_BATCH];
     fourbit_batch(problems, count, p);
     return unisvq::launch_fourbit_batch(p, count, M, x_dtype, y_dtype, workspace, workspace_bytes,
