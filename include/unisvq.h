@@ -780,11 +780,12 @@ int unisvq_attn_prompt(int64_t sequences, int64_t q_tokens, int64_t k_tokens, co
  *   residual      the stream, device [tokens][n], x_dtype or F32, or NULL;
  *   residual_out  the stream after the addition, same type: NULL exactly where
  *                 residual is.  May be residual, or x where the types are the
- *                 same, each with the same stride (UNISVQ_EINVAL otherwise), and
- *                 may not overlap an input in any other way
+ *                 same, each with the same stride, and may not overlap an input
+ *                 in any other way (UNISVQ_EINVAL)
  *   y             device [tokens][n], x_dtype, F32 or I8; may be x or residual
- *                 on the same terms, and not residual_out
- *   y_scales      device fp32 [tokens] for I8, ignored otherwise
+ *                 on the same terms, and may not overlap residual_out
+ *   y_scales      device fp32 [tokens] for I8, apart from all others (UNISVQ_EINVAL);
+ *                 ignored otherwise
  * A row whose squares' sum passes fp32's range (magnitudes of 10^18) gives zeros. */
 int unisvq_rmsnorm(int64_t tokens, int64_t n, const void* x, int64_t x_stride, int x_dtype, const void* weight,
                    int weight_dtype, float weight_offset, float eps, const void* residual, int64_t residual_stride,
@@ -801,9 +802,10 @@ typedef enum {
  *   gate, up  device [tokens][n], F16 or BF16 (the two outputs of a gate and up
  *             product, or the halves of one fused row)
  *   y         device [tokens][n], x_dtype, F32 or I8; may be gate or up with the
- *             same type and stride (UNISVQ_EINVAL otherwise), and may not overlap
- *             them in any other way
- *   y_scales  device fp32 [tokens] for I8, ignored otherwise
+ *             same type and stride, and may not overlap them in any other way
+ *             (UNISVQ_EINVAL)
+ *   y_scales  device fp32 [tokens] for I8, apart from all others (UNISVQ_EINVAL);
+ *             ignored otherwise
  * act(gate) of magnitudes below 10^-36 may be taken as 0. */
 int unisvq_gated(int64_t tokens, int64_t n, const void* gate, int64_t gate_stride, const void* up, int64_t up_stride,
                  int x_dtype, int activation, void* y, int64_t y_stride, int y_dtype, float* y_scales, void* stream);

@@ -1,5 +1,6 @@
 // C entry points of the norm, the gated activation and the 4-bit products:
 // argument validation (host only, before any HIP call) and dispatch.
+#include <algorithm>
 #include <cmath>
 #include <limits>
 
@@ -16,14 +17,56 @@ constexpr int64_t kMostColumns = int64_t{1} << 20;
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 int status(hipError_t e) { return e == hipSuccess ? UNISVQ_OK : UNISVQ_EHIP; }
+int size_of(int t) { return t == UNISVQ_I8 ? 1 : t == UNISVQ_F32 ? 4 : 2; }
 bool half_type(int t) { return t == UNISVQ_F16 || t == UNISVQ_BF16; }
 // (a single row's stride says nothing)
 bool row_aligned(const void* p, int64_t stride, int64_t tokens) { return aligned(p, 16) && (tokens <= 1 || stride % 8 == 0); }
 
-// Rows of an output lie apart, and where an input lies there they are its rows.
+// Rows of an output lie apart.
 bool rows_apart(int64_t stride, int64_t n, int64_t tokens) { return tokens <= 1 || stride >= n || stride <= -n; }
-bool in_place_ok(const void* out, int out_type, int64_t out_stride, const void* in, int type, int64_t stride, int64_t tokens) {
-    return out != in || (out_type == type && (tokens <= 1 || out_stride == stride));
+
+// An operand of rows, in bytes: `count` of `width`, `stride` apart.
+struct Rows {
+    __int128 at, stride, width, count;
+};
+Rows rows_of(const void* p, int64_t stride, int64_t n, int64_t tokens, int size) {
+    Rows r{static_cast<__int128>(reinterpret_cast<uintptr_t>(p)), static_cast<__int128>(stride) * size,
+           static_cast<__int128>(n) * size, tokens};
+    if (r.count == 1) r.stride = r.width;
+    if (r.stride < 0) r.at += (r.count - 1) * r.stride, r.stride = -r.stride;  // (their order is of no matter)
+    return r;
+}
+Rows row_of(const void* p, int64_t n, int size) { return rows_of(p, 0, n, 1, size); }
+
+// Whether the bytes from..to have one in common with a row of r.
+bool row_meets(__int128 from, __int128 to, const Rows& r) {
+    if (to <= r.at) return false;
+    // the last row that begins before `to`
+    const __int128 last = r.stride ? std::min(r.count - 1, (to - 1 - r.at) / r.stride) : 0;
+    return r.at + last * r.stride + r.width > from;
+}
+
+// Whether two operands have a byte in common (absent ones have none).  Rows of the same
+// stride meet as the first of one does with those of the other; of different ones, where
+// one operand lies about the other, they are gone through.
+bool meet(const Rows& a, const Rows& b) {
+    const __int128 a_end = a.at + (a.count - 1) * a.stride + a.width, b_end = b.at + (b.count - 1) * b.stride + b.width;
+    if (!a.at || !b.at || a_end <= b.at || b_end <= a.at) return false;
+    if (a.stride == b.stride) return row_meets(a.at, a.at + a.width, b) || row_meets(b.at, b.at + b.width, a);
+    const Rows &wide = a.stride > b.stride ? a : b, &other = a.stride > b.stride ? b : a;
+    const __int128 end = &other == &b ? b_end : a_end;
+    for (__int128 t = std::max<__int128>(0, (other.at - wide.at - wide.width) / wide.stride); t < wide.count; ++t) {
+        const __int128 from = wide.at + t * wide.stride;
+        if (from >= end) break;
+        if (row_meets(from, from + wide.width, other)) return true;
+    }
+    return false;
+}
+
+// An output lies apart from an input, or is the same rows of the same type.
+bool in_place_ok(const void* out, int out_type, int64_t out_stride, const void* in, int type, int64_t stride, int64_t n, int64_t tokens) {
+    if (out == in && out_type == type && (tokens <= 1 || out_stride == stride)) return true;
+    return !meet(rows_of(out, out_stride, n, tokens, size_of(out_type)), rows_of(in, stride, n, tokens, size_of(type)));
 }
 
 // Rows of outputs: as x, fp32, or bytes with a scale a row.
@@ -78,12 +121,24 @@ int unisvq_rmsnorm(int64_t tokens, int64_t n, const void* x, int64_t x_stride, i
         return UNISVQ_EALIGN;
     if (n % 8 != 0 || n > unisvq::kMaxRow) return UNISVQ_EUNSUP;
     if (tokens == 0) return UNISVQ_OK;
-    if (!rows_apart(y_stride, n, tokens) || !in_place_ok(y, y_dtype, y_stride, x, x_dtype, x_stride, tokens)) return UNISVQ_EINVAL;
-    if (residual && (y == residual_out || !rows_apart(residual_out_stride, n, tokens) ||
-                     !in_place_ok(y, y_dtype, y_stride, residual, residual_dtype, residual_stride, tokens) ||
-                     !in_place_ok(residual_out, residual_dtype, residual_out_stride, residual, residual_dtype, residual_stride, tokens) ||
-                     !in_place_ok(residual_out, residual_dtype, residual_out_stride, x, x_dtype, x_stride, tokens)))
-        return UNISVQ_EINVAL;
+    if (!rows_apart(y_stride, n, tokens) || !in_place_ok(y, y_dtype, y_stride, x, x_dtype, x_stride, n, tokens)) return UNISVQ_EINVAL;
+    const Rows y_rows = rows_of(y, y_stride, n, tokens, size_of(y_dtype)), w_row = row_of(weight, n, size_of(weight_dtype));
+    if (meet(y_rows, w_row)) return UNISVQ_EINVAL;
+    if (residual) {
+        const Rows h_rows = rows_of(residual_out, residual_out_stride, n, tokens, size_of(residual_dtype));
+        if (!rows_apart(residual_out_stride, n, tokens) || meet(y_rows, h_rows) || meet(h_rows, w_row) ||
+            !in_place_ok(y, y_dtype, y_stride, residual, residual_dtype, residual_stride, n, tokens) ||
+            !in_place_ok(residual_out, residual_dtype, residual_out_stride, residual, residual_dtype, residual_stride, n, tokens) ||
+            !in_place_ok(residual_out, residual_dtype, residual_out_stride, x, x_dtype, x_stride, n, tokens))
+            return UNISVQ_EINVAL;
+    }
+    if (y_dtype == UNISVQ_I8) {
+        const Rows scales = row_of(y_scales, tokens, 4);
+        if (meet(scales, y_rows) || meet(scales, w_row) || meet(scales, rows_of(x, x_stride, n, tokens, size_of(x_dtype))) ||
+            (residual && (meet(scales, rows_of(residual, residual_stride, n, tokens, size_of(residual_dtype))) ||
+                          meet(scales, rows_of(residual_out, residual_out_stride, n, tokens, size_of(residual_dtype))))))
+            return UNISVQ_EINVAL;
+    }
     return status(unisvq::launch_rmsnorm(
         unisvq::NormArgs{tokens, static_cast<int>(n), x, weight, residual, residual_out, y, x_stride, residual_stride,
                          residual_out_stride, y_stride, x_dtype, weight_dtype, residual_dtype, y_dtype, weight_offset,
@@ -102,9 +157,15 @@ int unisvq_gated(int64_t tokens, int64_t n, const void* gate, int64_t gate_strid
     if (n % 8 != 0 || (y_dtype == UNISVQ_I8 ? n > unisvq::kMaxRow : n > kMost || tokens * (n / 8) > kMost))
         return UNISVQ_EUNSUP;
     if (tokens == 0) return UNISVQ_OK;
-    if (!rows_apart(y_stride, n, tokens) || !in_place_ok(y, y_dtype, y_stride, gate, x_dtype, gate_stride, tokens) ||
-        !in_place_ok(y, y_dtype, y_stride, up, x_dtype, up_stride, tokens))
+    if (!rows_apart(y_stride, n, tokens) || !in_place_ok(y, y_dtype, y_stride, gate, x_dtype, gate_stride, n, tokens) ||
+        !in_place_ok(y, y_dtype, y_stride, up, x_dtype, up_stride, n, tokens))
         return UNISVQ_EINVAL;
+    if (y_dtype == UNISVQ_I8) {
+        const Rows scales = row_of(y_scales, tokens, 4);
+        if (meet(scales, rows_of(y, y_stride, n, tokens, 1)) || meet(scales, rows_of(gate, gate_stride, n, tokens, 2)) ||
+            meet(scales, rows_of(up, up_stride, n, tokens, 2)))
+            return UNISVQ_EINVAL;
+    }
     return status(unisvq::launch_gated(unisvq::GatedArgs{tokens, static_cast<int>(n), gate, up, y, gate_stride, up_stride,
                                                          y_stride, x_dtype, y_dtype, activation, y_scales},
                                        static_cast<hipStream_t>(stream)));
