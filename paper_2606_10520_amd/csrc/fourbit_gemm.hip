@@ -785,10 +785,14 @@ constexpr float kPaired[2][2][2][7] = {
      {{0, 0, 0, 0.70f, 0.80f, 0.95f, 0}, {0, 0, 0, 1.20f, 1.50f, 1.80f, 2.36f}}}};
 
 // The plan with the least expected time: what the workgroups take, two to a CU, or
-// the weights' read (4.2 TB/s with one to a CU, 5.8 with two); 3 to 9 us to start and
-// end; a launch for the sums of activations, where they are given; parts of K and the
-// launch that joins them. Of 25 shapes from 16 to 4096 tokens the plan took 0 to 9% more
-// than the fastest of those considered.
+// the weights' read (4.2 TB/s to 256 workgroups, 5.0 to 384, 5.8 above); 3 to 9 us to
+// start and end; a launch for the sums of activations, where they are given; parts of K
+// and the launch that joins them.  Of 162 calls of 17 to 4096 tokens the plan took at most
+// 5% more than the fastest of up to 24 others on 134, at most 10% more on 146.  The rest are
+// mostly of 1025 to 1535 workgroups, whose third round costs more than the share of a round
+// that is counted (12 of the 17 such calls more than 10%): 256 tokens of 8 bits, 22016 rows
+// of 4096, 1032 workgroups 65.9 us, tiles of 64 x 256 with given sums 41.7; of 16 bits 80.6
+// and 61.5.
 Plan plan_of(const FourbitProblem* probs, int count, int64_t M, bool i8) {
     Plan best{};
     best.us = 1e30;
@@ -949,7 +953,9 @@ int launch_tiled(const FourbitProblem* probs, int count, int64_t M, int y_dtype,
 // Which kernel serves a batch.
 // x in LDS: up to four tokens, where it fits; up to eight of 16 bits on 2048 to 4096
 // columns, of 4097 to 24576 rows (8 tokens, 8192 rows of 4096: 7.8 us, tiles 9.7; 22016
-// rows: 14.0, 16.4; 28672 rows of 2048: 10.8, 9.9; 22016 of 5120: 17.1, 16.5).
+// rows: 14.0, 16.4; 28672 rows of 2048: 10.8, 9.9; 22016 of 5120: 17.1, 16.5; 22016 of 2048:
+// 9.6, 9.9, of 1920 9.6, 9.5, and of 2176, a share of threes with a third empty, 11.2, 10.4;
+// 11008 of 2048: 7.9, 8.9, of 1920 8.0, 9.0).
 // Else up to sixteen tokens without a second launch, every workgroup with x from the L2:
 // 4096 rows while x is at most 128 KB (16 bits, 1024 rows: 16 tokens of 4096 columns 7.2 us,
 // tiles 7.0, of 6144 9.7 and 7.6; 8 of 8192 8.7 and 8.2; 8 bits, 16 of 8192 7.9 and 8.3, of

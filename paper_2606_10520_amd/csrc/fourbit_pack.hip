@@ -1,7 +1,8 @@
 // 4-bit weights on gfx950: packing, its inverse, and rounding to the nearest
 // codes.  Set-up work, once for a model's weights: simple kernels, a word of eight
 // codes a thread.  8192 x 28672: pack 105 + 11 us, unpack 152, rounding from f16 225 to
-// 250 (2.5 TB/s; an exact division for each weight).
+// 250 (2.5 TB/s; words of a line are written by threads far apart, and an exact division
+// for each weight).  A copy of the same bytes: 70, 70 and 116.
 #include <algorithm>
 
 #include "layer.hpp"
